@@ -359,6 +359,61 @@ TWIST_API twist_status twist_ce_raw(twist_ctx *ctx, void *logits, int64_t ld, co
 TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32_t B, int32_t N, const void *tok_embed, const void *pos_embed,
                                        float *x, const float *dx, float *d_tok, float *d_pos);
 
+/* Kernel-level entry points of twist_subnet_decode: the steps of generating tokens that training does not have, on the ctx's stream.  Device pointers owned
+ * by the caller, "dtype" means desc.dtype, d_head and rotary positions come from the ctx's model description.
+ *
+ * A paged cache of keys and values: pools k and v (dtype), each n_pages pages of [Hs][page_tokens][d_head] whose starts lie page_stride elements apart
+ * (at least Hs * page_tokens * d_head), as many key/value heads as query heads.  Row s of the table names the pages of sequence s in order: token p of it
+ * lies in page table[s][p / page_tokens], at place p % page_tokens.  Entries outside [0, n_pages) are pages that the sequence does not have: no key
+ * is written there, and attention sees none.  A sequence holds max_pages * page_tokens tokens at most. */
+typedef struct {
+  const int32_t *table;  /* dev [n_seqs] rows of max_pages entries, ld_table apart */
+  int64_t ld_table;
+  int32_t n_seqs, max_pages;
+  int32_t n_pages, page_tokens; /* page_tokens: a power of two, 1 to 4096 */
+} twist_pages;
+/* twist_cache_append_raw     T new tokens, rows of qkv [T, 3*Hs*d_head] (q | k | v, dtype, rows ld elements apart): row t is token lens[t] - 1 of sequence
+ *                            seq[t] (t itself with seq NULL).  Its v, and its k turned by the rotary embedding of that position (desc.use_rope; angles in
+ *                            fp64, one rounding), go to their place in the pools; its q, turned likewise, to row t of q_out (rows ldq apart; q_out may be
+ *                            the q part of qkv itself, or NULL: queries are not asked for).  Rows with lens[t] < 1 or a seq[t] outside [0, n_seqs) are
+ *                            unused ones of the batch: nothing is written for them.  Where two rows name the same token, it holds values of either.
+ * twist_cache_attention_raw  for row t of q [T, Hs*d_head] (dtype, rows ldq apart) and every head, with the scale 1/sqrt(d_head): softmax attention over
+ *                            tokens 0 .. lens[t] - 1 of sequence seq[t] (t itself with seq NULL), those on pages that it has; several rows may share a
+ *                            sequence.  o [T, Hs*d_head] (dtype, rows ldo apart), lse [T, Hs] fp32 (log-sum-exp of the scaled scores; may be NULL).  A row that
+ *                            sees no token gives o = 0, lse = -infinity; one with lens[t] < 0 or a seq[t] outside [0, n_seqs) is left as it was.  What lies
+ *                            in the pools beyond lens[t] is never used.  max_len (host): no row sees more than its first max_len tokens; kernels are
+ *                            chosen, and scratch of twist_cache_attention_floats floats is sized, by it, so a captured call serves all shorter lengths.
+ *                            scratch need not be cleared; it may be NULL where 0 floats are asked for.  fp32 scores, softmax and sums.
+ * TWIST_ESHAPE if d_head exceeds 256, strides overlap, page_tokens is none of the above or a buffer is too small. */
+TWIST_API twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages *pages, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld,
+                                              int32_t T, int32_t Hs, const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq);
+TWIST_API twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist_pages *pages, int32_t T, int32_t Hs, int32_t max_len, size_t *floats);
+TWIST_API twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pages *pages, const void *k, const void *v, int64_t page_stride, const void *q,
+                                                 int64_t ldq, int32_t T, int32_t Hs, const int32_t *seq, const int32_t *lens, int32_t max_len, void *o,
+                                                 int64_t ldo, float *lse, float *scratch, size_t scratch_floats);
+
+/* Rules that change logits before a token is drawn from them.  Any pointer may be NULL: the rule is not applied (without a history: no penalty).  Row t: */
+typedef struct {
+  const int32_t *history; /* dev [T] rows of hist_cap token ids, ld_history apart: the prompt's, then the generated ones; ids outside the vocabulary count nowhere */
+  int64_t ld_history;
+  int32_t hist_cap;
+  const int32_t *n_history; /* dev [T]: ids in row t (NULL: hist_cap), capped to hist_cap */
+  const int32_t *n_prompt;  /* dev [T]: how many of them, from the start, are the prompt's (NULL: none) */
+  const float *repetition;  /* dev [T], > 0: a token that is in the history has its logit divided by it if positive, multiplied otherwise */
+  const float *frequency;   /* dev [T]: times the number of times that the token was generated is taken off */
+  const float *presence;    /* dev [T]: taken off if the token was generated at all */
+  const int32_t *bias_ids;  /* dev [T] rows of bias_cap token ids, ld_bias apart, and what is added to their logits; an id named twice takes its last */
+  const float *bias_values; /* entry; ids outside the vocabulary count nowhere */
+  int64_t ld_bias;
+  int32_t bias_cap;
+  const int32_t *n_bias;    /* dev [T]: entries in row t (NULL: bias_cap), capped to bias_cap */
+  const uint32_t *allowed;  /* dev [T] rows of ceil(vocab / 32) words, ld_allowed apart: bit v % 32 of word v / 32 is 0 where token v is not allowed: */
+  int64_t ld_allowed;       /* its logit becomes -infinity, whatever it was */
+} twist_logit_rules;
+/* The rules in the order of their fields (repetition, frequency, presence, bias, mask) on T rows of logits [T, vocab] (dtype, rows ld apart), in fp32; out
+ * [T, vocab] fp32, rows ldo apart, receives the result; columns beyond vocab are left as they were.  fp32 models: out may be the logits themselves. */
+TWIST_API twist_status twist_logits_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t T, const twist_logit_rules *rules, float *out, int64_t ldo);
+
 /* Measurement aid for benchmarks (not part of the method): while enabled, every projection (GEMM) launch on
  * this ctx is bracketed by two HIP events on the ctx's stream.  twist_profile_gemm_read synchronises the
  * stream, returns the number of launches, their summed duration in milliseconds and their summed algorithmic

@@ -10,7 +10,7 @@ import torch
 __all__ = [
     "TwistError", "ModelDesc", "SampleDesc", "OptDesc", "lib", "Context", "Plan", "Subnet", "FullWeights",
     "LAYER_TENSORS", "GLOBAL_TENSORS", "F32", "BF16", "KIND_HEAD", "KIND_FFN", "STORE_PARAMS", "STORE_GRADS",
-    "STORE_ADAMW", "OPT_SGD", "OPT_ADAMW", "SCALE_NONE", "SCALE_SQRT_RATIO", "desc_from_cfg",
+    "STORE_ADAMW", "OPT_SGD", "OPT_ADAMW", "SCALE_NONE", "SCALE_SQRT_RATIO", "desc_from_cfg", "Pages", "PagedCache", "LogitRules",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -72,6 +72,17 @@ class WeightGrad(C.Structure):
                 ("out", C.c_void_p), ("alpha", C.c_float)]
 
 
+class PagesC(C.Structure):
+    _fields_ = [("table", C.c_void_p), ("ld_table", C.c_int64), ("n_seqs", C.c_int32), ("max_pages", C.c_int32), ("n_pages", C.c_int32),
+                ("page_tokens", C.c_int32)]
+
+
+class LogitRulesC(C.Structure):
+    _fields_ = [("history", C.c_void_p), ("ld_history", C.c_int64), ("hist_cap", C.c_int32), ("n_history", C.c_void_p), ("n_prompt", C.c_void_p),
+                ("repetition", C.c_void_p), ("frequency", C.c_void_p), ("presence", C.c_void_p), ("bias_ids", C.c_void_p), ("bias_values", C.c_void_p),
+                ("ld_bias", C.c_int64), ("bias_cap", C.c_int32), ("n_bias", C.c_void_p), ("allowed", C.c_void_p), ("ld_allowed", C.c_int64)]
+
+
 _vp, _i32, _sz = C.c_void_p, C.c_int32, C.c_size_t
 _PI32 = C.POINTER(C.c_int32)
 _SIGS = {
@@ -114,6 +125,10 @@ _SIGS = {
     "twist_act_raw": ([_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i32], _i32),
     "twist_ce_raw": ([_vp, _vp, C.c_int64, _vp, _i32, _vp, _vp], _i32),
     "twist_embed_raw": ([_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
+    "twist_cache_append_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _vp, C.c_int64], _i32),
+    "twist_cache_attention_floats": ([_vp, C.POINTER(PagesC), _i32, _i32, _i32, C.POINTER(_sz)], _i32),
+    "twist_cache_attention_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _i32, _vp, C.c_int64, _vp, _vp, _sz], _i32),
+    "twist_logits_raw": ([_vp, _vp, C.c_int64, _i32, C.POINTER(LogitRulesC), _vp, C.c_int64], _i32),
     "twist_set_kernel_choice": ([_vp, _i32, _i32, _i32], _i32),
     "twist_profile_gemm": ([_vp, _i32], _i32),
     "twist_set_overlap": ([_vp, _i32], _i32),
@@ -130,6 +145,21 @@ EXPORTS = tuple(_SIGS)
 def _ptr(t):
     """Device address of a tensor as a void pointer argument (None stays NULL)."""
     return None if t is None else _vp(t.data_ptr())
+
+
+def _addr(t):
+    """_ptr as a plain number, which ctypes takes faster (the calls of a decoding step are many and short)."""
+    return None if t is None else t.data_ptr()
+
+
+def _want(ok, message):
+    if not ok:
+        raise TwistError(1, message)
+
+
+def _ints(t, n, what, device):
+    """An optional int32 vector of n on the context's GPU."""
+    _want(t is None or (t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous() and t.device == device), f"{what}: needs a contiguous int32 vector of {n}")
 
 
 def _check(status, ctx=None):
@@ -154,6 +184,17 @@ class Context:
         _check(lib.twist_create(C.byref(desc), _vp(self.stream.cuda_stream), C.byref(h)))
         self.h = h
         self.torch_dtype = torch.bfloat16 if desc.dtype == BF16 else torch.float32
+        self.device = self.stream.device
+
+    def _call(self, f, *args, scratch=None):
+        """f(*args) on the context's GPU, also where that is not the current one; `scratch` is a tensor of the caller's current stream that the call's
+        kernels use and nobody holds afterwards."""
+        if scratch is not None and torch.cuda.current_stream(self.device) != self.stream:
+            scratch.record_stream(self.stream)
+        if torch.cuda.current_device() == self.device.index:
+            return _check(f(self.h, *args), self.h)
+        with torch.cuda.device(self.device):
+            return _check(f(self.h, *args), self.h)
 
     def close(self):
         if getattr(self, "h", None):
@@ -388,6 +429,63 @@ class Context:
         _check(lib.twist_embed_raw(self.h, _ptr(tok), B, N, _ptr(tok_embed), _ptr(pos_embed), _ptr(x), _ptr(dx), _ptr(d_tok), _ptr(d_pos)), self.h)
         return x, d_tok, d_pos
 
+    def _rows(self, t: torch.Tensor, T: int, cols: int, what: str, dtype=None) -> int:
+        """Row stride of a [T, cols] operand with contiguous rows on the context's GPU."""
+        _want(t.dtype == (dtype or self.torch_dtype) and t.dim() == 2 and t.shape[0] == T and t.shape[1] == cols and (t.stride(1) == 1 or cols == 1)
+              and t.device == self.device, f"{what}: needs [{T}, {cols}] of {dtype or self.torch_dtype} with contiguous rows on {self.device}")
+        return t.stride(0) if T > 1 else max(t.stride(0), cols)
+
+    def twist_cache_append_raw(self, cache: "PagedCache", qkv: torch.Tensor, lens: torch.Tensor, seq: torch.Tensor | None = None,
+                               q_out: torch.Tensor | None = None) -> None:
+        """Keys and values of qkv [T, 3*Hs*d_head] (q | k | v) to their places in the cache, queries to q_out [T, Hs*d_head] (or nowhere), q and k turned by the
+        rotary positions; row t is token lens[t] - 1 of sequence seq[t] (default t).  See include/twist.h."""
+        cache._fits(self)
+        T, HD = qkv.shape[0], cache.Hs * cache.d_head
+        ld = self._rows(qkv, T, 3 * HD, "qkv")
+        ldq = self._rows(q_out, T, HD, "q_out") if q_out is not None else 0
+        _ints(lens, T, "lens", self.device)
+        _ints(seq, T, "seq", self.device)
+        self._call(lib.twist_cache_append_raw, cache.pages.ref, cache.k.data_ptr(), cache.v.data_ptr(), cache.page_stride, qkv.data_ptr(), ld, T, cache.Hs, _addr(seq),
+                   lens.data_ptr(), _addr(q_out), ldq)
+
+    def twist_cache_attention_floats(self, cache: "PagedCache", T: int, max_len: int) -> int:
+        n = _sz()
+        _check(lib.twist_cache_attention_floats(self.h, cache.pages.ref, T, cache.Hs, max_len, C.byref(n)), self.h)
+        return n.value
+
+    def twist_cache_attention_raw(self, cache: "PagedCache", q: torch.Tensor, lens: torch.Tensor, max_len: int, seq: torch.Tensor | None = None,
+                                  out: torch.Tensor | None = None, lse: torch.Tensor | None = None):
+        """(o, lse): attention of q [T, Hs*d_head] over the first lens[t] <= max_len tokens of sequence seq[t] (default t) in the cache.  out and lse, where
+        given, receive the results (rows with lens[t] < 0 keep what is there).  See include/twist.h."""
+        cache._fits(self)
+        T, HD = q.shape[0], cache.Hs * cache.d_head
+        ldq = self._rows(q, T, HD, "q")
+        _ints(lens, T, "lens", self.device)
+        _ints(seq, T, "seq", self.device)
+        if out is None:
+            out = torch.empty((T, HD), dtype=self.torch_dtype, device=self.device)
+        if lse is None:
+            lse = torch.empty((T, cache.Hs), dtype=torch.float32, device=self.device)
+        _want(lse.dtype == torch.float32 and lse.shape == (T, cache.Hs) and lse.is_contiguous() and lse.device == self.device, "lse: needs a contiguous fp32 [T, Hs]")
+        ldo = self._rows(out, T, HD, "out")
+        n = self.twist_cache_attention_floats(cache, T, max_len)
+        scratch = torch.empty(n, dtype=torch.float32, device=self.device) if n else None
+        self._call(lib.twist_cache_attention_raw, cache.pages.ref, cache.k.data_ptr(), cache.v.data_ptr(), cache.page_stride, q.data_ptr(), ldq, T, cache.Hs, _addr(seq),
+                   lens.data_ptr(), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n, scratch=scratch)
+        return out, lse
+
+    def twist_logits_raw(self, logits: torch.Tensor, rules: "LogitRules", out: torch.Tensor | None = None) -> torch.Tensor:
+        """The rules applied to logits [T, vocab]; returns out, fp32 [T, vocab] (fp32 models: out may be logits).  See include/twist.h."""
+        T, V = logits.shape[0], self.desc.vocab
+        ld = self._rows(logits, T, V, "logits")
+        _want(rules.T in (None, T) and rules.device in (None, self.device) and (rules.words is None or rules.words >= (V + 31) // 32),
+              f"rules: need {T} rows on {self.device}, and a mask of {(V + 31) // 32} words a row")
+        if out is None:
+            out = torch.empty((T, V), dtype=torch.float32, device=self.device)
+        ldo = self._rows(out, T, V, "out", torch.float32)
+        self._call(lib.twist_logits_raw, logits.data_ptr(), ld, T, rules.ref, out.data_ptr(), ldo)
+        return out
+
     def twist_set_kernel_choice(self, gemm_tile: int = 0, plain_only: bool = False, staged_attention: bool = False) -> None:
         _check(lib.twist_set_kernel_choice(self.h, gemm_tile, int(plain_only), int(staged_attention)), self.h)
 
@@ -498,6 +596,59 @@ class Subnet:
             self.h = None
 
     __del__ = close
+
+
+class Pages:
+    """A page table [n_seqs, max_pages] (int32, entries outside [0, n_pages): no page) over pools of n_pages pages of page_tokens tokens."""
+
+    def __init__(self, table: torch.Tensor, n_pages: int, page_tokens: int):
+        _want(table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.is_cuda,
+              "table: needs a CUDA int32 [n_seqs, max_pages] with contiguous rows")
+        self.table, self.n_pages, self.page_tokens = table, n_pages, page_tokens
+        n_seqs, max_pages = table.shape
+        self.c = PagesC(table.data_ptr(), table.stride(0) if n_seqs > 1 else max(table.stride(0), max_pages), n_seqs, max_pages, n_pages, page_tokens)
+        self.ref = C.pointer(self.c)
+
+
+class PagedCache:
+    """Pools k, v [n_pages, Hs, page_tokens, d_head] of one layer (pages contiguous in themselves, equal strides between them) and the page table over them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        n_pages, self.Hs, page_tokens, self.d_head = k.shape
+        _want(k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device == table.device, "k and v: need one shape, type and device")
+        _want(k.numel() > 0 and k[0].is_contiguous(), "k and v: a page is contiguous")
+        self.k, self.v, self.page_stride = k, v, k.stride(0) if n_pages > 1 else k[0].numel()
+        self.pages = Pages(table, n_pages, page_tokens)
+
+    def _fits(self, ctx: Context):
+        _want(self.k.dtype == ctx.torch_dtype and self.d_head == ctx.desc.d_head and self.k.device == ctx.device, "cache: another type, head width or GPU than the context's")
+
+
+class LogitRules:
+    """What twist_logits_raw applies, in this order (every tensor optional, T rows): repetition, frequency and presence penalties (fp32 [T]) for tokens of
+    history (int32 [T, cap], of which row t uses n_history[t], the first n_prompt[t] of them prompt), bias_values (fp32) added to bias_ids (int32 [T, cap],
+    n_bias[t] of them), and the bit mask allowed (int32 [T, words])."""
+
+    def __init__(self, history=None, n_history=None, n_prompt=None, repetition=None, frequency=None, presence=None, bias_ids=None, bias_values=None, n_bias=None,
+                 allowed=None):
+        self.keep = dict(history=history, n_history=n_history, n_prompt=n_prompt, repetition=repetition, frequency=frequency, presence=presence, bias_ids=bias_ids,
+                         bias_values=bias_values, n_bias=n_bias, allowed=allowed)
+        self.T = self.device = None
+        for name, t in self.keep.items():
+            if t is None:
+                continue
+            fp, matrix = name in ("repetition", "frequency", "presence", "bias_values"), name in ("history", "bias_ids", "bias_values", "allowed")
+            _want(t.is_cuda and t.dtype == (torch.float32 if fp else torch.int32) and t.dim() == 1 + matrix and (t.shape[-1] < 2 or t.stride(-1) == 1),
+                  f"{name}: needs CUDA {'fp32' if fp else 'int32'} {'rows' if matrix else 'values'}, contiguous")
+            _want(self.T in (None, t.shape[0]) and self.device in (None, t.device), f"{name}: another number of rows or GPU than the others")
+            self.T, self.device = t.shape[0], t.device
+        ld = lambda t: 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])  # noqa: E731
+        cap = lambda t: 0 if t is None else t.shape[1]  # noqa: E731
+        _want(bias_ids is None or bias_values is None or (bias_ids.shape == bias_values.shape and ld(bias_ids) == ld(bias_values)), "biases: ids and values differ in shape")
+        self.words = None if allowed is None else allowed.shape[1]
+        self.c = LogitRulesC(_addr(history), ld(history), cap(history), _addr(n_history), _addr(n_prompt), _addr(repetition), _addr(frequency), _addr(presence),
+                             _addr(bias_ids), _addr(bias_values), ld(bias_ids), cap(bias_ids), _addr(n_bias), _addr(allowed), ld(allowed))
+        self.ref = C.pointer(self.c)
 
 
 class FullWeights:

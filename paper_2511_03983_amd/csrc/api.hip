@@ -2,6 +2,7 @@
 // turn one layer's tensors into a fused gather (dispatcher, Section 3.2) or pull-average (aggregator,
 // Section 3.3) launch.
 #include <algorithm>
+#include <cmath>
 #include <cstring>
 #include <atomic>
 #include <new>
@@ -40,6 +41,8 @@ extern "C" twist_status twist_create(const twist_model_desc *desc, void *hip_str
   if (!c) TW_FAIL(nullptr, TWIST_ENOMEM, "twist_create: out of host memory");
   c->d = d;
   c->stream = reinterpret_cast<hipStream_t>(hip_stream);
+  if (d.use_rope)
+    for (int i = 0; i < d.d_head / 2 && i < 128; ++i) c->rope_turns[i] = pow((double)d.rope_theta, -2.0 * i / d.d_head) / (2.0 * M_PI);
   *out = c;
   return TWIST_OK;
 }
