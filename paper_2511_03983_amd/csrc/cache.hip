@@ -1,5 +1,7 @@
 // The paged cache of keys and values behind twist_subnet_decode: appending to it, with the rotary embedding on the way, and attention of
 // new tokens over it.
+#include <algorithm>
+
 #include "nn.h"
 
 namespace {
@@ -22,12 +24,6 @@ template <> struct El<1> {
     static_cast<uint16_t *>(p)[i] = (uint16_t)u;
   }
 };
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
 
 // the page table as the kernels use it
 struct Pages {
@@ -91,40 +87,457 @@ __global__ __launch_bounds__(kT) void append_plain_kernel(Pages pg, void *k, voi
 }
 
 // ------------------------------------------------------------------------------------------- attention
-constexpr int kE = 4;  // d_head <= 64 * kE
+constexpr int kMaxHead = 256;
+constexpr int kMaxIds = 2048;    // pages that a part of a sequence lies on (their offsets are kept in LDS)
+constexpr int kMaxParts = 1024;  // parts of a sequence
 
-// A wave per (row, head), one key at a time, running maximum and sum of the softmax.
-template <int BF>
-__global__ __launch_bounds__(kT) void cache_attention_plain_kernel(Pages pg, const void *k, const void *v, int64_t page_stride, const void *q, int64_t ldq, int T,
-                                                                   int Hs, int dh, const int32_t *seq, const int32_t *lens, int max_len, void *o, int64_t ldo,
-                                                                   float *lse, float scale) {
-  const int64_t w = (int64_t)blockIdx.x * (kT / 64) + (threadIdx.x >> 6);
-  if (w >= (int64_t)T * Hs) return;
-  const int h = (int)(w % Hs), t = (int)(w / Hs), lane = threadIdx.x & 63, s = seq ? seq[t] : t, len = min(lens[t], max_len);
-  if (lens[t] < 0 || (unsigned)s >= (unsigned)pg.n_seqs) return;
-  float x[kE], acc[kE];
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+// value of a lane from the lane that its row of 16 (or quad) permutation names
+template <int CTRL> __device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+// sum over aligned groups of G lanes, in every lane of the group
+template <int G> __device__ __forceinline__ float group_sum(float v) {
+  if (G > 1) v += dpp<0xB1>(v);    // quad_perm 1 0 3 2
+  if (G > 2) v += dpp<0x4E>(v);    // quad_perm 2 3 0 1
+  if (G > 4) v += dpp<0x141>(v);   // row_half_mirror: the other quad of 8
+  if (G > 8) v += dpp<0x140>(v);   // row_mirror: the other 8 of 16
+  if (G > 16) v += __shfl_xor(v, 16, 64);
+  if (G > 32) v += __shfl_xor(v, 32, 64);
+  return v;
+}
+
+// 16 bytes of a row of dh elements from element e on; element by element where rows are not aligned (zeros beyond the row)
+template <int BF, bool VEC> __device__ __forceinline__ u32x4v piece(const void *p, int64_t i, int e, int dh) {
+  constexpr int N = BF ? 8 : 4;
+  if (VEC) return *reinterpret_cast<const u32x4v *>(static_cast<const char *>(p) + (i + e) * (16 / N));
+  u32x4v r = {0u, 0u, 0u, 0u};
 #pragma unroll
-  for (int j = 0; j < kE; ++j) { const int e = lane + 64 * j; x[j] = e < dh ? El<BF>::ld(q, t * ldq + (int64_t)h * dh + e) : 0.f; acc[j] = 0.f; }
-  float m = -INFINITY, l = 0.f;
-  bool any = false;
-  for (int p = 0; p < len; ++p) {
-    const int64_t at = place(pg, page_stride, s, p, h, dh);
-    if (at < 0) continue;
-    any = true;
-    float d = 0.f;
+  for (int j = 0; j < N; ++j) {
+    if (e + j < dh) {
+      if (BF) r[j / 2] |= (uint32_t) static_cast<const uint16_t *>(p)[i + e + j] << (16 * (j & 1));
+      else r[j] = static_cast<const uint32_t *>(p)[i + e + j];
+    }
+  }
+  return r;
+}
+template <int BF> __device__ __forceinline__ float value(const u32x4v &r, int j) {
+  if (BF) return __uint_as_float(j & 1 ? r[j / 2] & 0xffff0000u : r[j / 2] << 16);
+  return __uint_as_float(r[j]);
+}
+
+struct AttentionArgs {
+  Pages pg;
+  const void *k, *v, *q;
+  int64_t page_stride, ldq, ldo;
+  const int32_t *seq, *lens;
+  void *o;
+  float *lse, *acc_parts, *ml_parts;
+  int32_t T, Hs, dh, max_len, parts, chunk, turns;  // a sequence is cut into `parts` parts of `chunk` tokens
+  float scale;
+};
+
+// the end of a row: o = acc / l, and lse; `seen`: it saw a token (if only with scores of -infinity, there is no number to give)
+template <int BF> __device__ __forceinline__ void finish(const AttentionArgs &A, int t, int h, int e, float acc, float m, float l, bool seen) {
+  El<BF>::st(A.o, t * A.ldo + (int64_t)h * A.dh + e, seen ? acc / l : 0.f);
+  if (e == 0 && A.lse) A.lse[(int64_t)t * A.Hs + h] = m == -INFINITY && l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718056f;
+}
+
+// what a workgroup found of a row of unit `unit`: the result, or a part of it
+template <int BF> __device__ __forceinline__ void leave(const AttentionArgs &A, int64_t unit, int part, int t, int h, int e, float acc, float m, float l, bool seen) {
+  if (A.parts == 1) {
+    finish<BF>(A, t, h, e, acc, m, l, seen);
+  } else {
+    const int64_t at = unit * A.parts + part;
+    A.acc_parts[at * A.dh + e] = acc;
+    if (e == 0) reinterpret_cast<float2 *>(A.ml_parts)[at] = {m, seen && l == 0.f ? -1.f : l};  // (-1: tokens, but no weight)
+  }
+}
+
+// Attention of one query to the keys of its sequence: with one key/value head per query head every key and value is used once, 4 flop for its 4 bytes (bf16),
+// so reading them is the bound.  A workgroup of NW waves takes one (row, head, part).  G lanes hold a token, 16 bytes each, so a load instruction
+// fetches 64 / G whole rows; a wave has four of them for keys and four for values in flight.  Every group of G lanes runs a softmax of its own over
+// the tokens that it meets (running maximum and sum, one rescaling for four tokens), and nothing is exchanged until the end, where groups, waves
+// and (in cache_attention_join_kernel) parts are joined by the usual rule.  Scores are in base 2: q carries scale * log2(e).
+template <int BF, int G, bool VEC, int NW>
+__global__ __launch_bounds__(64 * NW) void cache_attention_kernel(AttentionArgs A) {
+  constexpr int N = BF ? 8 : 4, TPS = 64 / G, W = G * N, U = 4;
+  __shared__ int64_t ids[kMaxIds];
+  __shared__ float s_acc[NW][W], s_m[NW], s_l[NW];
+  __shared__ int s_seen[NW];
+  const int part = blockIdx.x % A.parts, unit = blockIdx.x / A.parts, h = unit % A.Hs, t = unit / A.Hs;
+  const int s = A.seq ? A.seq[t] : t, given = A.lens[t], dh = A.dh;
+  if (given < 0 || (unsigned)s >= (unsigned)A.pg.n_seqs) return;
+  const int len = min(given, A.max_len), p0 = part * A.chunk, p1 = min(p0 + A.chunk, len);
+  if (part && p0 >= len) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane / G, e = (lane % G) * N;
+  const int shift = A.pg.shift, first = p0 >> shift, n_ids = p1 > p0 ? ((p1 - 1) >> shift) - first + 1 : 0;
+  for (int i = tid; i < n_ids; i += 64 * NW) {
+    const int page = A.pg.table[s * A.pg.ld + first + i];
+    ids[i] = (unsigned)page < (unsigned)A.pg.n_pages ? page * A.page_stride + (((int64_t)h << shift)) * dh : -1;
+  }
+  float q[N], acc[N], m = -INFINITY, l = 0.f;
+  const bool active = e < dh;
+  const u32x4v qr = piece<BF, VEC>(A.q, t * A.ldq + (int64_t)h * dh, active ? e : 0, dh);
 #pragma unroll
-    for (int j = 0; j < kE; ++j) { const int e = lane + 64 * j; if (e < dh) d += x[j] * El<BF>::ld(k, at + e); }
-    d = wave_sum(d) * scale;
-    const float mn = fmaxf(m, d), ref = mn == -INFINITY ? 0.f : mn;  // scores of -infinity have no weight beside others
-    const float c = expf(m - ref), e1 = expf(d - ref);
-    l = l * c + e1;
+  for (int j = 0; j < N; ++j) { q[j] = active ? value<BF>(qr, j) * A.scale : 0.f; acc[j] = 0.f; }
+  bool seen = false;
+  __syncthreads();
+  for (int tok0 = p0 + wave * (U * TPS); tok0 < p1; tok0 += NW * U * TPS) {
+    u32x4v kr[U], vr[U];
+    bool ok[U], all = true;
 #pragma unroll
-    for (int j = 0; j < kE; ++j) { const int e = lane + 64 * j; if (e < dh) acc[j] = acc[j] * c + e1 * El<BF>::ld(v, at + e); }
+    for (int u = 0; u < U; ++u) {
+      const int tok = tok0 + u * TPS + g;
+      const int64_t base = ids[min((tok >> shift) - first, n_ids - 1)];
+      ok[u] = tok < p1 && base >= 0;
+      all &= ok[u];
+      const int64_t at = ok[u] ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0;  // (unused ones read the pool's first row)
+      kr[u] = piece<BF, VEC>(A.k, at, active ? e : 0, dh);
+      vr[u] = piece<BF, VEC>(A.v, at, active ? e : 0, dh);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (left alone, the compiler moves the values' loads behind the keys' use)
+    float sc[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float d = 0.f;
+#pragma unroll
+      for (int j = 0; j < N; ++j) d = fmaf(q[j], value<BF>(kr[u], j), d);
+      sc[u] = group_sum<G>(active ? d : 0.f);
+    }
+    if (!__all(all)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        sc[u] = ok[u] ? sc[u] : -INFINITY;
+        vr[u] = ok[u] ? vr[u] : u32x4v{0u, 0u, 0u, 0u};
+        seen |= ok[u];
+      }
+    } else {
+      seen = true;
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, sc[u]);
+    const float ref = mn == -INFINITY ? 0.f : mn, c = __builtin_amdgcn_exp2f(m - ref);
+    l *= c;
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] *= c;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float w = __builtin_amdgcn_exp2f(sc[u] - ref);
+      l += w;
+#pragma unroll
+      for (int j = 0; j < N; ++j) acc[j] = fmaf(w, value<BF>(vr[u], j), acc[j]);
+    }
     m = mn;
   }
+  // the groups of the wave
 #pragma unroll
-  for (int j = 0; j < kE; ++j) { const int e = lane + 64 * j; if (e < dh) El<BF>::st(o, t * ldo + (int64_t)h * dh + e, any ? acc[j] / l : 0.f); }
-  if (lse && lane == 0) lse[(int64_t)t * Hs + h] = m + logf(l);
+  for (int off = G; off < 64; off *= 2) {
+    const float m2 = __shfl_xor(m, off, 64), mn = fmaxf(m, m2), ref = mn == -INFINITY ? 0.f : mn;
+    const float c = __builtin_amdgcn_exp2f(m - ref), c2 = __builtin_amdgcn_exp2f(m2 - ref);
+    l = l * c + __shfl_xor(l, off, 64) * c2;
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[j] = acc[j] * c + __shfl_xor(acc[j], off, 64) * c2;
+    m = mn;
+  }
+  const bool wave_seen = __any(seen);
+  if (lane < G) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) s_acc[wave][e + j] = acc[j];
+    if (lane == 0) { s_m[wave] = m; s_l[wave] = l; s_seen[wave] = wave_seen; }
+  }
+  __syncthreads();
+  // the waves of the workgroup
+  if (tid < dh) {
+    float M = s_m[0];
+    bool any = s_seen[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) { M = fmaxf(M, s_m[w]); any |= s_seen[w]; }
+    const float ref = M == -INFINITY ? 0.f : M;
+    float L = 0.f, a = 0.f;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float c = __builtin_amdgcn_exp2f(s_m[w] - ref);
+      L += c * s_l[w];
+      a += c * s_acc[w][tid];
+    }
+    leave<BF>(A, unit, part, t, h, tid, a, M, L, any);
+  }
+}
+
+// ------------------------------------------------------------------------------------------- rows that share a sequence, bf16
+typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
+typedef short s16x4v __attribute__((ext_vector_type(4)));
+typedef short s16x8v __attribute__((ext_vector_type(8)));
+typedef float f32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
+constexpr int kTile = 16;  // rows of a group
+
+// Rows of the batch that follow each other and share a sequence (prompts, drafted tokens), up to kTile of them from a multiple of kTile on, read its keys
+// once: their scores are the 16 columns of v_mfma_f32_16x16x32_bf16.  S^T = K Q^T for two tiles of 16 tokens, the keys' fragments straight from memory: lane
+// (j = lane / 16, c = lane % 16) holds 16 bytes of token c and gets the scores of tokens 4 j .. 4 j + 3 of either tile for row c.  These eight
+// are the eight contraction indices that the lane has in O^T += V^T P^T, so the weights stay where they are; the values pass through LDS (a tile
+// of the wave's own, no barrier) and come back transposed in the same order of tokens.  Weights go in as two bf16 terms, cut off and rounded: at most 2^-16 of
+// them is lost, a fraction of the rounding of the output (2^-9).  What bounds it is the reading again, of 16 rows at once.
+template <int KS, int NW>
+__global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(AttentionArgs A) {
+  constexpr int MT = 2 * KS, RB = 64 * KS + 32, TILE_B = 32 * RB, LDR = 32 * KS + 4;  // bytes of a row of values in LDS (the padding spreads the banks), floats of one of results
+  static_assert(kTile * LDR * 4 <= TILE_B, "results take the place of the values");
+  __shared__ int64_t ids[kMaxIds];
+  __shared__ __attribute__((aligned(16))) char tiles[NW][TILE_B];
+  __shared__ float s_m[NW][kTile], s_l[NW][kTile];
+  __shared__ int s_seen[NW][kTile];
+  const int part = blockIdx.x % A.parts, turn = blockIdx.x / A.parts % A.turns, unit = blockIdx.x / A.parts / A.turns, h = unit % A.Hs, t0 = unit / A.Hs * kTile, dh = A.dh;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane >> 4, c = lane & 15;
+  // the first rows of the groups among rows t0 .. t0 + 15, of which every A.turns-th is this workgroup's
+  const int own = t0 + c < A.T ? A.seq[t0 + c] : -1, prev = __shfl_up(own, 1, 64);
+  uint32_t starts = (uint32_t)__ballot(t0 + c < A.T && (c == 0 || own != prev)) & 0xffffu;
+  for (int n = 0; starts; ++n) {
+    const int r0 = __builtin_ctz(starts), t = t0 + r0;
+    starts &= starts - 1;
+    if (n % A.turns != turn) continue;
+    const int rows = (starts ? __builtin_ctz(starts) : min(kTile, A.T - t0)) - r0;
+    const int s = __builtin_amdgcn_readfirstlane(__shfl(own, r0, 64));
+    if ((unsigned)s >= (unsigned)A.pg.n_seqs) continue;
+    const int given = c < rows ? A.lens[t + c] : -1, len = min(given, A.max_len);
+    int longest = len, shortest = c < rows ? len : INT32_MAX;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) {
+      longest = max(longest, __shfl_xor(longest, o, 64));
+      shortest = min(shortest, __shfl_xor(shortest, o, 64));
+    }
+    longest = __builtin_amdgcn_readfirstlane(longest);
+    shortest = __builtin_amdgcn_readfirstlane(shortest);
+    const int p0 = part * A.chunk, p1 = min(p0 + A.chunk, longest);
+    if (longest < 0 || (part && p0 >= longest)) continue;
+    const int shift = A.pg.shift, first = p0 >> shift, n_ids = p1 > p0 ? ((p1 - 1) >> shift) - first + 1 : 0;
+    for (int i = tid; i < n_ids; i += 64 * NW) {
+      const int page = A.pg.table[s * A.pg.ld + first + i];
+      ids[i] = (unsigned)page < (unsigned)A.pg.n_pages ? page * A.page_stride + (((int64_t)h << shift)) * dh : -1;
+    }
+    const u32x4v none = {0u, 0u, 0u, 0u};
+    const char *q = static_cast<const char *>(A.q) + ((t + min(c, rows - 1)) * A.ldq + (int64_t)h * dh) * 2;
+    u32x4v qf[KS];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) qf[k] = 32 * k + 8 * j < dh ? *reinterpret_cast<const u32x4v *>(q + 64 * k + 16 * j) : none;
+    f32x4v acc[MT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;  // of row c: the maximum of all scores, the sum of this lane's weights
+    bool seen = false;
+    char *tile = tiles[wave];
+    const int wr = c * RB + 16 * j, rd = (4 * j + (c >> 2)) * RB + (c & 3) * 8;  // where the lane's values go, and what it reads of 4 x 16 of them
+    __syncthreads();
+    for (int tok0 = p0 + 32 * wave; tok0 < p1; tok0 += 32 * NW) {
+      u32x4v kf[2][KS], vf[2][KS];
+      uint32_t there = 0;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int tok = tok0 + 16 * i + c;
+        const int64_t base = ids[min((tok >> shift) - first, n_ids - 1)];
+        const bool ok = tok < p1 && base >= 0;
+        there |= ((uint32_t)__ballot(ok) & 0xffffu) << (16 * i);
+        const int64_t at = (ok ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0) * 2 + 16 * j;  // (unused ones read the pool's first row)
+        const char *kp = static_cast<const char *>(A.k) + at, *vp = static_cast<const char *>(A.v) + at;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) kf[i][k] = 32 * k + 8 * j < dh ? *reinterpret_cast<const u32x4v *>(kp + 64 * k) : none;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) vf[i][k] = 32 * k + 8 * j < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 64 * k) : none;
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (all loads before the first product)
+      f32x4v sc[2] = {f32x4v{0.f, 0.f, 0.f, 0.f}, f32x4v{0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[i][k]), __builtin_bit_cast(bf16x8v, qf[k]), sc[i], 0, 0, 0);
+      const bool whole = there == 0xffffffffu && tok0 + 32 <= shortest;
+      uint32_t on = 0xffu;  // which of the lane's eight tokens its row sees
+      if (!whole) {
+        on = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const int tok = 16 * (e >> 2) + 4 * j + (e & 3);
+          if ((there >> tok & 1) && tok0 + tok < len) on |= 1u << e;
+          else sc[e >> 2][e & 3] = -INFINITY;
+        }
+      }
+      seen |= on != 0;
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
+      if (__any(mn > m)) {
+        const float alpha = __builtin_amdgcn_exp2f((m - ref) * A.scale);
+        l *= alpha;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) acc[i] *= alpha;
+        m = mn;
+      }
+      float p[8];
+      u32x4v hi, lo;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        p[e] = __builtin_amdgcn_exp2f((sc[e >> 2][e & 3] - ref) * A.scale);
+        l += p[e];
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t a = __float_as_uint(p[2 * e]), b = __float_as_uint(p[2 * e + 1]);
+        hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
+        typedef float f32x2 __attribute__((ext_vector_type(2)));
+        const f32x2 rest = {p[2 * e] - __uint_as_float(a & 0xffff0000u), p[2 * e + 1] - __uint_as_float(b & 0xffff0000u)};
+        lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
+      }
+      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 top = {0, 0};  // largest magnitude among the values
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+          *reinterpret_cast<u32x4v *>(tile + 16 * i * RB + wr + 64 * k) = vf[i][k];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[i][k][e] & 0x7fff7fffu));
+        }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // read by the wave's other lanes
+      if (!__any(top.x >= 0x7f80 || top.y >= 0x7f80)) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          typedef s16x4v __attribute__((address_space(3))) * lds_ptr;
+          const s16x4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + rd + 32 * i)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + 16 * RB + rd + 32 * i));
+          const bf16x8v vt = __builtin_bit_cast(bf16x8v, s16x8v{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, hi), acc[i], 0, 0, 0);
+          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, lo), acc[i], 0, 0, 0);
+        }
+      } else {  // infinities and NaNs, which times the zero of a term or of a hidden token are no number: one by one, for the rows that see them
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+          for (int x = 0; x < 4; ++x) {
+            const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
+            const float w = __shfl(p[e], 16 * x + c, 64);
+            if (!(there >> tok & 1) || tok0 + tok >= len) continue;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+              const u32x2v u = *reinterpret_cast<const u32x2v *>(tile + tok * RB + 32 * i + 8 * j);
+              acc[i][0] = fmaf(w, __uint_as_float(u.x << 16), acc[i][0]);
+              acc[i][1] = fmaf(w, __uint_as_float(u.x & 0xffff0000u), acc[i][1]);
+              acc[i][2] = fmaf(w, __uint_as_float(u.y << 16), acc[i][2]);
+              acc[i][3] = fmaf(w, __uint_as_float(u.y & 0xffff0000u), acc[i][3]);
+            }
+          }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next tokens' values take the place of these
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+    const uint64_t any = __ballot(seen);
+    float *res = reinterpret_cast<float *>(tile);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4v *>(res + c * LDR + 16 * i + 4 * j) = acc[i];
+    if (j == 0) { s_m[wave][c] = m; s_l[wave][c] = l; s_seen[wave][c] = (any >> c | any >> (c + 16) | any >> (c + 32) | any >> (c + 48)) & 1; }
+    __syncthreads();
+    for (int i = tid; i < rows * dh; i += 64 * NW) {
+      const int r = i / dh, e = i - r * dh, row_len = A.lens[t + r];
+      if (row_len < 0 || (part && p0 >= min(row_len, A.max_len))) continue;
+      float M = s_m[0][r];
+      bool some = s_seen[0][r];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) { M = fmaxf(M, s_m[w][r]); some |= s_seen[w][r]; }
+      const float ref = M == -INFINITY ? 0.f : M;
+      float L = 0.f, a = 0.f;
+#pragma unroll
+      for (int w = 0; w < NW; ++w) {
+        const float x = __builtin_amdgcn_exp2f((s_m[w][r] - ref) * A.scale);
+        L += x * s_l[w][r];
+        a += x * reinterpret_cast<const float *>(tiles[w])[r * LDR + e];
+      }
+      leave<1>(A, (int64_t)(t + r) * A.Hs + h, part, t + r, h, e, a, M * A.scale, L, some);
+    }
+    __syncthreads();
+  }
+}
+
+// Joins the parts of a (row, head): parts with m = maximum, l = sum of weights against it, acc likewise.  A thread takes an element of every
+// (kT / D)-th part, D the power of two that holds a head, with its loads in flight together; the threads of an element are added in a fixed order.
+template <int BF>
+__global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs A, int dlog) {
+  __shared__ float s_w[kMaxParts], s_l[kT / 64], s_m[kT / 64], s_a[kT];
+  __shared__ int s_seen[kT / 64];
+  const int unit = blockIdx.x, h = unit % A.Hs, t = unit / A.Hs, s = A.seq ? A.seq[t] : t, given = A.lens[t], tid = threadIdx.x;
+  if (given < 0 || (unsigned)s >= (unsigned)A.pg.n_seqs) return;
+  const int len = min(given, A.max_len), n = max(1, (len + A.chunk - 1) / A.chunk);
+  const float2 *ml = reinterpret_cast<const float2 *>(A.ml_parts) + (int64_t)unit * A.parts;
+  const float *parts = A.acc_parts + (int64_t)unit * A.parts * A.dh;
+  float2 own[kMaxParts / kT];
+  float M = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < kMaxParts / kT; ++j) {
+    const int i = tid + j * kT;
+    own[j] = i < n ? ml[i] : float2{-INFINITY, 0.f};
+    M = fmaxf(M, own[j].x);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  if ((tid & 63) == 0) s_m[tid >> 6] = M;
+  __syncthreads();
+  M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+  const float ref = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  bool any = false;
+#pragma unroll
+  for (int j = 0; j < kMaxParts / kT; ++j) {
+    const int i = tid + j * kT;
+    const float w = __builtin_amdgcn_exp2f(own[j].x - ref);
+    if (i < n) s_w[i] = w;
+    L += w * own[j].y;
+    any |= own[j].y != 0.f;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) L += __shfl_xor(L, o, 64);
+  any = __any(any);
+  if ((tid & 63) == 0) { s_l[tid >> 6] = L; s_seen[tid >> 6] = any; }
+  __syncthreads();
+  L = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+  any = s_seen[0] | s_seen[1] | s_seen[2] | s_seen[3];
+  const int D = 1 << dlog, e = tid & (D - 1);
+  float a = 0.f;
+  if (e < A.dh) {
+#pragma unroll 4
+    for (int i = tid >> dlog; i < n; i += kT >> dlog) a += s_w[i] * parts[(int64_t)i * A.dh + e];
+  }
+  s_a[tid] = a;
+  __syncthreads();
+  if (tid >= A.dh) return;
+  for (int i = 1; i < kT >> dlog; ++i) a += s_a[(i << dlog) + tid];
+  finish<BF>(A, t, h, tid, a, M, L, any);
+}
+
+// Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens (row_bytes: of a head's key).  Figures
+// are us on the device, launch included.
+//  - Tiles (turns > 0): where there are at least twice as many rows as sequences, so that most of them must share one.  A workgroup takes every turns-th
+//    group among 16 rows.  bf16, heads of 128, tiles / rows by themselves: 16 x 4 rows over 2000 tokens, 16 heads 44 / 68, 16 x 8 over 8000 152 / 351,
+//    a prompt of 1000, 8 heads 40 / 173; one row a sequence, 16 x 16384, 32 heads 527 / 507, 1 x 1000, 12 heads of 64 11.5 / 7.1.
+//  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42 (one row of one head of 16384 x 128 bf16 alone); 256 of either draw what the HBM gives.  Rows that
+//    cannot feed 16 waves take 4.  16 / 4 waves: 4 heads of 64 over 20 tokens 4.6 / 3.8, 12 over 1000 7.1 / 8.1, 96 over 1000 8.4 / 10.4; heads of 128: 2048
+//    over 200 39 / 29, 1024 over 1000 62 / 64, 256 over 2048 37.5 / 38.6.
+//  - Where there are fewer of them than CUs, a sequence is cut, into parts of 512 KB at least (6 us of a workgroup's reading; the second launch, which joins
+//    them, costs 4): 16 heads of 128 over 32768 tokens in parts of 256 / 1024 / 2048: 58 / 54.8 / 53.3.
+struct Split { int waves, parts, chunk, turns; };
+Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int row_bytes, bool tiles) {
+  Split s;
+  s.turns = tiles && T >= 2 * (int64_t)n_seqs ? std::min(8, std::max(1, (int)((int64_t)kTile * n_seqs / T))) : 0;
+  const int64_t units = (int64_t)(s.turns ? (T + kTile - 1) / kTile * s.turns : T) * Hs, want = std::max<int64_t>(1, 256 / units), least = std::max(64, (256 << 10) / row_bytes);
+  int64_t c = std::max<int64_t>(least, (max_len + want - 1) / want);
+  c = std::max<int64_t>(c, (max_len + kMaxParts - 1) / kMaxParts);
+  c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)kMaxIds << shift);
+  s.waves = (int64_t)max_len * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
+  s.chunk = (int)c;
+  s.parts = (int)((max_len + c - 1) / c);
+  return s;
 }
 
 twist_status check_pages(twist_ctx *ctx, const char *who, const twist_pages *p) {
@@ -133,7 +546,7 @@ twist_status check_pages(twist_ctx *ctx, const char *who, const twist_pages *p) 
   if (p->ld_table < p->max_pages) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows of the page table overlap", who);
   if (p->page_tokens < 1 || p->page_tokens > 4096 || (p->page_tokens & (p->page_tokens - 1)))
     TW_FAIL(ctx, TWIST_ESHAPE, "%s: page_tokens=%d is not a power of two up to 4096", who, p->page_tokens);
-  if ((int64_t)p->max_pages * p->page_tokens > INT32_MAX) TW_FAIL(ctx, TWIST_ESHAPE, "%s: positions beyond 2^31", who);
+  if ((int64_t)p->max_pages * p->page_tokens > (int64_t)1 << 30) TW_FAIL(ctx, TWIST_ESHAPE, "%s: a sequence has room for 2^30 tokens at most", who);
   return TWIST_OK;
 }
 
@@ -142,8 +555,8 @@ twist_status check_cache(twist_ctx *ctx, const char *who, const twist_pages *p, 
   TW_TRY(check_pages(ctx, who, p));
   const int64_t dh = ctx->d.d_head;
   if (T < 1 || Hs < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: empty input", who);
-  if (dh > 64 * kE) TW_FAIL(ctx, TWIST_ESHAPE, "%s: d_head=%lld above %d is not supported", who, (long long)dh, 64 * kE);
-  if ((int64_t)T * Hs > (int64_t)1 << 24 || Hs > 65535) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads are too many for one call", who, T, Hs);
+  if (dh > kMaxHead) TW_FAIL(ctx, TWIST_ESHAPE, "%s: d_head=%lld above %d is not supported", who, (long long)dh, kMaxHead);
+  if ((int64_t)T * Hs > (int64_t)1 << 22) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads are too many for one call", who, T, Hs);
   if (page_stride < Hs * dh * p->page_tokens) TW_FAIL(ctx, TWIST_ESHAPE, "%s: page_stride=%lld is less than a page", who, (long long)page_stride);
   return TWIST_OK;
 }
@@ -151,6 +564,58 @@ twist_status check_cache(twist_ctx *ctx, const char *who, const twist_pages *p, 
 Pages device_pages(const twist_pages *p) {
   return {p->table, p->ld_table, p->n_seqs, p->max_pages, p->n_pages, __builtin_ctz((unsigned)p->page_tokens)};
 }
+
+Split attention_split(const twist_ctx *ctx, const twist_pages *p, int T, int Hs, int &max_len, bool seq) {
+  max_len = (int)std::min<int64_t>(max_len, (int64_t)p->max_pages * p->page_tokens);
+  return choose_split(T, p->n_seqs, Hs, max_len, __builtin_ctz((unsigned)p->page_tokens), ctx->d.d_head * ctx->esize(),
+                      seq && ctx->d.dtype == TWIST_BF16 && ctx->d.d_head % 8 == 0);
+}
+
+void launch_attention_join(int bf16, hipStream_t st, const AttentionArgs &a) {
+  int dlog = 0;
+  while (1 << dlog < a.dh) ++dlog;
+  if (bf16) hipLaunchKernelGGL((cache_attention_join_kernel<1>), dim3((unsigned)(a.T * a.Hs)), dim3(kT), 0, st, a, dlog);
+  else hipLaunchKernelGGL((cache_attention_join_kernel<0>), dim3((unsigned)(a.T * a.Hs)), dim3(kT), 0, st, a, dlog);
+}
+template <int BF, int G, bool VEC>
+void launch_attention(hipStream_t st, const AttentionArgs &a, int waves) {
+  const dim3 grid((unsigned)((int64_t)a.T * a.Hs * a.parts));
+  if (waves == 16) hipLaunchKernelGGL((cache_attention_kernel<BF, G, VEC, 16>), grid, dim3(1024), 0, st, a);
+  else hipLaunchKernelGGL((cache_attention_kernel<BF, G, VEC, 4>), grid, dim3(256), 0, st, a);
+}
+template <int BF, bool VEC>
+void launch_attention_of(hipStream_t st, const AttentionArgs &a, int waves) {
+  const int pieces = (a.dh + (BF ? 7 : 3)) / (BF ? 8 : 4);
+  if (pieces <= 1) launch_attention<BF, 1, VEC>(st, a, waves);
+  else if (pieces <= 2) launch_attention<BF, 2, VEC>(st, a, waves);
+  else if (pieces <= 4) launch_attention<BF, 4, VEC>(st, a, waves);
+  else if (pieces <= 8) launch_attention<BF, 8, VEC>(st, a, waves);
+  else if (pieces <= 16) launch_attention<BF, 16, VEC>(st, a, waves);
+  else if (pieces <= 32) launch_attention<BF, 32, VEC>(st, a, waves);
+  else if constexpr (!BF) launch_attention<BF, 64, VEC>(st, a, waves);
+  if (a.parts > 1) launch_attention_join(BF, st, a);
+}
+
+template <int KS>
+void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a) {
+  constexpr int NW = KS > 4 ? 4 : 8;
+  hipLaunchKernelGGL((cache_attention_tile_kernel<KS, NW>), dim3((unsigned)((int64_t)((a.T + kTile - 1) / kTile) * a.turns * a.Hs * a.parts)), dim3(64 * NW), 0, st, a);
+}
+void launch_attention_tile(hipStream_t st, const AttentionArgs &a) {
+  switch ((a.dh + 31) / 32) {
+    case 1: launch_attention_tile_of<1>(st, a); break;
+    case 2: launch_attention_tile_of<2>(st, a); break;
+    case 3: launch_attention_tile_of<3>(st, a); break;
+    case 4: launch_attention_tile_of<4>(st, a); break;
+    case 5: launch_attention_tile_of<5>(st, a); break;
+    case 6: launch_attention_tile_of<6>(st, a); break;
+    case 7: launch_attention_tile_of<7>(st, a); break;
+    default: launch_attention_tile_of<8>(st, a); break;
+  }
+  if (a.parts > 1) launch_attention_join(1, st, a);
+}
+
+bool al16(const void *p, int64_t stride_bytes = 0) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0; }
 
 }  // namespace
 
@@ -181,7 +646,15 @@ extern "C" twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist
   if (!ctx || !floats) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
   TW_TRY(check_cache(ctx, who, pages, INT64_MAX, T, Hs));
   if (max_len < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: max_len=%d", who, max_len);
-  *floats = 0;
+  size_t need = 0;
+  for (int seq = 0; seq < 2; ++seq) {  // the caller's rows may share sequences, or not
+    int most = max_len;
+    const Split s = attention_split(ctx, pages, T, Hs, most, seq);
+    if (s.parts > kMaxParts || (int64_t)T * Hs * s.parts > (int64_t)1 << 22)
+      TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
+    if (s.parts > 1) need = std::max(need, (size_t)T * Hs * s.parts * (ctx->d.d_head + 2));
+  }
+  *floats = need;
   return TWIST_OK;
 }
 
@@ -194,19 +667,31 @@ extern "C" twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pa
   size_t need = 0;
   TW_TRY(twist_cache_attention_floats(ctx, pages, T, Hs, max_len, &need));
   if (need && !scratch) TW_FAIL(ctx, TWIST_EINVAL, "%s: null scratch", who);
+  if (reinterpret_cast<uintptr_t>(scratch) % 16) TW_FAIL(ctx, TWIST_ESHAPE, "%s: scratch must be 16-byte aligned", who);
   if (scratch_floats < need) TW_FAIL(ctx, TWIST_ESHAPE, "%s: scratch of %zu floats is smaller than the %zu needed", who, scratch_floats, need);
   const int dh = ctx->d.d_head;
   const int64_t HD = (int64_t)Hs * dh;
   if (ldq < HD || ldo < HD) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows overlap", who);
-  const Pages pg = device_pages(pages);
-  const int64_t cap = (int64_t)pages->max_pages * pages->page_tokens;
-  if (max_len > cap) max_len = (int32_t)cap;
-  const dim3 grid((unsigned)(((int64_t)T * Hs + 3) / 4));
-  const float scale = 1.f / sqrtf((float)dh);
-  if (ctx->d.dtype == TWIST_BF16)
-    hipLaunchKernelGGL((cache_attention_plain_kernel<1>), grid, dim3(kT), 0, ctx->stream, pg, k, v, page_stride, q, ldq, T, Hs, dh, seq, lens, max_len, o, ldo, lse, scale);
-  else
-    hipLaunchKernelGGL((cache_attention_plain_kernel<0>), grid, dim3(kT), 0, ctx->stream, pg, k, v, page_stride, q, ldq, T, Hs, dh, seq, lens, max_len, o, ldo, lse, scale);
+  AttentionArgs a{};
+  a.pg = device_pages(pages);
+  a.k = k; a.v = v; a.q = q; a.o = o;
+  a.page_stride = page_stride; a.ldq = ldq; a.ldo = ldo;
+  a.seq = seq; a.lens = lens; a.lse = lse;
+  a.T = T; a.Hs = Hs; a.dh = dh; a.max_len = max_len;
+  const Split split = attention_split(ctx, pages, T, Hs, a.max_len, seq != nullptr);
+  a.turns = split.turns; a.parts = split.parts; a.chunk = split.chunk;
+  a.ml_parts = scratch;
+  a.acc_parts = need ? scratch + (size_t)T * Hs * a.parts * 2 : nullptr;
+  a.scale = 1.44269504089f / sqrtf((float)dh);
+  const int es = ctx->esize();
+  const bool vec = dh * es % 16 == 0 && al16(k, page_stride * es) && al16(v) && al16(q, ldq * es);
+  if (split.turns && vec) {
+    launch_attention_tile(ctx->stream, a);
+    TW_HIP(ctx, hipGetLastError());
+    return TWIST_OK;
+  }
+  if (ctx->d.dtype == TWIST_BF16) { if (vec) launch_attention_of<1, true>(ctx->stream, a, split.waves); else launch_attention_of<1, false>(ctx->stream, a, split.waves); }
+  else { if (vec) launch_attention_of<0, true>(ctx->stream, a, split.waves); else launch_attention_of<0, false>(ctx->stream, a, split.waves); }
   TW_HIP(ctx, hipGetLastError());
   return TWIST_OK;
 }

@@ -194,6 +194,8 @@ def test_append_of_many_rows(lib):
 # ------------------------------------------------------------------------------------------------ attention
 def _attention_want(k, v, table, q, lens, seq, max_len, Hs, dh):
     """(o, lse, bound of o beside its rounding, bound of lse), 64 bits; rows that are left alone are NaN."""
+    # rows with a list of sequences, bf16: weights in two bf16 terms, the first cut off (what is left is below 2^-7 of the weight), the second rounded (2^-9)
+    terms = 2.0 ** -16 if seq is not None and k.dtype == torch.bfloat16 else 0.0
     n_pages, _, page, _ = k.shape
     T = q.shape[0]
     o = torch.full((T, Hs * dh), NAN, dtype=torch.float64)
@@ -221,7 +223,7 @@ def _attention_want(k, v, table, q, lens, seq, max_len, Hs, dh):
         # magnitudes; a sum over n keys: n + 8 roundings, of the softmax's sum and of the output's alike
         mag = (kk * qq).abs().sum(-1) / math.sqrt(dh)
         ds = (dh + 4) * E24 * mag.amax(0) + 2.0 ** -22                                  # [Hs]
-        rel = 2 * ds + 2 * (len(pos) + 8) * E24
+        rel = 2 * ds + 2 * (len(pos) + 8) * E24 + terms
         eo[t] = (rel[:, None] * (p[..., None] * vv.abs()).sum(0)).reshape(-1)
         el[t] = ds + (len(pos) + 8) * E24 + lse[t].abs() * 2.0 ** -23
     return o, lse, eo, el
@@ -290,12 +292,45 @@ def test_attention_over_long_sequences_of_few_rows(lib, dtype, Hs, dh, page, T, 
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_attention_of_rows_that_share_sequences(lib, dtype):
+@pytest.mark.parametrize("Hs,dh,page", [(2, 128, 16), (3, 64, 16), (2, 32, 8), (1, 256, 16), (3, 40, 32), (2, 80, 16), (1, 96, 64), (2, 20, 8), (1, 8, 1), (1, 160, 16), (1, 192, 16), (1, 224, 16)])
+def test_attention_of_rows_that_share_sequences(lib, dtype, Hs, dh, page):
+    """Runs of rows of one sequence that start and end anywhere, in any order of lengths, beside rows of their own and unused ones; NaN behind each sequence."""
     lens = [97, 98, 99, 100, 1, 2, 3, 40, 41, 0, 50, 50, -1]
     seq = [0, 0, 0, 0, 2, 2, 2, 1, 1, 1, 7, -1, 0]
-    _check_attention(lib, dtype, 3, 64, 16, lens, seq, n_seqs=3, poison=False)
-    _check_attention(lib, dtype, 2, 128, 16, list(range(1, 71)), [0] * 70, n_seqs=1)       # a whole prompt at once
-    _check_attention(lib, dtype, 2, 80, 8, list(range(1, 71)), [1] * 70, n_seqs=2)
+    _check_attention(lib, dtype, Hs, dh, page, lens, seq, n_seqs=3)
+    _check_attention(lib, dtype, Hs, dh, page, list(range(1, 71)), [0] * 70, n_seqs=1)       # a whole prompt at once
+    _check_attention(lib, dtype, Hs, dh, page, list(range(230, 195, -1)) + [-1, 0, 3], [1] * 38, n_seqs=2)
+    _check_attention(lib, dtype, Hs, dh, page, [1, 64, 65, 200, 0, 31, 32, 33, 16, 17, 300], list(range(11)), n_seqs=11)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hs,dh", [(1, 128), (2, 64), (1, 40)])
+def test_attention_of_drafts_over_long_sequences(lib, dtype, Hs, dh):
+    """Rows of one sequence whose last parts only some of them reach, missing pages among them."""
+    _check_attention(lib, dtype, Hs, dh, 16, [4500, 4501, 4502, 4503, 4096, 4097, 1], [0] * 7, n_seqs=1)
+    _check_attention(lib, dtype, Hs, dh, 16, [4500, 4501, 60, 2500, 2501], [1, 1, 1, 0, 0], n_seqs=2, holes=[(1, 3), (1, 200), (0, 0)] + [(1, i) for i in range(64, 128)])
+
+
+def test_attention_of_values_that_are_no_numbers(lib):
+    """An infinity reaches the rows that see it and no others, also where their scores leave nothing of a term of its weight."""
+    ctx, g, dh = _ctx(lib, BF, 64), _gen(8), 64
+    k, v = _pools(g, 8, 1, 16, dh, BF)
+    table = torch.arange(8, dtype=torch.int32, device="cuda").view(1, -1)
+    cache = lib.PagedCache(k, v, table)
+    q = torch.zeros((4, dh), dtype=torch.bfloat16, device="cuda")
+    lens, seq = _i32(40, 41, 100, 128), _i32(0, 0, 0, 0)
+    base, _ = ctx.twist_cache_attention_raw(cache, q, lens, 128, seq=seq)
+    v[2, 0, 8, 5] = INF                                    # token 40: the last of row 1, none of row 0
+    v[6, 0, 2, 7] = -INF                                   # token 98
+    v[6, 0, 5, 9] = NAN                                    # token 101: row 3 only
+    o, lse = ctx.twist_cache_attention_raw(cache, q, lens, 128, seq=seq)
+    torch.cuda.synchronize()
+    assert torch.equal(o[0], base[0])
+    assert (o[1:, 5] == INF).all() and torch.isfinite(o[1, 7]) and (o[2:, 7] == -INF).all()
+    assert torch.isfinite(o[:3, 9]).all() and torch.isnan(o[3, 9])
+    rest = [e for e in range(dh) if e not in (5, 7, 9)]
+    # (such tokens go another way through the kernel: equal up to the 2^-16 of the weights' terms and one rounding)
+    assert ((o - base).float().abs()[:, rest] <= 2.0 ** -7 * base.float().abs()[:, rest] + 2.0 ** -15).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
