@@ -152,14 +152,17 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-def _want(ok, message):
-    if not ok:
-        raise TwistError(1, message)
+def _refuse(message):
+    raise TwistError(1, message)
 
 
-def _ints(t, n, what, device):
-    """An optional int32 vector of n on the context's GPU."""
-    _want(t is None or (t.dtype == torch.int32 and t.shape == (n,) and t.is_contiguous() and t.device == device), f"{what}: needs a contiguous int32 vector of {n}")
+def _ints(t, n, what, index):
+    """Address of an int32 vector of n on GPU `index` (None stays NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != index:
+        _refuse(f"{what}: needs a contiguous int32 vector of {n} on GPU {index}")
+    return t.data_ptr()
 
 
 def _check(status, ctx=None):
@@ -185,16 +188,20 @@ class Context:
         self.h = h
         self.torch_dtype = torch.bfloat16 if desc.dtype == BF16 else torch.float32
         self.device = self.stream.device
+        self.gpu = self.device.index
 
     def _call(self, f, *args, scratch=None):
         """f(*args) on the context's GPU, also where that is not the current one; `scratch` is a tensor of the caller's current stream that the call's
         kernels use and nobody holds afterwards."""
         if scratch is not None and torch.cuda.current_stream(self.device) != self.stream:
             scratch.record_stream(self.stream)
-        if torch.cuda.current_device() == self.device.index:
-            return _check(f(self.h, *args), self.h)
-        with torch.cuda.device(self.device):
-            return _check(f(self.h, *args), self.h)
+        if torch.cuda.current_device() == self.gpu:
+            status = f(self.h, *args)
+        else:
+            with torch.cuda.device(self.device):
+                status = f(self.h, *args)
+        if status:
+            _check(status, self.h)
 
     def close(self):
         if getattr(self, "h", None):
@@ -429,11 +436,12 @@ class Context:
         _check(lib.twist_embed_raw(self.h, _ptr(tok), B, N, _ptr(tok_embed), _ptr(pos_embed), _ptr(x), _ptr(dx), _ptr(d_tok), _ptr(d_pos)), self.h)
         return x, d_tok, d_pos
 
-    def _rows(self, t: torch.Tensor, T: int, cols: int, what: str, dtype=None) -> int:
+    def _rows(self, t: torch.Tensor, T: int, cols: int, what: str, dtype) -> int:
         """Row stride of a [T, cols] operand with contiguous rows on the context's GPU."""
-        _want(t.dtype == (dtype or self.torch_dtype) and t.dim() == 2 and t.shape[0] == T and t.shape[1] == cols and (t.stride(1) == 1 or cols == 1)
-              and t.device == self.device, f"{what}: needs [{T}, {cols}] of {dtype or self.torch_dtype} with contiguous rows on {self.device}")
-        return t.stride(0) if T > 1 else max(t.stride(0), cols)
+        stride = t.stride()
+        if t.dtype is not dtype or t.shape != (T, cols) or (stride[1] != 1 and cols > 1) or t.get_device() != self.gpu:
+            _refuse(f"{what}: needs [{T}, {cols}] of {dtype} with contiguous rows on {self.device}")
+        return stride[0] if T > 1 or stride[0] > cols else cols
 
     def twist_cache_append_raw(self, cache: "PagedCache", qkv: torch.Tensor, lens: torch.Tensor, seq: torch.Tensor | None = None,
                                q_out: torch.Tensor | None = None) -> None:
@@ -441,12 +449,10 @@ class Context:
         rotary positions; row t is token lens[t] - 1 of sequence seq[t] (default t).  See include/twist.h."""
         cache._fits(self)
         T, HD = qkv.shape[0], cache.Hs * cache.d_head
-        ld = self._rows(qkv, T, 3 * HD, "qkv")
-        ldq = self._rows(q_out, T, HD, "q_out") if q_out is not None else 0
-        _ints(lens, T, "lens", self.device)
-        _ints(seq, T, "seq", self.device)
-        self._call(lib.twist_cache_append_raw, cache.pages.ref, cache.k.data_ptr(), cache.v.data_ptr(), cache.page_stride, qkv.data_ptr(), ld, T, cache.Hs, _addr(seq),
-                   lens.data_ptr(), _addr(q_out), ldq)
+        ld = self._rows(qkv, T, 3 * HD, "qkv", self.torch_dtype)
+        ldq = self._rows(q_out, T, HD, "q_out", self.torch_dtype) if q_out is not None else 0
+        self._call(lib.twist_cache_append_raw, cache.pages.ref, cache.k_addr, cache.v_addr, cache.page_stride, qkv.data_ptr(), ld, T, cache.Hs,
+                   _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), _addr(q_out), ldq)
 
     def twist_cache_attention_floats(self, cache: "PagedCache", T: int, max_len: int) -> int:
         n = _sz()
@@ -459,30 +465,35 @@ class Context:
         given, receive the results (rows with lens[t] < 0 keep what is there).  See include/twist.h."""
         cache._fits(self)
         T, HD = q.shape[0], cache.Hs * cache.d_head
-        ldq = self._rows(q, T, HD, "q")
-        _ints(lens, T, "lens", self.device)
-        _ints(seq, T, "seq", self.device)
+        ldq = self._rows(q, T, HD, "q", self.torch_dtype)
         if out is None:
-            out = torch.empty((T, HD), dtype=self.torch_dtype, device=self.device)
+            out, ldo = torch.empty((T, HD), dtype=self.torch_dtype, device=self.device), HD
+        else:
+            ldo = self._rows(out, T, HD, "out", self.torch_dtype)
         if lse is None:
             lse = torch.empty((T, cache.Hs), dtype=torch.float32, device=self.device)
-        _want(lse.dtype == torch.float32 and lse.shape == (T, cache.Hs) and lse.is_contiguous() and lse.device == self.device, "lse: needs a contiguous fp32 [T, Hs]")
-        ldo = self._rows(out, T, HD, "out")
-        n = self.twist_cache_attention_floats(cache, T, max_len)
+        elif self._rows(lse, T, cache.Hs, "lse", torch.float32) != cache.Hs:
+            _refuse("lse: needs rows without padding")
+        n = cache.floats.get((T, max_len))
+        if n is None:
+            if len(cache.floats) > 999:
+                cache.floats.clear()
+            n = cache.floats[T, max_len] = self.twist_cache_attention_floats(cache, T, max_len)
         scratch = torch.empty(n, dtype=torch.float32, device=self.device) if n else None
-        self._call(lib.twist_cache_attention_raw, cache.pages.ref, cache.k.data_ptr(), cache.v.data_ptr(), cache.page_stride, q.data_ptr(), ldq, T, cache.Hs, _addr(seq),
-                   lens.data_ptr(), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n, scratch=scratch)
+        self._call(lib.twist_cache_attention_raw, cache.pages.ref, cache.k_addr, cache.v_addr, cache.page_stride, q.data_ptr(), ldq, T, cache.Hs,
+                   _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n, scratch=scratch)
         return out, lse
 
     def twist_logits_raw(self, logits: torch.Tensor, rules: "LogitRules", out: torch.Tensor | None = None) -> torch.Tensor:
         """The rules applied to logits [T, vocab]; returns out, fp32 [T, vocab] (fp32 models: out may be logits).  See include/twist.h."""
         T, V = logits.shape[0], self.desc.vocab
-        ld = self._rows(logits, T, V, "logits")
-        _want(rules.T in (None, T) and rules.device in (None, self.device) and (rules.words is None or rules.words >= (V + 31) // 32),
-              f"rules: need {T} rows on {self.device}, and a mask of {(V + 31) // 32} words a row")
+        ld = self._rows(logits, T, V, "logits", self.torch_dtype)
+        if not (rules.T in (None, T) and rules.gpu in (None, self.gpu) and (rules.words is None or rules.words * 32 >= V)):
+            _refuse(f"rules: need {T} rows on {self.device}, and a mask of {(V + 31) // 32} words a row")
         if out is None:
-            out = torch.empty((T, V), dtype=torch.float32, device=self.device)
-        ldo = self._rows(out, T, V, "out", torch.float32)
+            out, ldo = torch.empty((T, V), dtype=torch.float32, device=self.device), V
+        else:
+            ldo = self._rows(out, T, V, "out", torch.float32)
         self._call(lib.twist_logits_raw, logits.data_ptr(), ld, T, rules.ref, out.data_ptr(), ldo)
         return out
 
@@ -602,9 +613,9 @@ class Pages:
     """A page table [n_seqs, max_pages] (int32, entries outside [0, n_pages): no page) over pools of n_pages pages of page_tokens tokens."""
 
     def __init__(self, table: torch.Tensor, n_pages: int, page_tokens: int):
-        _want(table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1) and table.is_cuda,
-              "table: needs a CUDA int32 [n_seqs, max_pages] with contiguous rows")
-        self.table, self.n_pages, self.page_tokens = table, n_pages, page_tokens
+        if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1)):
+            _refuse("table: needs a CUDA int32 [n_seqs, max_pages] with contiguous rows")
+        self.table, self.n_pages, self.page_tokens, self.gpu = table, n_pages, page_tokens, table.get_device()
         n_seqs, max_pages = table.shape
         self.c = PagesC(table.data_ptr(), table.stride(0) if n_seqs > 1 else max(table.stride(0), max_pages), n_seqs, max_pages, n_pages, page_tokens)
         self.ref = C.pointer(self.c)
@@ -614,14 +625,18 @@ class PagedCache:
     """Pools k, v [n_pages, Hs, page_tokens, d_head] of one layer (pages contiguous in themselves, equal strides between them) and the page table over them."""
 
     def __init__(self, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor):
+        if not (k.dim() == 4 and k.numel() and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device == table.device
+                and k[0].is_contiguous()):
+            _refuse("k and v: need one shape [n_pages, Hs, page_tokens, d_head], type, device and layout, every page contiguous")
         n_pages, self.Hs, page_tokens, self.d_head = k.shape
-        _want(k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device == table.device, "k and v: need one shape, type and device")
-        _want(k.numel() > 0 and k[0].is_contiguous(), "k and v: a page is contiguous")
         self.k, self.v, self.page_stride = k, v, k.stride(0) if n_pages > 1 else k[0].numel()
+        self.k_addr, self.v_addr, self.gpu, self.dtype = k.data_ptr(), v.data_ptr(), k.get_device(), k.dtype
         self.pages = Pages(table, n_pages, page_tokens)
+        self.floats = {}  # (T, max_len): scratch of twist_cache_attention_raw
 
     def _fits(self, ctx: Context):
-        _want(self.k.dtype == ctx.torch_dtype and self.d_head == ctx.desc.d_head and self.k.device == ctx.device, "cache: another type, head width or GPU than the context's")
+        if self.dtype is not ctx.torch_dtype or self.d_head != ctx.desc.d_head or self.gpu != ctx.gpu:
+            _refuse("cache: another type, head width or GPU than the context's")
 
 
 class LogitRules:
@@ -633,18 +648,20 @@ class LogitRules:
                  allowed=None):
         self.keep = dict(history=history, n_history=n_history, n_prompt=n_prompt, repetition=repetition, frequency=frequency, presence=presence, bias_ids=bias_ids,
                          bias_values=bias_values, n_bias=n_bias, allowed=allowed)
-        self.T = self.device = None
+        self.T = self.gpu = None
         for name, t in self.keep.items():
             if t is None:
                 continue
             fp, matrix = name in ("repetition", "frequency", "presence", "bias_values"), name in ("history", "bias_ids", "bias_values", "allowed")
-            _want(t.is_cuda and t.dtype == (torch.float32 if fp else torch.int32) and t.dim() == 1 + matrix and (t.shape[-1] < 2 or t.stride(-1) == 1),
-                  f"{name}: needs CUDA {'fp32' if fp else 'int32'} {'rows' if matrix else 'values'}, contiguous")
-            _want(self.T in (None, t.shape[0]) and self.device in (None, t.device), f"{name}: another number of rows or GPU than the others")
-            self.T, self.device = t.shape[0], t.device
+            if not (t.is_cuda and t.dtype == (torch.float32 if fp else torch.int32) and t.dim() == 1 + matrix and (t.shape[-1] < 2 or t.stride(-1) == 1)):
+                _refuse(f"{name}: needs CUDA {'fp32' if fp else 'int32'} {'rows' if matrix else 'values'}, contiguous")
+            if self.T not in (None, t.shape[0]) or self.gpu not in (None, t.get_device()):
+                _refuse(f"{name}: another number of rows or GPU than the others")
+            self.T, self.gpu = t.shape[0], t.get_device()
         ld = lambda t: 0 if t is None else t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])  # noqa: E731
         cap = lambda t: 0 if t is None else t.shape[1]  # noqa: E731
-        _want(bias_ids is None or bias_values is None or (bias_ids.shape == bias_values.shape and ld(bias_ids) == ld(bias_values)), "biases: ids and values differ in shape")
+        if bias_ids is not None and bias_values is not None and (bias_ids.shape != bias_values.shape or ld(bias_ids) != ld(bias_values)):
+            _refuse("biases: ids and values differ in shape")
         self.words = None if allowed is None else allowed.shape[1]
         self.c = LogitRulesC(_addr(history), ld(history), cap(history), _addr(n_history), _addr(n_prompt), _addr(repetition), _addr(frequency), _addr(presence),
                              _addr(bias_ids), _addr(bias_values), ld(bias_ids), cap(bias_ids), _addr(n_bias), _addr(allowed), ld(allowed))

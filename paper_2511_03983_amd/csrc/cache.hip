@@ -51,39 +51,97 @@ __device__ __forceinline__ void rotation(int p, double turns, float &c, float &s
 
 struct Turns { double f[128]; };  // theta^(-2i/dh) / 2 pi
 
-// A thread per (row, head, pair (i, i + dh/2)) with rotation, per (row, head, element) without.
-template <int BF, bool ROPE>
-__global__ __launch_bounds__(kT) void append_plain_kernel(Pages pg, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld, int Hs, int dh,
-                                                          const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq, Turns turns, int64_t total) {
-  const int64_t i = (int64_t)blockIdx.x * kT + threadIdx.x;
-  if (i >= total) return;
-  const int n = ROPE ? dh / 2 : dh;
-  const int f = (int)(i % n);
-  const int64_t r = i / n;
-  const int h = (int)(r % Hs);
-  const int t = (int)(r / Hs), p = lens[t] - 1, s = seq ? seq[t] : t;
-  if (p < 0 || (unsigned)s >= (unsigned)pg.n_seqs) return;
-  const int64_t HD = (int64_t)Hs * dh, in = t * ld + (int64_t)h * dh + f, out = t * ldq + (int64_t)h * dh + f, at = place(pg, page_stride, s, p, h, dh);
-  if (!ROPE) {
-    if (q_out) El<BF>::st(q_out, out, El<BF>::ld(qkv, in));
-    if (at < 0) return;
-    El<BF>::st(k, at + f, El<BF>::ld(qkv, in + HD));
-    El<BF>::st(v, at + f, El<BF>::ld(qkv, in + 2 * HD));
-    return;
+// BYTES (16 to an element's) of consecutive elements in registers
+template <int BYTES> struct Vec;
+template <> struct Vec<16> { typedef uint32_t T __attribute__((ext_vector_type(4))); };
+template <> struct Vec<8> { typedef uint32_t T __attribute__((ext_vector_type(2))); };
+template <> struct Vec<4> { typedef uint32_t T; };
+template <> struct Vec<2> { typedef uint16_t T; };
+template <int BF, int BYTES> struct Elems {
+  static constexpr int N = BYTES / (BF ? 2 : 4);
+  typename Vec<BYTES>::T raw;
+  __device__ __forceinline__ void load(const void *p, int64_t i) { raw = *reinterpret_cast<const typename Vec<BYTES>::T *>(static_cast<const char *>(p) + i * (BF ? 2 : 4)); }
+  __device__ __forceinline__ void store(void *p, int64_t i) const { *reinterpret_cast<typename Vec<BYTES>::T *>(static_cast<char *>(p) + i * (BF ? 2 : 4)) = raw; }
+  __device__ __forceinline__ float get(int j) const {
+    float v;
+    if (BF) v = __uint_as_float((uint32_t)reinterpret_cast<const uint16_t *>(&raw)[j] << 16);
+    else v = reinterpret_cast<const float *>(&raw)[j];
+    return v;
   }
-  float c, sn;
-  rotation(p, turns.f[f], c, sn);
-  if (q_out) {
-    const float a = El<BF>::ld(qkv, in), b = El<BF>::ld(qkv, in + n);
-    El<BF>::st(q_out, out, a * c - b * sn);
-    El<BF>::st(q_out, out + n, b * c + a * sn);
+  __device__ __forceinline__ void set(int j, float v) { El<BF>::st(&raw, j, v); }
+};
+
+constexpr int kAngles = 1024;  // (row, pair) angles of a workgroup
+constexpr int kAppendRows = 16;
+
+// Bound by copying (every value read and written once), by a launch's latency for few rows.  A workgroup takes `rows` rows; the angles, the same for all heads,
+// are formed once in LDS (left to every thread they took 1.5 times as long as the copying) while the first values are on their way; a
+// thread then turns BYTES of the first half of a head against the same of the second, for q and k, and copies v.
+template <int BF, int BYTES, bool ROPE>
+__global__ __launch_bounds__(kT) void append_kernel(Pages pg, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld, int T, int Hs, int dh,
+                                                    const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq, Turns turns, int rows) {
+  using E = Elems<BF, BYTES>;
+  constexpr int N = E::N, HALVES = ROPE ? 2 : 1;
+  __shared__ float2 angle[ROPE ? kAngles : 1];
+  __shared__ int64_t to[kAppendRows];  // where a row's keys and values go, less the head; -1: nowhere, -2: the row is unused
+  const int t0 = blockIdx.x * rows, here = min(rows, T - t0), tid = threadIdx.x;
+  const int width = dh / HALVES, per_head = width / N, per_row = Hs * per_head, total = here * per_row;
+  const int64_t HD = (int64_t)Hs * dh;
+  E x[3][HALVES];
+  int r = 0, h = 0, f = 0;
+  auto load = [&](int i) {
+    r = i / per_row;
+    h = (i - r * per_row) / per_head;
+    f = (i - r * per_row - h * per_head) * N;
+    const int64_t in = (t0 + r) * ld + (int64_t)h * dh + f;
+#pragma unroll
+    for (int c = 0; c < 3; ++c)
+#pragma unroll
+      for (int a = 0; a < HALVES; ++a) x[c][a].load(qkv, in + c * HD + a * width);
+  };
+  int i = tid;
+  if (i < total) load(i);
+  if (tid < here) {
+    const int p = max(0, lens[t0 + tid]) - 1, s = seq ? seq[t0 + tid] : t0 + tid;
+    int64_t at = -2;
+    if (p >= 0 && (unsigned)s < (unsigned)pg.n_seqs) at = place(pg, page_stride, s, p, 0, dh);
+    to[tid] = at;
   }
-  if (at < 0) return;
-  const float a = El<BF>::ld(qkv, in + HD), b = El<BF>::ld(qkv, in + HD + n);
-  El<BF>::st(k, at + f, a * c - b * sn);
-  El<BF>::st(k, at + f + n, b * c + a * sn);
-  El<BF>::st(v, at + f, El<BF>::ld(qkv, in + 2 * HD));
-  El<BF>::st(v, at + f + n, El<BF>::ld(qkv, in + 2 * HD + n));
+  if (ROPE) {
+    for (int j = tid; j < here * width; j += kT) {
+      const int row = j / width, pair = j - row * width;
+      rotation(max(1, lens[t0 + row]) - 1, turns.f[pair], angle[j].x, angle[j].y);
+    }
+  }
+  __syncthreads();
+  for (; i < total; ) {
+    const int64_t at = to[r];
+    if (at != -2) {
+      if (ROPE) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const float2 w = angle[r * width + f + e];
+#pragma unroll
+          for (int c = 0; c < 2; ++c) {
+            const float a = x[c][0].get(e), b = x[c][HALVES - 1].get(e);
+            x[c][0].set(e, a * w.x - b * w.y);
+            x[c][HALVES - 1].set(e, b * w.x + a * w.y);
+          }
+        }
+      }
+#pragma unroll
+      for (int a = 0; a < HALVES; ++a) {
+        if (q_out) x[0][a].store(q_out, (t0 + r) * ldq + (int64_t)h * dh + f + a * width);
+        if (at >= 0) {
+          const int64_t out = at + (((int64_t)h << pg.shift) * dh) + f + a * width;
+          x[1][a].store(k, out);
+          x[2][a].store(v, out);
+        }
+      }
+    }
+    i += kT;
+    if (i < total) load(i);
+  }
 }
 
 // ------------------------------------------------------------------------------------------- attention
@@ -627,15 +685,28 @@ extern "C" twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages
   const int dh = ctx->d.d_head;
   const int64_t HD = (int64_t)Hs * dh;
   if (ld < 3 * HD || (q_out && ldq < HD)) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows overlap", who);
-  const Pages pg = device_pages(pages);
+  const int rope = ctx->d.use_rope, es = ctx->esize(), width = rope ? dh / 2 : dh;
   Turns turns;
-  for (int i = 0; i < 128; ++i) turns.f[i] = ctx->rope_turns[i];
-  const int rope = ctx->d.use_rope;
-  const int64_t total = (int64_t)T * Hs * (rope ? dh / 2 : dh);
-  const dim3 grid((unsigned)((total + kT - 1) / kT));
-#define APPEND(BF, R) hipLaunchKernelGGL((append_plain_kernel<BF, R>), grid, dim3(kT), 0, ctx->stream, pg, k, v, page_stride, qkv, ld, Hs, dh, seq, lens, q_out, ldq, turns, total)
-  if (ctx->d.dtype == TWIST_BF16) { if (rope) APPEND(1, true); else APPEND(1, false); }
-  else { if (rope) APPEND(0, true); else APPEND(0, false); }
+  if (rope) std::copy(ctx->rope_turns, ctx->rope_turns + 128, turns.f);
+  // the widest pieces that a head's halves, and all addresses, are multiples of
+  uintptr_t bits = reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(qkv) | (uintptr_t)(width * es) | (uintptr_t)(ld * es) |
+                   (uintptr_t)(page_stride * es);
+  if (q_out) bits |= reinterpret_cast<uintptr_t>(q_out) | (uintptr_t)(ldq * es);
+  const int bytes = bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 2;
+  // rows of a workgroup: what keeps its threads busy, but 512 workgroups before that
+  const int per_row = (int)(HD / (rope ? 2 : 1) * es / bytes);
+  const int rows = std::max(1, std::min({kT / per_row, (T + 511) / 512, kAppendRows, rope ? kAngles / width : kAppendRows}));
+  const dim3 grid((unsigned)((T + rows - 1) / rows));
+#define APPEND(BF, BYTES)                                                                                                                                    \
+  if (rope) hipLaunchKernelGGL((append_kernel<BF, BYTES, true>), grid, dim3(kT), 0, ctx->stream, device_pages(pages), k, v, page_stride, qkv, ld, T, Hs, dh, seq, \
+                               lens, q_out, ldq, turns, rows);                                                                                               \
+  else hipLaunchKernelGGL((append_kernel<BF, BYTES, false>), grid, dim3(kT), 0, ctx->stream, device_pages(pages), k, v, page_stride, qkv, ld, T, Hs, dh, seq,     \
+                          lens, q_out, ldq, turns, rows)
+  if (ctx->d.dtype == TWIST_BF16) {
+    if (bytes == 16) { APPEND(1, 16); } else if (bytes == 8) { APPEND(1, 8); } else if (bytes == 4) { APPEND(1, 4); } else { APPEND(1, 2); }
+  } else {
+    if (bytes == 16) { APPEND(0, 16); } else if (bytes == 8) { APPEND(0, 8); } else { APPEND(0, 4); }
+  }
 #undef APPEND
   TW_HIP(ctx, hipGetLastError());
   return TWIST_OK;
