@@ -1,6 +1,7 @@
 """Kernel-level parity of the steps of generating tokens (appending to a paged cache, attention over it, rules on logits), each against the formula in
 64 bits on identical inputs, element by element.  u below is the rounding of the stored type (half a step: bf16 2^-8, fp32 2^-24)."""
 import math
+from collections import Counter
 
 import numpy as np
 import pytest
@@ -418,8 +419,9 @@ def _logits_want(x, r, V):
         hist = hist[: max(0, int(at("n_history", t, len(hist))))]
         n_prompt = int(at("n_prompt", t, 0))
         rep, freq, pres = at("repetition", t), at("frequency", t, 0.0), at("presence", t, 0.0)
+        times = Counter(hist[max(0, n_prompt):])
         for c in {h for h in hist if 0 <= h < V}:
-            n = sum(1 for i, h in enumerate(hist) if h == c and i >= n_prompt)
+            n = times[c]
             if rep is not None:
                 x[t, c] = x[t, c] / rep if x[t, c] > 0 else x[t, c] * rep
                 mag[t, c] = max(mag[t, c], x[t, c].abs())
@@ -428,9 +430,10 @@ def _logits_want(x, r, V):
                 mag[t, c] += abs(freq) * n + abs(pres)
         ids = [] if r["bias_ids"] is None else r["bias_ids"][t].tolist()
         last = {c: i for i, c in enumerate(ids[: max(0, int(at("n_bias", t, len(ids))))]) if 0 <= c < V}
+        values = [] if r["bias_values"] is None else r["bias_values"][t].double().tolist()
         for c, i in last.items():
-            x[t, c] += r["bias_values"][t, i].double().item()
-            mag[t, c] += abs(r["bias_values"][t, i].double().item())
+            x[t, c] += values[i]
+            mag[t, c] += abs(values[i])
         if r["allowed"] is not None:
             w = r["allowed"][t].cpu().numpy().view(np.uint32)
             bit = torch.tensor(np.unpackbits(w.view(np.uint8), bitorder="little")[:V].astype(bool))
@@ -495,6 +498,8 @@ def test_logits_single_rules_and_strides(lib, dtype):
     _check_logits(lib, dtype, 4, 700, hist=1, prompt=False)
     _check_logits(lib, dtype, 4, 700, hist=5000, span=700)
     _check_logits(lib, dtype, 4, 700, hist=60, penalties=False)
+    _check_logits(lib, dtype, 2, 9001, hist=70000, nb=600)             # lists that are longer than 16 bits count
+    _check_logits(lib, dtype, 1, 9001, hist=20, nb=40000, allow=0.5)
 
 
 def test_logits_in_place_and_of_no_number(lib):
