@@ -223,6 +223,34 @@ TWIST_API twist_status twist_masked_form(twist_ctx *ctx, const twist_plan *plan,
 TWIST_API twist_status twist_subnet_forward(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets,
                                             int32_t B, int32_t N, void *workspace, size_t workspace_bytes, float *loss_dev);
 
+/* A paged cache of keys and values: pools k and v (desc.dtype), each n_pages pages of [Hs][page_tokens][d_head] whose starts lie page_stride elements apart
+ * (at least Hs * page_tokens * d_head), as many key/value heads as query heads.  Row s of the table names the pages of sequence s in order: token p of it
+ * lies in page table[s][p / page_tokens], at place p % page_tokens.  Entries outside [0, n_pages) are pages that the sequence does not have: no key
+ * is written there, and attention sees none.  A sequence holds max_pages * page_tokens tokens at most. */
+typedef struct {
+  const int32_t *table;  /* dev [n_seqs] rows of max_pages entries, ld_table apart */
+  int64_t ld_table;
+  int32_t n_seqs, max_pages;
+  int32_t n_pages, page_tokens; /* page_tokens: a power of two, 1 to 4096 */
+} twist_pages;
+
+/* Generating tokens with a deployed subnet: one step for T rows, row t being token lens[t] - 1 of sequence seq[t] (t itself with seq NULL), whose id is
+ * tokens[t].  Its keys and values are appended to the paged cache (all rows of all sequences first), then it attends to the tokens of its sequence up to
+ * itself; logits [T, vocab] (desc.dtype, rows ldl elements apart) receives the next token's.  One row a sequence is ordinary decoding; several consecutive ones
+ * are a prompt, or drafted tokens to check.  Same layers, scales and precision as twist_subnet_forward, which gives the same logits up to rounding.
+ *   pages    one table for all layers; rows with lens[t] < 1, lens[t] > max_len or a seq[t] outside [0, n_seqs)
+ *            are unused ones: nothing is cached for them and their logits are undefined.  An id outside the vocabulary counts as a zero embedding.
+ *   cache    (dev, 256-byte aligned, >= twist_cache_bytes) the pools of all layers, caller-owned, need not be cleared: what is beyond a sequence's
+ *            length is never used.  Valid for this subnet's widths and this n_pages and page_tokens.
+ *   max_len  (host) the longest length of this call, at most desc.max_seq; kernels and workspace (dev, 256-byte aligned, >=
+ *            twist_decode_workspace_bytes) are chosen by it and T alone, so a captured step serves all shorter lengths.
+ * No loss, no gradients, any storage mode.  TWIST_ESHAPE without a vocabulary, and as twist_subnet_forward. */
+TWIST_API twist_status twist_cache_bytes(twist_ctx *ctx, const twist_subnet *sub, const twist_pages *pages, size_t *bytes);
+TWIST_API twist_status twist_decode_workspace_bytes(twist_ctx *ctx, const twist_subnet *sub, const twist_pages *pages, int32_t T, int32_t max_len, size_t *bytes);
+TWIST_API twist_status twist_subnet_decode(twist_ctx *ctx, twist_subnet *sub, const int32_t *tokens, int32_t T, const int32_t *seq, const int32_t *lens,
+                                           int32_t max_len, const twist_pages *pages, void *cache, size_t cache_bytes, void *workspace,
+                                           size_t workspace_bytes, void *logits, int64_t ldl);
+
 /* Local optimizer step on every subnet parameter from the current gradients: SGD  w -= lr g,  or AdamW
  * (bias-corrected, decoupled decay on matrices only; needs TWIST_STORE_ADAMW).  bf16 models update fp32
  * master weights and re-round the bf16 copy. */
@@ -362,17 +390,7 @@ TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32
 /* Kernel-level entry points of twist_subnet_decode: the steps of generating tokens that training does not have, on the ctx's stream.  Device pointers owned
  * by the caller, "dtype" means desc.dtype, d_head and rotary positions come from the ctx's model description.
  *
- * A paged cache of keys and values: pools k and v (dtype), each n_pages pages of [Hs][page_tokens][d_head] whose starts lie page_stride elements apart
- * (at least Hs * page_tokens * d_head), as many key/value heads as query heads.  Row s of the table names the pages of sequence s in order: token p of it
- * lies in page table[s][p / page_tokens], at place p % page_tokens.  Entries outside [0, n_pages) are pages that the sequence does not have: no key
- * is written there, and attention sees none.  A sequence holds max_pages * page_tokens tokens at most. */
-typedef struct {
-  const int32_t *table;  /* dev [n_seqs] rows of max_pages entries, ld_table apart */
-  int64_t ld_table;
-  int32_t n_seqs, max_pages;
-  int32_t n_pages, page_tokens; /* page_tokens: a power of two, 1 to 4096 */
-} twist_pages;
-/* twist_cache_append_raw     T new tokens, rows of qkv [T, 3*Hs*d_head] (q | k | v, dtype, rows ld elements apart): row t is token lens[t] - 1 of sequence
+ * twist_cache_append_raw     T new tokens, rows of qkv [T, 3*Hs*d_head] (q | k | v, dtype, rows ld elements apart): row t is token lens[t] - 1 of sequence
  *                            seq[t] (t itself with seq NULL).  Its v, and its k turned by the rotary embedding of that position (desc.use_rope; angles in
  *                            fp64, one rounding), go to their place in the pools; its q, turned likewise, to row t of q_out (rows ldq apart; q_out may be
  *                            the q part of qkv itself, or NULL: queries are not asked for).  Rows with lens[t] < 1 or a seq[t] outside [0, n_seqs) are

@@ -125,6 +125,9 @@ _SIGS = {
     "twist_act_raw": ([_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _i32], _i32),
     "twist_ce_raw": ([_vp, _vp, C.c_int64, _vp, _i32, _vp, _vp], _i32),
     "twist_embed_raw": ([_vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
+    "twist_cache_bytes": ([_vp, _vp, C.POINTER(PagesC), C.POINTER(_sz)], _i32),
+    "twist_decode_workspace_bytes": ([_vp, _vp, C.POINTER(PagesC), _i32, _i32, C.POINTER(_sz)], _i32),
+    "twist_subnet_decode": ([_vp, _vp, _vp, _i32, _vp, _vp, _i32, C.POINTER(PagesC), _vp, _sz, _vp, _sz, _vp, C.c_int64], _i32),
     "twist_cache_append_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _vp, C.c_int64], _i32),
     "twist_cache_attention_floats": ([_vp, C.POINTER(PagesC), _i32, _i32, _i32, C.POINTER(_sz)], _i32),
     "twist_cache_attention_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _i32, _vp, C.c_int64, _vp, _vp, _sz], _i32),
@@ -272,6 +275,31 @@ class Context:
         B, N = inputs.shape[0], inputs.shape[1]
         _check(lib.twist_subnet_forward(self.h, sub.h, _vp(inputs.data_ptr()), _vp(targets.data_ptr()), B, N,
                                         _vp(workspace.data_ptr()), workspace.numel(), _vp(loss.data_ptr())), self.h)
+
+    def twist_cache_bytes(self, sub: "Subnet", pages: "Pages") -> int:
+        n = _sz()
+        _check(lib.twist_cache_bytes(self.h, sub.h, pages.ref, C.byref(n)), self.h)
+        return n.value
+
+    def twist_decode_workspace_bytes(self, sub: "Subnet", pages: "Pages", T: int, max_len: int) -> int:
+        n = _sz()
+        _check(lib.twist_decode_workspace_bytes(self.h, sub.h, pages.ref, T, max_len, C.byref(n)), self.h)
+        return n.value
+
+    def twist_subnet_decode(self, sub: "Subnet", tokens: torch.Tensor, lens: torch.Tensor, max_len: int, pages: "Pages", cache: torch.Tensor,
+                            workspace: torch.Tensor, seq: torch.Tensor | None = None, logits: torch.Tensor | None = None) -> torch.Tensor:
+        """Logits [T, vocab] of the tokens that follow tokens [T] (int32), row t being token lens[t] - 1 <= max_len - 1 of sequence seq[t] (default t); their keys
+        and values go to the cache (storage of twist_cache_bytes).  See include/twist.h."""
+        T, V = tokens.shape[0], self.desc.vocab
+        if logits is None:      # rows that start at multiples of 16 bytes
+            logits = torch.empty((T, (V + 7) // 8 * 8), dtype=self.torch_dtype, device=self.device)[:, :V]
+        ldl = self._rows(logits, T, V, "logits", self.torch_dtype)
+        if pages.gpu != self.gpu or cache.get_device() != self.gpu or workspace.get_device() != self.gpu:
+            _refuse(f"table, cache and workspace: need to be on {self.device}")
+        self._call(lib.twist_subnet_decode, sub.h, _ints(tokens, T, "tokens", self.gpu), T, _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len,
+                   pages.ref, cache.data_ptr(), cache.numel() * cache.element_size(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
+                   logits.data_ptr(), ldl)
+        return logits
 
     def twist_subnet_step(self, sub: "Subnet", kind=OPT_SGD, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) -> None:
         od = OptDesc(kind, lr, beta1, beta2, eps, weight_decay)
