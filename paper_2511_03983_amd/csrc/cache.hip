@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_kernel(AttentionArgs 
   __shared__ int64_t ids[kMaxIds];
   __shared__ float s_acc[NW][W], s_m[NW], s_l[NW];
   __shared__ int s_seen[NW];
-  const int part = blockIdx.x % A.parts, unit = blockIdx.x / A.parts, h = unit % A.Hs, t = unit / A.Hs;
+  const int part = blockIdx.x / (A.T * A.Hs), unit = blockIdx.x % (A.T * A.Hs), h = unit % A.Hs, t = unit / A.Hs;
   const int s = A.seq ? A.seq[t] : t, given = A.lens[t], dh = A.dh;
   if (given < 0 || (unsigned)s >= (unsigned)A.pg.n_seqs) return;
   const int len = min(given, A.max_len), p0 = part * A.chunk, p1 = min(p0 + A.chunk, len);
@@ -348,7 +348,8 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
   __shared__ __attribute__((aligned(16))) char tiles[NW][TILE_B];
   __shared__ float s_m[NW][kTile], s_l[NW][kTile];
   __shared__ int s_seen[NW][kTile];
-  const int part = blockIdx.x % A.parts, turn = blockIdx.x / A.parts % A.turns, unit = blockIdx.x / A.parts / A.turns, h = unit % A.Hs, t0 = unit / A.Hs * kTile, dh = A.dh;
+  const int units = (A.T + kTile - 1) / kTile * A.Hs, unit = blockIdx.x % units, turn = blockIdx.x / units % A.turns, part = blockIdx.x / units / A.turns;
+  const int h = unit % A.Hs, t0 = unit / A.Hs * kTile, dh = A.dh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane >> 4, c = lane & 15;
   // the first rows of the groups among rows t0 .. t0 + 15, of which every A.turns-th is this workgroup's
   const int own = t0 + c < A.T ? A.seq[t0 + c] : -1, prev = __shfl_up(own, 1, 64);
@@ -575,24 +576,31 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 }
 
 // Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens (row_bytes: of a head's key).  Figures
-// are us on the device, launch included.
+// are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
 //  - Tiles (turns > 0): where there are at least twice as many rows as sequences, so that most of them must share one.  A workgroup takes every turns-th
-//    group among 16 rows.  bf16, heads of 128, tiles / rows by themselves: 16 x 4 rows over 2000 tokens, 16 heads 44 / 68, 16 x 8 over 8000 152 / 351,
-//    a prompt of 1000, 8 heads 40 / 173; one row a sequence, 16 x 16384, 32 heads 527 / 507, 1 x 1000, 12 heads of 64 11.5 / 7.1.
-//  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42 (one row of one head of 16384 x 128 bf16 alone); 256 of either draw what the HBM gives.  Rows that
-//    cannot feed 16 waves take 4.  16 / 4 waves: 4 heads of 64 over 20 tokens 4.6 / 3.8, 12 over 1000 7.1 / 8.1, 96 over 1000 8.4 / 10.4; heads of 128: 2048
-//    over 200 39 / 29, 1024 over 1000 62 / 64, 256 over 2048 37.5 / 38.6.
-//  - Where there are fewer of them than CUs, a sequence is cut, into parts of 512 KB at least (6 us of a workgroup's reading; the second launch, which joins
-//    them, costs 4): 16 heads of 128 over 32768 tokens in parts of 256 / 1024 / 2048: 58 / 54.8 / 53.3.
+//    group among 16 rows.  Tiles / rows by themselves: (16 x 16) x 2000, 4 rows each 44 / 68, x 8000, 8 rows each 148 / 351, a prompt of 1000, 8 heads 36 / 173;
+//    one row a sequence, (32 x 16) x 16384 527 / 507, 12 heads of 64 x 1000 11.5 / 7.1.
+//  - Up to 384 KB of keys and values a head are read by one workgroup; where heads and rows are at most half the CUs, longer sequences are cut so that there are
+//    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
+//    8 x 4096 22 / 10.5 / 11, 32 x 2048 17 / 12.6 / 12.5, 32 x 8192 - / 30.5 / 32.5, 16 x 32768 - / 53.4 / 55.2;
+//    beyond that half, 12 heads of 64 x 16 in fp32 x 2000 32 / 35 / -.  Tiles, whose waves take 32 tokens at a
+//    time: 256 KB (16 heads x 4096, 8 rows: parts of 256 / 512 / 1024 22.9 / 18.5 / 25).
+//  - From 4 MB on parts of 1 MB even out rows of different lengths: uncut / cut (32 x 16) x 16384 511 / 478, (16 x 16) x 8192 143 / 134, (32 x 16) x 8192 259 / 260; on
+//    the other side (32 x 16) x 4096 132 / 134, (16 x 128) x 2048 238 / 246.
+//  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
+//    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.
 struct Split { int waves, parts, chunk, turns; };
 Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int row_bytes, bool tiles) {
   Split s;
+  const int64_t blocks = (T + kTile - 1) / kTile, pair = 2 * row_bytes;
   s.turns = tiles && T >= 2 * (int64_t)n_seqs ? std::min(8, std::max(1, (int)((int64_t)kTile * n_seqs / T))) : 0;
-  const int64_t units = (int64_t)(s.turns ? (T + kTile - 1) / kTile * s.turns : T) * Hs, want = std::max<int64_t>(1, 256 / units), least = std::max(64, (256 << 10) / row_bytes);
-  int64_t c = std::max<int64_t>(least, (max_len + want - 1) / want);
+  const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
+  int64_t c = max_len;
+  if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
+  if (max_len * pair >= 4 << 20) c = std::min<int64_t>(c, (1 << 20) / pair);
   c = std::max<int64_t>(c, (max_len + kMaxParts - 1) / kMaxParts);
   c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)kMaxIds << shift);
-  s.waves = (int64_t)max_len * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
+  s.waves = c * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
   s.chunk = (int)c;
   s.parts = (int)((max_len + c - 1) / c);
   return s;
