@@ -191,14 +191,14 @@ class Context:
         self.h = h
         self.torch_dtype = torch.bfloat16 if desc.dtype == BF16 else torch.float32
         self.device = self.stream.device
-        self.gpu = self.device.index
+        self.gpu, self.only_gpu = self.device.index, torch.cuda.device_count() == 1
 
     def _call(self, f, *args, scratch=None):
         """f(*args) on the context's GPU, also where that is not the current one; `scratch` is a tensor of the caller's current stream that the call's
         kernels use and nobody holds afterwards."""
         if scratch is not None and torch.cuda.current_stream(self.device) != self.stream:
             scratch.record_stream(self.stream)
-        if torch.cuda.current_device() == self.gpu:
+        if self.only_gpu or torch.cuda.current_device() == self.gpu:
             status = f(self.h, *args)
         else:
             with torch.cuda.device(self.device):

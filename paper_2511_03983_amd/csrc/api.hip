@@ -42,7 +42,7 @@ extern "C" twist_status twist_create(const twist_model_desc *desc, void *hip_str
   c->d = d;
   c->stream = reinterpret_cast<hipStream_t>(hip_stream);
   if (d.use_rope)
-    for (int i = 0; i < d.d_head / 2 && i < 128; ++i) c->rope_turns[i] = pow((double)d.rope_theta, -2.0 * i / d.d_head) / (2.0 * M_PI);
+    for (int i = 0; i < 8 + 16; ++i) c->rope_turns[i] = pow((double)d.rope_theta, -2.0 * (i < 8 ? 16 * i : i - 8) / d.d_head) / (i < 8 ? 2.0 * M_PI : 1.0);
   *out = c;
   return TWIST_OK;
 }

@@ -49,7 +49,11 @@ __device__ __forceinline__ void rotation(int p, double turns, float &c, float &s
   sincospif(2.f * (float)(t - rint(t)), &s, &c);
 }
 
-struct Turns { double f[128]; };  // theta^(-2i/dh) / 2 pi
+// theta^(-2i/dh) / 2 pi for pair i < 128, as a product (whose rounding, 2^-53, is nothing at any position).  All 128 as kernel arguments took the host 0.8 us more.
+struct Turns {
+  double coarse[8], fine[16];
+  __device__ __forceinline__ double of(int i) const { return coarse[i >> 4] * fine[i & 15]; }
+};
 
 // BYTES (16 to an element's) of consecutive elements in registers
 template <int BYTES> struct Vec;
@@ -110,7 +114,7 @@ __global__ __launch_bounds__(kT) void append_kernel(Pages pg, void *k, void *v, 
   if (ROPE) {
     for (int j = tid; j < here * width; j += kT) {
       const int row = j / width, pair = j - row * width;
-      rotation(max(1, lens[t0 + row]) - 1, turns.f[pair], angle[j].x, angle[j].y);
+      rotation(max(1, lens[t0 + row]) - 1, turns.of(pair), angle[j].x, angle[j].y);
     }
   }
   __syncthreads();
@@ -695,7 +699,8 @@ extern "C" twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages
   if (ld < 3 * HD || (q_out && ldq < HD)) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows overlap", who);
   const int rope = ctx->d.use_rope, es = ctx->esize(), width = rope ? dh / 2 : dh;
   Turns turns;
-  if (rope) std::copy(ctx->rope_turns, ctx->rope_turns + 128, turns.f);
+  std::copy(ctx->rope_turns, ctx->rope_turns + 8, turns.coarse);
+  std::copy(ctx->rope_turns + 8, ctx->rope_turns + 24, turns.fine);
   // the widest pieces that a head's halves, and all addresses, are multiples of
   uintptr_t bits = reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | reinterpret_cast<uintptr_t>(qkv) | (uintptr_t)(width * es) | (uintptr_t)(ld * es) |
                    (uintptr_t)(page_stride * es);

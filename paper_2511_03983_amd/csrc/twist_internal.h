@@ -61,7 +61,7 @@ struct PlanEntry {
 struct twist_ctx {
   twist_model_desc d;
   hipStream_t stream = nullptr;
-  double rope_turns[128] = {};  // rotary models with d_head up to 256: theta^(-2i/d_head) / 2 pi of pair i, turns of a position
+  double rope_turns[8 + 16] = {};  // rotary models: pair i turns by theta^(-2i/d_head) / 2 pi of a full turn at every position, [i / 16] [8 + i % 16] for i < 128
   mutable std::string err;
   // optional per-launch timing of the projection kernels (see twist_profile_gemm)
   bool prof_gemm = false;
