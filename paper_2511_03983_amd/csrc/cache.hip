@@ -597,7 +597,7 @@ struct Split { int waves, parts, chunk, turns; };
 Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int row_bytes, bool tiles) {
   Split s;
   const int64_t blocks = (T + kTile - 1) / kTile, pair = 2 * row_bytes;
-  s.turns = tiles && T >= 2 * (int64_t)n_seqs ? std::min(8, std::max(1, (int)((int64_t)kTile * n_seqs / T))) : 0;
+  s.turns = tiles && T >= 2 * (int64_t)n_seqs ? std::min({8, T, std::max(1, (int)((int64_t)kTile * n_seqs / T))}) : 0;
   const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
   int64_t c = max_len;
   if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
@@ -626,8 +626,9 @@ twist_status check_cache(twist_ctx *ctx, const char *who, const twist_pages *p, 
   const int64_t dh = ctx->d.d_head;
   if (T < 1 || Hs < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: empty input", who);
   if (dh > kMaxHead) TW_FAIL(ctx, TWIST_ESHAPE, "%s: d_head=%lld above %d is not supported", who, (long long)dh, kMaxHead);
-  if ((int64_t)T * Hs > (int64_t)1 << 22) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads are too many for one call", who, T, Hs);
+  if ((int64_t)T * Hs >= (int64_t)1 << 22) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads are too many for one call", who, T, Hs);
   if (page_stride < Hs * dh * p->page_tokens) TW_FAIL(ctx, TWIST_ESHAPE, "%s: page_stride=%lld is less than a page", who, (long long)page_stride);
+  if (page_stride > INT64_MAX / 8 / p->n_pages) TW_FAIL(ctx, TWIST_ESHAPE, "%s: page_stride=%lld is beyond any memory", who, (long long)page_stride);
   return TWIST_OK;
 }
 
@@ -728,13 +729,14 @@ extern "C" twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages
 extern "C" twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist_pages *pages, int32_t T, int32_t Hs, int32_t max_len, size_t *floats) {
   const char *who = "twist_cache_attention_floats";
   if (!ctx || !floats) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
-  TW_TRY(check_cache(ctx, who, pages, INT64_MAX, T, Hs));
+  TW_TRY(check_pages(ctx, who, pages));
+  TW_TRY(check_cache(ctx, who, pages, (int64_t)Hs * ctx->d.d_head * pages->page_tokens, T, Hs));
   if (max_len < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: max_len=%d", who, max_len);
   size_t need = 0;
   for (int seq = 0; seq < 2; ++seq) {  // the caller's rows may share sequences, or not
     int most = max_len;
     const Split s = attention_split(ctx, pages, T, Hs, most, seq);
-    if (s.parts > kMaxParts || (int64_t)T * Hs * s.parts > (int64_t)1 << 22)
+    if (s.parts > kMaxParts || (int64_t)T * Hs * s.parts >= (int64_t)1 << 22)  // (workgroups of 1024 threads, of which a launch has less than 2^32)
       TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
     if (s.parts > 1) need = std::max(need, (size_t)T * Hs * s.parts * (ctx->d.d_head + 2));
   }

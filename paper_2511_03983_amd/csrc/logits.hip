@@ -148,6 +148,7 @@ extern "C" twist_status twist_logits_raw(twist_ctx *ctx, const void *logits, int
   if (T < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: empty input", who);
   if (T > 65535) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows are too many for one call", who, T);
   const twist_logit_rules &r = *rules;
+  if (V >= 1 << 30 || r.hist_cap >= 1 << 30 || r.bias_cap >= 1 << 30) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows of 2^30 and more", who);
   if (ld < V || ldo < V) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows overlap", who);
   if (logits == static_cast<const void *>(out) && (ctx->d.dtype != TWIST_F32 || ld != ldo))
     TW_FAIL(ctx, TWIST_EINVAL, "%s: only fp32 logits can be changed in place", who);

@@ -50,7 +50,7 @@ def test_append_refusals(tw):
         assert _append(tw, h, _pages(tw, **kw)) == status, kw
         assert b"twist_cache_append_raw" in tw.lib.twist_last_error(h)
     for kw, status in [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(qkv=None), EINVAL), (dict(lens=None), EINVAL), (dict(T=0), EINVAL), (dict(T=-1), EINVAL),
-                       (dict(Hs=0), EINVAL), (dict(stride=S - 1), ESHAPE), (dict(ld=383), ESHAPE), (dict(ldq=127), ESHAPE), (dict(T=2 ** 24), ESHAPE)]:
+                       (dict(Hs=0), EINVAL), (dict(stride=S - 1), ESHAPE), (dict(ld=383), ESHAPE), (dict(ldq=127), ESHAPE), (dict(T=2 ** 24), ESHAPE), (dict(T=2 ** 21), ESHAPE), (dict(stride=2 ** 60), ESHAPE)]:
         assert _append(tw, h, _pages(tw), **kw) == status, kw
     assert _append(tw, h, None) == EINVAL
     assert tw.lib.twist_cache_append_raw(None, _pages(tw), P, P, S, P, 384, 4, 2, None, P, P, 128) == EINVAL
@@ -68,12 +68,22 @@ def test_attention_refusals(tw):
         assert tw.lib.twist_cache_attention_floats(h, _pages(tw, **kw), 4, 2, 64, ctypes.byref(n)) == status, kw
     for kw, status in [(dict(k=None), EINVAL), (dict(v=None), EINVAL), (dict(q=None), EINVAL), (dict(lens=None), EINVAL), (dict(o=None), EINVAL), (dict(T=0), EINVAL),
                        (dict(Hs=-2), EINVAL), (dict(max_len=0), EINVAL), (dict(max_len=-5), EINVAL), (dict(stride=S - 1), ESHAPE), (dict(ldq=127), ESHAPE),
-                       (dict(ldo=127), ESHAPE), (dict(Hs=2 ** 20, stride=2 ** 62), ESHAPE)]:
+                       (dict(ldo=127), ESHAPE), (dict(Hs=2 ** 20, stride=2 ** 50, ldq=2 ** 30, ldo=2 ** 30), ESHAPE), (dict(stride=2 ** 62), ESHAPE),
+                       (dict(scratch=P + 4), ESHAPE)]:
         assert _attend(tw, h, _pages(tw), **kw) == status, kw
     assert _attend(tw, h, None) == EINVAL
+    assert tw.lib.twist_cache_attention_floats(h, _pages(tw, max_pages=2 ** 10, ld_table=2 ** 10), 1, 2, 2 ** 14, ctypes.byref(n)) == 0 and n.value not in (0, 77)
+    need = n.value
+    n.value = 77
+    long = _pages(tw, max_pages=2 ** 10, ld_table=2 ** 10)             # a long sequence is cut: scratch
+    assert _attend(tw, h, long, T=1, max_len=2 ** 14, scratch=None) == EINVAL
+    assert _attend(tw, h, long, T=1, max_len=2 ** 14, floats=need - 1) == ESHAPE
     for args in ((h, _pages(tw), 0, 2, 64), (h, _pages(tw), 4, 0, 64), (h, _pages(tw), 4, 2, 0), (None, _pages(tw), 4, 2, 64), (h, None, 4, 2, 64)):
         assert tw.lib.twist_cache_attention_floats(*args, ctypes.byref(n)) == EINVAL
     assert tw.lib.twist_cache_attention_floats(h, _pages(tw), 4, 2, 64, None) == EINVAL
+    # more parts than can be joined: single-token pages, eight million of them
+    long = _pages(tw, page_tokens=1, max_pages=2 ** 23, ld_table=2 ** 23)
+    assert tw.lib.twist_cache_attention_floats(h, long, 1, 2, 2 ** 23, ctypes.byref(n)) == ESHAPE
     assert n.value == 77                                               # an error leaves the out-parameters alone
     tw.lib.twist_destroy(h)
 
@@ -90,7 +100,7 @@ def test_logits_refusals(tw):
 
     for kw, status in [(dict(logits=None), EINVAL), (dict(out=None), EINVAL), (dict(T=0), EINVAL), (dict(T=65536), ESHAPE), (dict(ld=99), ESHAPE), (dict(ldo=99), ESHAPE),
                        (dict(ld_history=7), ESHAPE), (dict(hist_cap=-1), ESHAPE), (dict(bias_values=None), EINVAL), (dict(ld_bias=3), ESHAPE), (dict(bias_cap=-1), ESHAPE),
-                       (dict(ld_allowed=3), ESHAPE), (dict(out=P), EINVAL)]:
+                       (dict(ld_allowed=3), ESHAPE), (dict(out=P), EINVAL), (dict(hist_cap=2 ** 30, ld_history=2 ** 30), ESHAPE), (dict(bias_cap=2 ** 30, ld_bias=2 ** 30), ESHAPE)]:
         assert call(**kw) == status, kw
         assert b"twist_logits_raw" in tw.lib.twist_last_error(h)
     assert tw.lib.twist_logits_raw(h, P, 100, 2, None, 2 * P, 100) == EINVAL

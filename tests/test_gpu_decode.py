@@ -301,6 +301,8 @@ def test_attention_of_rows_that_share_sequences(lib, dtype, Hs, dh, page):
     _check_attention(lib, dtype, Hs, dh, page, lens, seq, n_seqs=3)
     _check_attention(lib, dtype, Hs, dh, page, list(range(1, 71)), [0] * 70, n_seqs=1)       # a whole prompt at once
     _check_attention(lib, dtype, Hs, dh, page, list(range(230, 195, -1)) + [-1, 0, 3], [1] * 38, n_seqs=2)
+    _check_attention(lib, dtype, Hs, dh, page, [33, 34], [0, 0], n_seqs=1)                   # no more rows than a group has
+    _check_attention(lib, dtype, Hs, dh, page, [20, 33, 4], [0, -1, 0], n_seqs=1)
     _check_attention(lib, dtype, Hs, dh, page, [1, 64, 65, 200, 0, 31, 32, 33, 16, 17, 300], list(range(11)), n_seqs=11)
 
 
@@ -310,6 +312,37 @@ def test_attention_of_drafts_over_long_sequences(lib, dtype, Hs, dh):
     """Rows of one sequence whose last parts only some of them reach, missing pages among them."""
     _check_attention(lib, dtype, Hs, dh, 16, [4500, 4501, 4502, 4503, 4096, 4097, 1], [0] * 7, n_seqs=1)
     _check_attention(lib, dtype, Hs, dh, 16, [4500, 4501, 60, 2500, 2501], [1, 1, 1, 0, 0], n_seqs=2, holes=[(1, 3), (1, 200), (0, 0)] + [(1, i) for i in range(64, 128)])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_a_long_prompt(lib, dtype):
+    """2500 rows of two sequences, one after another and mixed, against causal attention in 64 bits; the bound of every row as for single ones."""
+    n, Hs, dh, page = 1250, 2, 64, 16
+    ctx, g = _ctx(lib, dtype, dh), _gen(11)
+    pages = -(-n // page)
+    k, v = _pools(g, 2 * pages, Hs, page, dh, dtype)
+    table = torch.randperm(2 * pages, generator=g, device="cuda").to(torch.int32).view(2, pages)
+    q = _randn(g, 2 * n, Hs * dh, dtype=dtype)
+    flat = lambda p, s: p[table[s].long()].permute(1, 0, 2, 3).reshape(Hs, -1, dh)[:, :n].double()  # noqa: E731
+    for order in (torch.arange(2 * n, device="cuda"), torch.randperm(2 * n, generator=g, device="cuda")):
+        seq, lens = (order // n).to(torch.int32), (order % n + 1).to(torch.int32)
+        o, lse = ctx.twist_cache_attention_raw(lib.PagedCache(k, v, table), q, lens, n, seq=seq)
+        torch.cuda.synchronize()
+        for s in range(2):
+            rows = torch.nonzero(seq == s)[:, 0]
+            rows = rows[torch.argsort(lens[rows])]
+            kk, vv, qq = flat(k, s), flat(v, s), q[rows].double().view(n, Hs, dh).transpose(0, 1)
+            sc = torch.matmul(qq, kk.transpose(1, 2).contiguous()) / math.sqrt(dh)
+            hidden = torch.ones((n, n), dtype=torch.bool, device="cuda").triu(1)
+            p = torch.softmax(sc.masked_fill(hidden, -INF), -1)
+            want = torch.matmul(p, vv)
+            mag = torch.matmul(qq.abs(), kk.abs().transpose(1, 2).contiguous()).masked_fill(hidden, 0).amax(-1) / math.sqrt(dh)
+            rel = 2 * ((dh + 4) * E24 * mag + 2.0 ** -22) + 2 * (n + 8) * E24 + (2.0 ** -16 if dtype == BF else 0.0)
+            err = rel[..., None] * torch.matmul(p, vv.abs())
+            got = o[rows].double().view(n, Hs, dh).transpose(0, 1)
+            assert ((got - want).abs() <= U[dtype] * want.abs() + err * (1 + U[dtype])).all()
+            wl = torch.logsumexp(sc.masked_fill(hidden, -INF), -1)
+            assert ((lse[rows].double().t() - wl).abs() <= (dh + 4) * E24 * mag + 2.0 ** -22 + (n + 8) * E24 + wl.abs() * 2.0 ** -23).all()
 
 
 def test_attention_of_values_that_are_no_numbers(lib):

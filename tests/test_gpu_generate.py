@@ -246,6 +246,43 @@ def test_generation_as_it_is_used(lib, name):
             assert hist[s][n] == int(np.argmax(o))
 
 
+@pytest.mark.parametrize("per", [1, 3])
+def test_captured_calls_serve_every_shorter_length(lib, per):
+    """Appending and attention recorded once for up to 6000 tokens (a sequence cut into parts, rows of their own and drafted ones), replayed at other lengths with
+    other inputs: the bits of calls of their own."""
+    stream, g = torch.cuda.Stream(), torch.Generator(device="cuda").manual_seed(5)
+    cfg = si.ModelCfg(arch="llama", d_model=64, n_heads=1, d_head=64, d_ff=8, vocab=8, rope=True, dtype="bf16")
+    randn = lambda *s: torch.randn(s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    with torch.cuda.stream(stream):
+        ctx = lib.Context(lib.desc_from_cfg(cfg), stream)
+        k, v = randn(800, 2, 16, 64), randn(800, 2, 16, 64)
+        cache = lib.PagedCache(k, v, torch.randperm(800, generator=g, device="cuda")[:750].to(torch.int32).view(2, 375))
+        seq = (torch.arange(2 * per, device="cuda") // per).to(torch.int32)
+        lens, qkv, q = torch.ones(2 * per, dtype=torch.int32, device="cuda"), randn(2 * per, 3 * 128), torch.empty((2 * per, 128), dtype=torch.bfloat16, device="cuda")
+        assert ctx.twist_cache_attention_floats(cache, 2 * per, 6000) > 0
+
+        def run():
+            ctx.twist_cache_append_raw(cache, qkv, lens, seq=seq, q_out=q)
+            return ctx.twist_cache_attention_raw(cache, q, lens, 6000, seq=seq)
+        run()
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            o, lse = run()
+        for n in (6000, 1, 700, 5999, 3, 4096):
+            lens.copy_(torch.tensor([max(1, n - per + 1 + i) for i in range(per)] * 2, dtype=torch.int32))
+            lens[-1] = 0 if n == 700 else lens[-1]
+            qkv.copy_(randn(2 * per, 3 * 128))
+            graph.replay()
+            stream.synchronize()
+            got = [x.clone() for x in (o, lse, k, v)]
+            torch.randn(1 << 16, device="cuda").sum().item()         # the program's own eager work between replays
+            want = run()
+            stream.synchronize()
+            for a, b in zip(got, (*want, k, v)):
+                assert torch.equal(a, b), n
+
+
 def test_another_stream_than_the_current_one(lib):
     """A context whose stream is not the current one: the calls' own temporaries live until their kernels are done."""
     stream, g = torch.cuda.Stream(), torch.Generator(device="cuda").manual_seed(3)
