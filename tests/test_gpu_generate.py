@@ -270,7 +270,7 @@ def test_captured_calls_serve_every_shorter_length(lib, per):
         with torch.cuda.graph(graph, stream=stream):
             o, lse = run()
         for n in (6000, 1, 700, 5999, 3, 4096):
-            lens.copy_(torch.tensor([max(1, n - per + 1 + i) for i in range(per)] * 2, dtype=torch.int32))
+            lens.copy_(torch.tensor([max(1, n - per + 1) + i for i in range(per)] * 2, dtype=torch.int32))
             lens[-1] = 0 if n == 700 else lens[-1]
             qkv.copy_(randn(2 * per, 3 * 128))
             graph.replay()
