@@ -603,7 +603,7 @@ Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int row_by
   if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
   if (max_len * pair >= 4 << 20) c = std::min<int64_t>(c, (1 << 20) / pair);
   c = std::max<int64_t>(c, (max_len + kMaxParts - 1) / kMaxParts);
-  c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)kMaxIds << shift);
+  c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)(kMaxIds - 1) << shift);  // (one page more where it begins inside one)
   s.waves = c * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
   s.chunk = (int)c;
   s.parts = (int)((max_len + c - 1) / c);

@@ -88,6 +88,23 @@ def test_attention_refusals(tw):
     tw.lib.twist_destroy(h)
 
 
+@pytest.mark.parametrize("page", [1, 64, 256, 4096])
+def test_a_part_of_a_sequence_lies_on_2048_pages_at_most(tw, page):
+    """Wherever it begins: the kernels keep the places of that many.  Narrow heads have the longest parts; lengths at which a part is no whole number of pages."""
+    n = ctypes.c_size_t()
+    for kw in (dict(d_head=1, rope=False), dict(d_head=2), dict(d_head=2, dtype="f32"), dict(d_head=64)):
+        h = _handle(tw, **kw)
+        for top in [1048448, 2 ** 20 - 128] + [2 ** e - 64 * i for e in range(17, 31) for i in (0, 1, 3, 1027)] + [1024 * (2047 * page + 64 * i) for i in (-1, 0, 1, page // 64)]:
+            pages = -(-top // page)
+            if not 0 < pages * page <= 2 ** 30:
+                continue
+            for units in (1, 2, 64, 128, 300):
+                if tw.lib.twist_cache_attention_floats(h, _pages(tw, page_tokens=page, max_pages=pages, ld_table=pages, n_pages=pages), units, 1, top, ctypes.byref(n)) == 0:
+                    parts = max(1, n.value // (units * (kw["d_head"] + 2)))
+                    assert -(-top // parts) <= 2047 * page, (kw, top, units, parts)
+        tw.lib.twist_destroy(h)
+
+
 def test_logits_refusals(tw):
     h = _handle(tw)
     good = dict(history=P, ld_history=8, hist_cap=8, bias_ids=P, bias_values=P, ld_bias=4, bias_cap=4, allowed=P, ld_allowed=4)

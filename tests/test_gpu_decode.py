@@ -441,6 +441,28 @@ def test_cache_beyond_32_bits(lib):
     assert ((lse.double().cpu() - wl).abs() <= el).all()
 
 
+def test_attention_of_parts_that_begin_inside_a_page(lib):
+    """A million tokens of a head of one number: the longest parts that there are, none a whole number of pages."""
+    Hs, page, n = 128, 256, 1048448
+    ctx, g = _ctx(lib, BF, 1), _gen(6)
+    pages = -(-n // page)
+    k, v = _pools(g, pages, Hs, page, 1, BF)
+    table = torch.randperm(pages, generator=g, device="cuda").to(torch.int32).view(1, -1)
+    q = _randn(g, 1, Hs, dtype=BF)
+    o, lse = ctx.twist_cache_attention_raw(lib.PagedCache(k, v, table), q, _i32(n), n)
+    torch.cuda.synchronize()
+    for h in range(Hs):
+        kk, vv = (p[table[0].long(), h].reshape(-1)[:n].double() for p in (k, v))
+        sc = kk * q[0, h].double()
+        p = torch.softmax(sc, 0)
+        want, wl = (p * vv).sum(), torch.logsumexp(sc, 0)
+        # a lane sums 2^20 / (2 parts, 16 waves, 64 lanes) = 512 tokens at most, the joins add 25
+        ds = 5 * E24 * sc.abs().max() + 2.0 ** -22
+        err = (2 * ds + 2 * 537 * E24) * (p * vv.abs()).sum()
+        assert (o[0, h].double() - want).abs() <= U[BF] * want.abs() + err * (1 + U[BF]), h
+        assert (lse[0, h].double() - wl).abs() <= ds + 537 * E24 + wl.abs() * 2.0 ** -23, h
+
+
 # ------------------------------------------------------------------------------------------------ logits
 def _logits_want(x, r, V):
     """(result, bound) in 64 bits, column by column from the definition."""
