@@ -13,16 +13,20 @@ template <int BF> __device__ __forceinline__ float weight(const void *p, int64_t
   return BF ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16) : static_cast<const float *>(p)[i];
 }
 
-// A wave per row: x = E[token] (+ P[position]), the position being the row's length less one; zeros for unused rows, whose length in
-// `used` becomes 0 (so that nothing is cached for them and they attend to nothing), and for ids outside the vocabulary.
+// A wave per row: x = E[token] (+ P[position]), the position being the row's length less one; zeros for ids outside the vocabulary and for unused rows,
+// which go on as rows of length 0 of sequence 0 (`used`, `of`): nothing is cached for them and they attend to nothing, but what they hold is a number
+// all the same (a projection in fp32 forms tiles with results that are none in another way, rows of other sequences among them).
 template <int BF>
 __global__ __launch_bounds__(kT) void decode_embed_kernel(const int32_t *tokens, const int32_t *seq, const int32_t *lens, int T, int n_seqs, int max_len, const void *E,
-                                                          const void *P, float *x, int32_t *used, int D, int vocab) {
+                                                          const void *P, float *x, int32_t *used, int32_t *of, int D, int vocab) {
   const int t = blockIdx.x * (kT / 64) + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   if (t >= T) return;
   const int len = lens[t], s = seq ? seq[t] : t, tok = tokens[t];
   const bool on = len >= 1 && len <= max_len && (unsigned)s < (unsigned)n_seqs, known = on && (unsigned)tok < (unsigned)vocab;
-  if (lane == 0) used[t] = on ? len : 0;
+  if (lane == 0) {
+    used[t] = on ? len : 0;
+    of[t] = on ? s : 0;
+  }
   for (int c = lane; c < D; c += 64) {
     float v = known ? weight<BF>(E, (int64_t)tok * D + c) : 0.f;
     if (P && on) v += weight<BF>(P, (int64_t)(len - 1) * D + c);
@@ -45,7 +49,7 @@ size_t cache_size(const twist_ctx *ctx, const twist_subnet *sub, const twist_pag
 
 struct Workspace {
   float *x[2], *stats, *scratch;
-  int32_t *used;
+  int32_t *used, *of;
   void *h, *qkv, *q, *o, *gu, *a;
   size_t scratch_floats, bytes;
 };
@@ -72,6 +76,7 @@ twist_status carve(twist_ctx *ctx, const twist_subnet *sub, const twist_pages *p
   for (float *&x : w.x) x = static_cast<float *>(take(T * D * 4));
   w.stats = static_cast<float *>(take((size_t)T * 2 * 4));
   w.used = static_cast<int32_t *>(take((size_t)T * 4));
+  w.of = static_cast<int32_t *>(take((size_t)T * 4));
   w.h = take(T * D * es);
   w.qkv = take(T * 3 * hd * es);
   w.q = d.use_rope ? take(T * hd * es) : nullptr;
@@ -144,10 +149,11 @@ extern "C" twist_status twist_subnet_decode(twist_ctx *ctx, twist_subnet *sub, c
   };
   const dim3 grid((T + kT / 64 - 1) / (kT / 64));
   if (bf) hipLaunchKernelGGL((decode_embed_kernel<1>), grid, dim3(kT), 0, ctx->stream, tokens, seq, lens, T, pages->n_seqs, max_len, P(L.global[TWIST_TOK_EMBED]),
-                             P(L.global[TWIST_POS_EMBED]), w.x[0], w.used, D, d.vocab);
+                             P(L.global[TWIST_POS_EMBED]), w.x[0], w.used, w.of, D, d.vocab);
   else hipLaunchKernelGGL((decode_embed_kernel<0>), grid, dim3(kT), 0, ctx->stream, tokens, seq, lens, T, pages->n_seqs, max_len, P(L.global[TWIST_TOK_EMBED]),
-                          P(L.global[TWIST_POS_EMBED]), w.x[0], w.used, D, d.vocab);
+                          P(L.global[TWIST_POS_EMBED]), w.x[0], w.used, w.of, D, d.vocab);
   TW_HIP(ctx, hipGetLastError());
+  const int32_t *of = seq || T > pages->n_seqs ? w.of : nullptr;  // (row t of sequence t needs no list)
   char *k = static_cast<char *>(cache), *v;
   for (int l = 0; l < d.n_layers; ++l, k = v + pool_bytes(ctx, sub, pages, l - 1)) {
     const int Hs = L.heads_sub[l], HD = Hs * dh, F = L.ffn_sub[l] * d.ffn_granule;
@@ -156,8 +162,8 @@ extern "C" twist_status twist_subnet_decode(twist_ctx *ctx, twist_subnet *sub, c
     v = k + pool_bytes(ctx, sub, pages, l);
     TW_TRY(twist_norm_fwd(ctx, bf, rms, w.x[0], P(L.at(l, TWIST_NORM1_W)), P(L.at(l, TWIST_NORM1_B)), w.h, w.stats, T, D, d.norm_eps));
     TW_TRY(gemm(GEMM_NT, 3 * HD, D, w.h, P(L.at(l, TWIST_WQ)), D, w.qkv, 3 * HD, 0, 1.f, P(L.at(l, TWIST_BQ))));
-    TW_TRY(twist_cache_append_raw(ctx, pages, k, v, page, w.qkv, 3 * HD, T, Hs, seq, w.used, w.q, HD));
-    TW_TRY(twist_cache_attention_raw(ctx, pages, k, v, page, w.q ? w.q : w.qkv, w.q ? HD : 3 * HD, T, Hs, seq, w.used, max_len, w.o, HD, nullptr, w.scratch,
+    TW_TRY(twist_cache_append_raw(ctx, pages, k, v, page, w.qkv, 3 * HD, T, Hs, of, w.used, w.q, HD));
+    TW_TRY(twist_cache_attention_raw(ctx, pages, k, v, page, w.q ? w.q : w.qkv, w.q ? HD : 3 * HD, T, Hs, of, w.used, max_len, w.o, HD, nullptr, w.scratch,
                                      w.scratch_floats));
     TW_TRY(gemm(um ? GEMM_NN : GEMM_NT, D, HD, w.o, P(L.at(l, TWIST_WO)), um ? D : HD, w.x[1], D, 1, c_a, P(L.at(l, TWIST_BO)), w.x[0]));
     TW_TRY(twist_norm_fwd(ctx, bf, rms, w.x[1], P(L.at(l, TWIST_NORM2_W)), P(L.at(l, TWIST_NORM2_B)), w.h, w.stats, T, D, d.norm_eps));

@@ -26,6 +26,8 @@ MODELS = {
     "gpt_bf16": (replace(si.CFG2, n_layers=2, d_model=256, n_heads=4, d_head=64, d_ff=1024, vocab=1003, max_seq=192), 2, 512, None),
     "llama_bf16": (replace(si.CFG3, n_layers=2, d_model=256, n_heads=4, d_head=128, d_ff=704, vocab=517, max_seq=256), 2, 352, None),
     "llama_bf16_um": (replace(si.CFG3, n_layers=2, d_model=256, n_heads=4, d_head=64, d_ff=704, vocab=512, max_seq=256, out_unit_major=True), 3, 352, None),
+    # wide enough for the fp32 products that form a tile anew where one of its results is no number
+    "gpt_f32_wide": (si.ModelCfg(n_layers=1, d_model=512, n_heads=8, d_head=64, d_ff=64, vocab=8003, max_seq=192), 6, 64, None),
     # layers of different widths
     "gpt_bf16_blocks": (replace(si.CFG2, n_layers=3, d_model=384, n_heads=6, d_head=64, d_ff=768, ffn_granule=64, vocab=1003, max_seq=128), 4, 8, [1, 0, 1]),
 }
@@ -150,6 +152,23 @@ def test_unused_rows_change_nothing(lib, name):
         assert changed == 2 * 2 * cfg.n_layers * hs * cfg.d_head
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("name", ["gpt_f32_wide", "llama_f32_um", "llama_bf16"])
+@pytest.mark.parametrize("listed", [True, False])
+def test_what_a_workspace_held_changes_nothing(lib, name, listed):
+    """Rows of no sequence, by the list and beyond the table: the others keep their bits whether the workspace held zeros or NaNs."""
+    T, good = 192, 189
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    out = []
+    for fill in (0, 0xff):
+        d = Deployed(lib, name, good, 16)
+        ws = torch.full((d.ctx.twist_decode_workspace_bytes(d.sub, d.pages, T, 16),), fill, dtype=torch.uint8, device="cuda")
+        seq = i32(list(range(good)) + [-1, good, 2 ** 31 - 1]) if listed else None
+        logits = d.ctx.twist_subnet_decode(d.sub, i32(list(range(T))), i32([1] * T), 16, d.pages, d.cache, ws, seq=seq)
+        torch.cuda.synchronize()
+        out.append(logits[:good].clone())
+    assert torch.isfinite(out[0]).all() and torch.equal(*out)
 
 
 @pytest.mark.parametrize("name", ["llama_f32_um", "gpt_bf16", "llama_bf16_um"])
