@@ -191,13 +191,10 @@ class Context:
         self.h = h
         self.torch_dtype = torch.bfloat16 if desc.dtype == BF16 else torch.float32
         self.device = self.stream.device
-        self.gpu, self.only_gpu = self.device.index, torch.cuda.device_count() == 1
+        self.gpu, self.only_gpu, self.raw_stream = self.device.index, torch.cuda.device_count() == 1, self.stream.cuda_stream
 
-    def _call(self, f, *args, scratch=None):
-        """f(*args) on the context's GPU, also where that is not the current one; `scratch` is a tensor of the caller's current stream that the call's
-        kernels use and nobody holds afterwards."""
-        if scratch is not None and torch.cuda.current_stream(self.device) != self.stream:
-            scratch.record_stream(self.stream)
+    def _call(self, f, *args):
+        """f(*args) on the context's GPU, also where that is not the current one."""
         if self.only_gpu or torch.cuda.current_device() == self.gpu:
             status = f(self.h, *args)
         else:
@@ -205,6 +202,16 @@ class Context:
                 status = f(self.h, *args)
         if status:
             _check(status, self.h)
+
+    def _empty(self, shape, dtype, result=True):
+        """Memory that the context's stream may write at once, whatever the current stream is; `result`: and that the current one may read until it is dropped."""
+        if torch._C._cuda_getCurrentRawStream(self.gpu) == self.raw_stream:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            t = torch.empty(shape, dtype=dtype, device=self.device)
+        if result:
+            t.record_stream(torch.cuda.current_stream(self.device))
+        return t
 
     def close(self):
         if getattr(self, "h", None):
@@ -292,7 +299,7 @@ class Context:
         and values go to the cache (storage of twist_cache_bytes).  See include/twist.h."""
         T, V = tokens.shape[0], self.desc.vocab
         if logits is None:      # rows that start at multiples of 16 bytes
-            logits = torch.empty((T, (V + 7) // 8 * 8), dtype=self.torch_dtype, device=self.device)[:, :V]
+            logits = self._empty((T, (V + 7) // 8 * 8), self.torch_dtype)[:, :V]
         ldl = self._rows(logits, T, V, "logits", self.torch_dtype)
         if pages.gpu != self.gpu or cache.get_device() != self.gpu or workspace.get_device() != self.gpu:
             _refuse(f"table, cache and workspace: need to be on {self.device}")
@@ -495,11 +502,11 @@ class Context:
         T, HD = q.shape[0], cache.Hs * cache.d_head
         ldq = self._rows(q, T, HD, "q", self.torch_dtype)
         if out is None:
-            out, ldo = torch.empty((T, HD), dtype=self.torch_dtype, device=self.device), HD
+            out, ldo = self._empty((T, HD), self.torch_dtype), HD
         else:
             ldo = self._rows(out, T, HD, "out", self.torch_dtype)
         if lse is None:
-            lse = torch.empty((T, cache.Hs), dtype=torch.float32, device=self.device)
+            lse = self._empty((T, cache.Hs), torch.float32)
         elif self._rows(lse, T, cache.Hs, "lse", torch.float32) != cache.Hs:
             _refuse("lse: needs rows without padding")
         n = cache.floats.get((T, max_len))
@@ -507,9 +514,9 @@ class Context:
             if len(cache.floats) > 999:
                 cache.floats.clear()
             n = cache.floats[T, max_len] = self.twist_cache_attention_floats(cache, T, max_len)
-        scratch = torch.empty(n, dtype=torch.float32, device=self.device) if n else None
+        scratch = self._empty(n, torch.float32, result=False) if n else None
         self._call(lib.twist_cache_attention_raw, cache.pages.ref, cache.k_addr, cache.v_addr, cache.page_stride, q.data_ptr(), ldq, T, cache.Hs,
-                   _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n, scratch=scratch)
+                   _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n)
         return out, lse
 
     def twist_logits_raw(self, logits: torch.Tensor, rules: "LogitRules", out: torch.Tensor | None = None) -> torch.Tensor:
@@ -519,7 +526,7 @@ class Context:
         if not (rules.T in (None, T) and rules.gpu in (None, self.gpu) and (rules.words is None or rules.words * 32 >= V)):
             _refuse(f"rules: need {T} rows on {self.device}, and a mask of {(V + 31) // 32} words a row")
         if out is None:
-            out, ldo = torch.empty((T, V), dtype=torch.float32, device=self.device), V
+            out, ldo = self._empty((T, V), torch.float32), V
         else:
             ldo = self._rows(out, T, V, "out", torch.float32)
         self._call(lib.twist_logits_raw, logits.data_ptr(), ld, T, rules.ref, out.data_ptr(), ldo)

@@ -322,6 +322,27 @@ def test_another_stream_than_the_current_one(lib):
         del junk
 
 
+def test_results_that_are_dropped_on_another_stream(lib):
+    """Memory of results that the current stream drops before the context's stream has written them is not handed out again till then."""
+    stream, g = torch.cuda.Stream(), torch.Generator(device="cuda").manual_seed(3)
+    cfg = si.ModelCfg(arch="llama", d_model=64, n_heads=1, d_head=128, d_ff=8, vocab=5000, rope=True, dtype="bf16")
+    ctx = lib.Context(lib.desc_from_cfg(cfg), stream)
+    k, v = (torch.randn((130, 8, 64, 128), generator=g, device="cuda").bfloat16() for _ in range(2))
+    cache = lib.PagedCache(k, v, torch.arange(128, dtype=torch.int32, device="cuda").view(1, -1))
+    q, lens = torch.randn((1, 1024), generator=g, device="cuda").bfloat16(), torch.tensor([8000], dtype=torch.int32).cuda()
+    x, big = torch.randn((1, 5000), generator=g, device="cuda").bfloat16(), torch.empty(1 << 28, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(stream):
+            for _ in range(8):
+                big.fill_(1.0)                                       # the calls wait behind these
+        ctx.twist_cache_attention_raw(cache, q, lens, 8192)
+        ctx.twist_logits_raw(x, lib.LogitRules())
+        mine = [torch.full(s, 3.0, dtype=t, device="cuda") for s, t in (((1, 1024), torch.bfloat16), ((1, 8), torch.float32), ((1, 5000), torch.float32))]
+        torch.cuda.synchronize()
+        assert all((m == 3).all() for m in mine)
+
+
 def test_decode_refusals(lib):
     d = Deployed(lib, "gpt_bf16", 2, 64)
     ok = dict(tokens=[1, 2], lens=[1, 1])
