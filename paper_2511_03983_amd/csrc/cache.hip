@@ -196,7 +196,8 @@ struct AttentionArgs {
   const int32_t *seq, *lens;
   void *o;
   float *lse, *acc_parts, *ml_parts;
-  int32_t T, Hs, dh, max_len, parts, chunk, turns;  // a sequence is cut into `parts` parts of `chunk` tokens
+  int32_t T, Hs, dh, max_len, parts, chunk;  // a sequence is cut into `parts` parts of `chunk` tokens
+  int32_t turns, run, places;                // places: workgroups of a part; turns, run: how they are dealt out (see the kernels)
   float scale;
 };
 
@@ -222,13 +223,24 @@ template <int BF> __device__ __forceinline__ void leave(const AttentionArgs &A, 
 // fetches 64 / G whole rows; a wave has four of them for keys and four for values in flight.  Every group of G lanes runs a softmax of its own over
 // the tokens that it meets (running maximum and sum, one rescaling for four tokens), and nothing is exchanged until the end, where groups, waves
 // and (in cache_attention_join_kernel) parts are joined by the usual rule.  Scores are in base 2: q carries scale * log2(e).
+// Workgroups go to the 8 XCDs in turn, each with an L2 of its own: eight pairs of (run of A.run rows, head) with the runs' first rows, then the same
+// eight with their next rows, so that rows of one sequence find what the first of them read (us for runs of 1 / 8: fp32, 13 heads of 256, 70 sequences of 91
+// tokens, 5 rows each 78.7 / 39.9; 7 x 64, 24 of 1503, 3 rows 41.0 / 24.0; where heads are a multiple of 8 their rows are together anyway, 16 x 64, 8 of 100,
+// 100 rows 24.5 / 27.8).
 template <int BF, int G, bool VEC, int NW>
 __global__ __launch_bounds__(64 * NW) void cache_attention_kernel(AttentionArgs A) {
   constexpr int N = BF ? 8 : 4, TPS = 64 / G, W = G * N, U = 4;
   __shared__ int64_t ids[kMaxIds];
   __shared__ float s_acc[NW][W], s_m[NW], s_l[NW];
   __shared__ int s_seen[NW];
-  const int part = blockIdx.x / (A.T * A.Hs), unit = blockIdx.x % (A.T * A.Hs), h = unit % A.Hs, t = unit / A.Hs;
+  const int part = blockIdx.y, place = blockIdx.x;
+  int pair = place, row = 0;
+  if (A.run > 1) {
+    pair = place / (8 * A.run) * 8 + place % 8;
+    row = place / 8 % A.run;
+  }
+  const int h = pair % A.Hs, t = pair / A.Hs * A.run + row, unit = t * A.Hs + h;
+  if (t >= A.T) return;
   const int s = A.seq ? A.seq[t] : t, given = A.lens[t], dh = A.dh;
   if (given < 0 || (unsigned)s >= (unsigned)A.pg.n_seqs) return;
   const int len = min(given, A.max_len), p0 = part * A.chunk, p1 = min(p0 + A.chunk, len);
@@ -329,7 +341,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_kernel(AttentionArgs 
   }
 }
 
-// ------------------------------------------------------------------------------------------- rows that share a sequence, bf16
+// ------------------------------------------------------------------------------------------- rows that share a sequence
 typedef __bf16 bf16x8v __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2v __attribute__((ext_vector_type(2)));
 typedef short s16x4v __attribute__((ext_vector_type(4)));
@@ -344,15 +356,20 @@ constexpr int kTile = 16;  // rows of a group
 // are the eight contraction indices that the lane has in O^T += V^T P^T, so the weights stay where they are; the values pass through LDS (a tile
 // of the wave's own, no barrier) and come back transposed in the same order of tokens.  Weights go in as two bf16 terms, cut off and rounded: at most 2^-16 of
 // them is lost, a fraction of the rounding of the output (2^-9).  What bounds it is the reading again, of 16 rows at once.
-template <int KS, int NW>
+// fp32: v_mfma_f32_16x16x4_f32, of which an instruction takes one of the four numbers in a lane's 16 bytes of a key; four tokens of values are 4 x 256
+// bytes as they lie, lane (j, c) with elements 4 c .. 4 c + 3 of token 4 j + e: number i of them belongs to an accumulator of elements 4 k + i, so that
+// nothing passes through LDS.  Loads and products of a wave take turns: 45 to 60 % of the read rate, where one row a sequence reaches 75 to 93.
+template <int BF, int KS, int NW>
 __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(AttentionArgs A) {
-  constexpr int MT = 2 * KS, RB = 64 * KS + 32, TILE_B = 32 * RB, LDR = 32 * KS + 4;  // bytes of a row of values in LDS (the padding spreads the banks), floats of one of results
+  constexpr int ES = BF ? 2 : 4, N = 16 / ES, VB = (KS + 3) / 4, MT = BF ? 2 * KS : 4 * VB;
+  constexpr int RB = 64 * KS + 32, LDR = 16 * MT + 4;  // bytes of a row of values in LDS, floats of one of results (the padding spreads the banks)
+  constexpr int TILE_B = BF ? 32 * RB : kTile * LDR * 4;
   static_assert(kTile * LDR * 4 <= TILE_B, "results take the place of the values");
   __shared__ int64_t ids[kMaxIds];
   __shared__ __attribute__((aligned(16))) char tiles[NW][TILE_B];
   __shared__ float s_m[NW][kTile], s_l[NW][kTile];
   __shared__ int s_seen[NW][kTile];
-  const int units = (A.T + kTile - 1) / kTile * A.Hs, unit = blockIdx.x % units, turn = blockIdx.x / units % A.turns, part = blockIdx.x / units / A.turns;
+  const int units = A.places / A.turns, unit = blockIdx.x % units, turn = blockIdx.x / units, part = blockIdx.y;
   const int h = unit % A.Hs, t0 = unit / A.Hs * kTile, dh = A.dh;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane >> 4, c = lane & 15;
   // the first rows of the groups among rows t0 .. t0 + 15, of which every A.turns-th is this workgroup's
@@ -382,10 +399,10 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
       ids[i] = (unsigned)page < (unsigned)A.pg.n_pages ? page * A.page_stride + (((int64_t)h << shift)) * dh : -1;
     }
     const u32x4v none = {0u, 0u, 0u, 0u};
-    const char *q = static_cast<const char *>(A.q) + ((t + min(c, rows - 1)) * A.ldq + (int64_t)h * dh) * 2;
+    const char *q = static_cast<const char *>(A.q) + ((t + min(c, rows - 1)) * A.ldq + (int64_t)h * dh) * ES;
     u32x4v qf[KS];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) qf[k] = 32 * k + 8 * j < dh ? *reinterpret_cast<const u32x4v *>(q + 64 * k + 16 * j) : none;
+    for (int k = 0; k < KS; ++k) qf[k] = (4 * k + j) * N < dh ? *reinterpret_cast<const u32x4v *>(q + 64 * k + 16 * j) : none;
     f32x4v acc[MT];
 #pragma unroll
     for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
@@ -395,7 +412,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
     const int wr = c * RB + 16 * j, rd = (4 * j + (c >> 2)) * RB + (c & 3) * 8;  // where the lane's values go, and what it reads of 4 x 16 of them
     __syncthreads();
     for (int tok0 = p0 + 32 * wave; tok0 < p1; tok0 += 32 * NW) {
-      u32x4v kf[2][KS], vf[2][KS];
+      u32x4v kf[2][KS], vf[2][BF ? KS : 4 * VB];
       uint32_t there = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -403,20 +420,41 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
         const int64_t base = ids[min((tok >> shift) - first, n_ids - 1)];
         const bool ok = tok < p1 && base >= 0;
         there |= ((uint32_t)__ballot(ok) & 0xffffu) << (16 * i);
-        const int64_t at = (ok ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0) * 2 + 16 * j;  // (unused ones read the pool's first row)
+        const int64_t at = (ok ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0) * ES + 16 * j;  // (unused ones read the pool's first row)
         const char *kp = static_cast<const char *>(A.k) + at, *vp = static_cast<const char *>(A.v) + at;
 #pragma unroll
-        for (int k = 0; k < KS; ++k) kf[i][k] = 32 * k + 8 * j < dh ? *reinterpret_cast<const u32x4v *>(kp + 64 * k) : none;
+        for (int k = 0; k < KS; ++k) kf[i][k] = (4 * k + j) * N < dh ? *reinterpret_cast<const u32x4v *>(kp + 64 * k) : none;
+        if constexpr (BF) {
 #pragma unroll
-        for (int k = 0; k < KS; ++k) vf[i][k] = 32 * k + 8 * j < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 64 * k) : none;
+          for (int k = 0; k < KS; ++k) vf[i][k] = (4 * k + j) * N < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 64 * k) : none;
+        }
+      }
+      if constexpr (!BF) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int tok = tok0 + 16 * i + 4 * j + e;
+            const int64_t base = ids[min((tok >> shift) - first, n_ids - 1)];
+            const bool ok = tok < p1 && base >= 0;
+            const char *vp = static_cast<const char *>(A.v) + (ok ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0) * 4 + 16 * c;
+#pragma unroll
+            for (int b = 0; b < VB; ++b) vf[i][4 * b + e] = 64 * b + 4 * c < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 256 * b) : none;
+          }
       }
       __builtin_amdgcn_sched_barrier(0);  // (all loads before the first product)
       f32x4v sc[2] = {f32x4v{0.f, 0.f, 0.f, 0.f}, f32x4v{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
-          sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[i][k]), __builtin_bit_cast(bf16x8v, qf[k]), sc[i], 0, 0, 0);
+        for (int k = 0; k < KS; ++k) {
+          if constexpr (BF) {
+            sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[i][k]), __builtin_bit_cast(bf16x8v, qf[k]), sc[i], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][k][e]), __uint_as_float(qf[k][e]), sc[i], 0, 0, 0);
+          }
+        }
       const bool whole = there == 0xffffffffu && tok0 + 32 <= shortest;
       uint32_t on = 0xffu;  // which of the lane's eight tokens its row sees
       if (!whole) {
@@ -441,66 +479,111 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
         m = mn;
       }
       float p[8];
-      u32x4v hi, lo;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         p[e] = __builtin_amdgcn_exp2f((sc[e >> 2][e & 3] - ref) * A.scale);
         l += p[e];
       }
+      if constexpr (BF) {
+        u32x4v hi, lo;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t a = __float_as_uint(p[2 * e]), b = __float_as_uint(p[2 * e + 1]);
-        hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-        typedef float f32x2 __attribute__((ext_vector_type(2)));
-        const f32x2 rest = {p[2 * e] - __uint_as_float(a & 0xffff0000u), p[2 * e + 1] - __uint_as_float(b & 0xffff0000u)};
-        lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
-      }
-      typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-      u16x2 top = {0, 0};  // largest magnitude among the values
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          *reinterpret_cast<u32x4v *>(tile + 16 * i * RB + wr + 64 * k) = vf[i][k];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[i][k][e] & 0x7fff7fffu));
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t a = __float_as_uint(p[2 * e]), b = __float_as_uint(p[2 * e + 1]);
+          hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
+          typedef float f32x2 __attribute__((ext_vector_type(2)));
+          const f32x2 rest = {p[2 * e] - __uint_as_float(a & 0xffff0000u), p[2 * e + 1] - __uint_as_float(b & 0xffff0000u)};
+          lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
         }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // read by the wave's other lanes
-      if (!__any(top.x >= 0x7f80 || top.y >= 0x7f80)) {
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        u16x2 top = {0, 0};  // largest magnitude among the values
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          typedef s16x4v __attribute__((address_space(3))) * lds_ptr;
-          const s16x4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + rd + 32 * i)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + 16 * RB + rd + 32 * i));
-          const bf16x8v vt = __builtin_bit_cast(bf16x8v, s16x8v{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, hi), acc[i], 0, 0, 0);
-          acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, lo), acc[i], 0, 0, 0);
-        }
-      } else {  // infinities and NaNs, which times the zero of a term or of a hidden token are no number: one by one, for the rows that see them
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-#pragma unroll 1
-          for (int x = 0; x < 4; ++x) {
-            const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
-            const float w = __shfl(p[e], 16 * x + c, 64);
-            if (!(there >> tok & 1) || tok0 + tok >= len) continue;
+          for (int k = 0; k < KS; ++k) {
+            *reinterpret_cast<u32x4v *>(tile + 16 * i * RB + wr + 64 * k) = vf[i][k];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-              const u32x2v u = *reinterpret_cast<const u32x2v *>(tile + tok * RB + 32 * i + 8 * j);
-              acc[i][0] = fmaf(w, __uint_as_float(u.x << 16), acc[i][0]);
-              acc[i][1] = fmaf(w, __uint_as_float(u.x & 0xffff0000u), acc[i][1]);
-              acc[i][2] = fmaf(w, __uint_as_float(u.y << 16), acc[i][2]);
-              acc[i][3] = fmaf(w, __uint_as_float(u.y & 0xffff0000u), acc[i][3]);
-            }
+            for (int e = 0; e < 4; ++e) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, vf[i][k][e] & 0x7fff7fffu));
           }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // read by the wave's other lanes
+        if (!__any(top.x >= 0x7f80 || top.y >= 0x7f80)) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            typedef s16x4v __attribute__((address_space(3))) * lds_ptr;
+            const s16x4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + rd + 32 * i)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + 16 * RB + rd + 32 * i));
+            const bf16x8v vt = __builtin_bit_cast(bf16x8v, s16x8v{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, hi), acc[i], 0, 0, 0);
+            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, lo), acc[i], 0, 0, 0);
+          }
+        } else {  // infinities and NaNs, which times the zero of a term or of a hidden token are no number: one by one, for the rows that see them
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+            for (int x = 0; x < 4; ++x) {
+              const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
+              const float w = __shfl(p[e], 16 * x + c, 64);
+              if (!(there >> tok & 1) || tok0 + tok >= len) continue;
+#pragma unroll
+              for (int i = 0; i < MT; ++i) {
+                const u32x2v u = *reinterpret_cast<const u32x2v *>(tile + tok * RB + 32 * i + 8 * j);
+                acc[i][0] = fmaf(w, __uint_as_float(u.x << 16), acc[i][0]);
+                acc[i][1] = fmaf(w, __uint_as_float(u.x & 0xffff0000u), acc[i][1]);
+                acc[i][2] = fmaf(w, __uint_as_float(u.y << 16), acc[i][2]);
+                acc[i][3] = fmaf(w, __uint_as_float(u.y & 0xffff0000u), acc[i][3]);
+              }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next tokens' values take the place of these
+      } else {
+        uint32_t top = 0;  // largest magnitude among the values
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int b = 0; b < 4 * VB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top = max(top, vf[i][b][e] & 0x7fffffffu);
+        if (!__any(top >= 0x7f800000u)) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+              acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[e >> 2][(i & ~3) + (e & 3)][i & 3]), p[e], acc[i], 0, 0, 0);
+        } else {  // as above; the values from memory again
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+            for (int x = 0; x < 4; ++x) {
+              const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
+              const float w = __shfl(p[e], 16 * x + c, 64);
+              if (!(there >> tok & 1) || tok0 + tok >= len) continue;
+              const float *vp = static_cast<const float *>(A.v) + ids[((tok0 + tok) >> shift) - first] + (int64_t)((tok0 + tok) & ((1 << shift) - 1)) * dh;
+#pragma unroll
+              for (int b = 0; b < VB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                  const int el = 64 * b + 16 * j + 4 * r;
+                  if (el < dh) {
+                    const f32x4v u = *reinterpret_cast<const f32x4v *>(vp + el);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[4 * b + i][r] = fmaf(w, u[i], acc[4 * b + i][r]);
+                  }
+                }
+            }
+        }
       }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next tokens' values take the place of these
     }
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
     const uint64_t any = __ballot(seen);
     float *res = reinterpret_cast<float *>(tile);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) *reinterpret_cast<f32x4v *>(res + c * LDR + 16 * i + 4 * j) = acc[i];
+    for (int i = 0; i < MT; ++i) {
+      if constexpr (BF) {
+        *reinterpret_cast<f32x4v *>(res + c * LDR + 16 * i + 4 * j) = acc[i];
+      } else {  // (elements 4 k + i % 4 of its 64)
+        const int b = i >> 2, r = i & 3;
+        *reinterpret_cast<f32x4v *>(res + c * LDR + 64 * b + 16 * j + 4 * r) = f32x4v{acc[4 * b][r], acc[4 * b + 1][r], acc[4 * b + 2][r], acc[4 * b + 3][r]};
+      }
+    }
     if (j == 0) { s_m[wave][c] = m; s_l[wave][c] = l; s_seen[wave][c] = (any >> c | any >> (c + 16) | any >> (c + 32) | any >> (c + 48)) & 1; }
     __syncthreads();
     for (int i = tid; i < rows * dh; i += 64 * NW) {
@@ -518,7 +601,7 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
         L += x * s_l[w][r];
         a += x * reinterpret_cast<const float *>(tiles[w])[r * LDR + e];
       }
-      leave<1>(A, (int64_t)(t + r) * A.Hs + h, part, t + r, h, e, a, M * A.scale, L, some);
+      leave<BF>(A, (int64_t)(t + r) * A.Hs + h, part, t + r, h, e, a, M * A.scale, L, some);
     }
     __syncthreads();
   }
@@ -579,25 +662,31 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
   finish<BF>(A, t, h, tid, a, M, L, any);
 }
 
-// Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens (row_bytes: of a head's key).  Figures
-// are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
-//  - Tiles (turns > 0): where there are at least twice as many rows as sequences, so that most of them must share one.  A workgroup takes every turns-th
-//    group among 16 rows.  Tiles / rows by themselves: (16 x 16) x 2000, 4 rows each 44 / 68, x 8000, 8 rows each 148 / 351, a prompt of 1000, 8 heads 36 / 173;
-//    one row a sequence, (32 x 16) x 16384 527 / 507, 12 heads of 64 x 1000 11.5 / 7.1.
+// Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens.  Figures are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
+//  - Tiles (turns > 0; a workgroup takes every turns-th group among 16 rows): where sequences have several rows each on average, the more the shorter they may be
+//    (rows beyond 16 a sequence fill no more of a tile), and enough of both to fill the chip.  bf16, (heads x sequences) x tokens, r rows each, rows / tiles: (16 x 16) x 64, 16 rows 12.5 / 7.1,
+//    (16 x 64) x 64, 8 rows 23.8 / 27.1, x 250 47 / 37.7, (12 x 32) of 64 x 100, 5 rows 8.8 / 10.9, x 300 15.8 / 15.6, (19 x 19) x 926, 8 rows 83 / 34.8, a prompt of 1000,
+//    8 heads 173 / 36; few rows: (8 x 6) x 1172, 2 rows 12.6 / 17.3, (15 x 4) x 343, 8 rows 9.6 / 11.8, (30 x 2) of 64 x 1299, 8 rows 14.7 / 15.6.
+//    fp32, whose matrix instruction has a sixteenth of the rate: (12 x 32) of 64 x 400, 5 rows 19.3 / 26, (16 x 16) of 64 x 128, 16 rows 13.5 / 9.6,
+//    (29 x 24) of 96 x 1512, 8 rows 547 / 138, (12 x 8) of 64 x 1003, 4 rows 14.3 / 19, (16 x 4) x 4170, 3 rows 64 / 54, (12 x 40) of 64 x 2133, 2 rows 77 / 89; a prompt
+//    of 2000, 16 heads 1089 / 342.
 //  - Up to 384 KB of keys and values a head are read by one workgroup; where heads and rows are at most half the CUs, longer sequences are cut so that there are
 //    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
 //    8 x 4096 22 / 10.5 / 11, 32 x 2048 17 / 12.6 / 12.5, 32 x 8192 - / 30.5 / 32.5, 16 x 32768 - / 53.4 / 55.2;
-//    beyond that half, 12 heads of 64 x 16 in fp32 x 2000 32 / 35 / -.  Tiles, whose waves take 32 tokens at a
-//    time: 256 KB (16 heads x 4096, 8 rows: parts of 256 / 512 / 1024 22.9 / 18.5 / 25).
+//    beyond that half, 12 heads of 64 x 16 in fp32 x 2000 32 / 35 / -.  Tiles, whose waves take 32 tokens at a time: 256 KB (16 heads x 4096, 8 rows: parts of 256 / 512 / 1024 22.9 / 18.5 / 25).
 //  - From 4 MB on parts of 1 MB even out rows of different lengths: uncut / cut (32 x 16) x 16384 511 / 478, (16 x 16) x 8192 143 / 134, (32 x 16) x 8192 259 / 260; on
 //    the other side (32 x 16) x 4096 132 / 134, (16 x 128) x 2048 238 / 246.
 //  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
 //    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.
-struct Split { int waves, parts, chunk, turns; };
-Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int row_bytes, bool tiles) {
+struct Split { int waves, parts, chunk, turns, run, places; };
+Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int dh, int es, bool listed, bool tiles) {
   Split s;
-  const int64_t blocks = (T + kTile - 1) / kTile, pair = 2 * row_bytes;
-  s.turns = tiles && T >= 2 * (int64_t)n_seqs ? std::min({8, T, std::max(1, (int)((int64_t)kTile * n_seqs / T))}) : 0;
+  const int64_t blocks = (T + kTile - 1) / kTile, row_bytes = dh * es, pair = 2 * row_bytes;
+  tiles = tiles && T >= (es == 2 ? 2 : 3) * (int64_t)n_seqs && std::min<int64_t>(16 * (int64_t)n_seqs, T) * max_len >= (es == 2 ? 1024 : 2048) * (int64_t)n_seqs &&
+          (T * Hs >= 2048 || (int64_t)T * Hs * dh >= ((1 << 25) + max_len - 1) / max_len);
+  s.turns = tiles ? std::min({8, T, (int)(((int64_t)kTile * n_seqs + T - 1) / T)}) : 0;
+  s.run = listed && T >= 2 * (int64_t)n_seqs && Hs % 8 ? std::min(T, 8) : 1;
+  s.places = (int)(tiles ? blocks * s.turns * Hs : s.run > 1 ? ((int64_t)(T + s.run - 1) / s.run * Hs + 7) / 8 * 8 * s.run : (int64_t)T * Hs);
   const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
   int64_t c = max_len;
   if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
@@ -636,10 +725,10 @@ Pages device_pages(const twist_pages *p) {
   return {p->table, p->ld_table, p->n_seqs, p->max_pages, p->n_pages, __builtin_ctz((unsigned)p->page_tokens)};
 }
 
-Split attention_split(const twist_ctx *ctx, const twist_pages *p, int T, int Hs, int &max_len, bool seq) {
+// listed: the rows' sequences are given (several may name one); vec: pieces of 16 bytes all through
+Split attention_split(const twist_ctx *ctx, const twist_pages *p, int T, int Hs, int &max_len, bool listed, bool vec) {
   max_len = (int)std::min<int64_t>(max_len, (int64_t)p->max_pages * p->page_tokens);
-  return choose_split(T, p->n_seqs, Hs, max_len, __builtin_ctz((unsigned)p->page_tokens), ctx->d.d_head * ctx->esize(),
-                      seq && ctx->d.dtype == TWIST_BF16 && ctx->d.d_head % 8 == 0);
+  return choose_split(T, p->n_seqs, Hs, max_len, __builtin_ctz((unsigned)p->page_tokens), ctx->d.d_head, ctx->esize(), listed, listed && vec);
 }
 
 void launch_attention_join(int bf16, hipStream_t st, const AttentionArgs &a) {
@@ -650,7 +739,7 @@ void launch_attention_join(int bf16, hipStream_t st, const AttentionArgs &a) {
 }
 template <int BF, int G, bool VEC>
 void launch_attention(hipStream_t st, const AttentionArgs &a, int waves) {
-  const dim3 grid((unsigned)((int64_t)a.T * a.Hs * a.parts));
+  const dim3 grid((unsigned)a.places, (unsigned)a.parts);
   if (waves == 16) hipLaunchKernelGGL((cache_attention_kernel<BF, G, VEC, 16>), grid, dim3(1024), 0, st, a);
   else hipLaunchKernelGGL((cache_attention_kernel<BF, G, VEC, 4>), grid, dim3(256), 0, st, a);
 }
@@ -667,23 +756,36 @@ void launch_attention_of(hipStream_t st, const AttentionArgs &a, int waves) {
   if (a.parts > 1) launch_attention_join(BF, st, a);
 }
 
-template <int KS>
+template <int BF, int KS>
 void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a) {
-  constexpr int NW = KS > 4 ? 4 : 8;
-  hipLaunchKernelGGL((cache_attention_tile_kernel<KS, NW>), dim3((unsigned)((int64_t)((a.T + kTile - 1) / kTile) * a.turns * a.Hs * a.parts)), dim3(64 * NW), 0, st, a);
+  constexpr int NW = KS > (BF ? 4 : 8) ? 4 : 8;
+  hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW>), dim3((unsigned)a.places, (unsigned)a.parts), dim3(64 * NW), 0, st, a);
 }
-void launch_attention_tile(hipStream_t st, const AttentionArgs &a) {
-  switch ((a.dh + 31) / 32) {
-    case 1: launch_attention_tile_of<1>(st, a); break;
-    case 2: launch_attention_tile_of<2>(st, a); break;
-    case 3: launch_attention_tile_of<3>(st, a); break;
-    case 4: launch_attention_tile_of<4>(st, a); break;
-    case 5: launch_attention_tile_of<5>(st, a); break;
-    case 6: launch_attention_tile_of<6>(st, a); break;
-    case 7: launch_attention_tile_of<7>(st, a); break;
-    default: launch_attention_tile_of<8>(st, a); break;
+void launch_attention_tile(int bf16, hipStream_t st, const AttentionArgs &a) {
+  const int pieces = (a.dh * (bf16 ? 2 : 4) + 63) / 64;  // of 64 bytes
+  if (bf16) {
+    switch (pieces) {
+      case 1: launch_attention_tile_of<1, 1>(st, a); break;
+      case 2: launch_attention_tile_of<1, 2>(st, a); break;
+      case 3: launch_attention_tile_of<1, 3>(st, a); break;
+      case 4: launch_attention_tile_of<1, 4>(st, a); break;
+      case 5: launch_attention_tile_of<1, 5>(st, a); break;
+      case 6: launch_attention_tile_of<1, 6>(st, a); break;
+      case 7: launch_attention_tile_of<1, 7>(st, a); break;
+      default: launch_attention_tile_of<1, 8>(st, a); break;
+    }
+  } else if (pieces <= 2) {
+    launch_attention_tile_of<0, 2>(st, a);
+  } else if (pieces <= 4) {
+    launch_attention_tile_of<0, 4>(st, a);
+  } else if (pieces <= 8) {
+    launch_attention_tile_of<0, 8>(st, a);
+  } else if (pieces <= 12) {
+    launch_attention_tile_of<0, 12>(st, a);
+  } else {
+    launch_attention_tile_of<0, 16>(st, a);
   }
-  if (a.parts > 1) launch_attention_join(1, st, a);
+  if (a.parts > 1) launch_attention_join(bf16, st, a);
 }
 
 bool al16(const void *p, int64_t stride_bytes = 0) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride_bytes % 16 == 0; }
@@ -733,10 +835,10 @@ extern "C" twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist
   TW_TRY(check_cache(ctx, who, pages, (int64_t)Hs * ctx->d.d_head * pages->page_tokens, T, Hs));
   if (max_len < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: max_len=%d", who, max_len);
   size_t need = 0;
-  for (int seq = 0; seq < 2; ++seq) {  // the caller's rows may share sequences, or not
+  for (int form = 0; form < 3; ++form) {  // whether the caller's rows may share sequences, and how they are aligned, is not known here
     int most = max_len;
-    const Split s = attention_split(ctx, pages, T, Hs, most, seq);
-    if (s.parts > kMaxParts || (int64_t)T * Hs * s.parts >= (int64_t)1 << 22)  // (workgroups of 1024 threads, of which a launch has less than 2^32)
+    const Split s = attention_split(ctx, pages, T, Hs, most, form > 0, form > 1 && ctx->d.d_head * ctx->esize() % 16 == 0);
+    if (s.parts > kMaxParts || (int64_t)s.places * s.parts >= (int64_t)1 << 22)  // (workgroups of 1024 threads, of which a launch has less than 2^32)
       TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
     if (s.parts > 1) need = std::max(need, (size_t)T * Hs * s.parts * (ctx->d.d_head + 2));
   }
@@ -764,15 +866,15 @@ extern "C" twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pa
   a.page_stride = page_stride; a.ldq = ldq; a.ldo = ldo;
   a.seq = seq; a.lens = lens; a.lse = lse;
   a.T = T; a.Hs = Hs; a.dh = dh; a.max_len = max_len;
-  const Split split = attention_split(ctx, pages, T, Hs, a.max_len, seq != nullptr);
-  a.turns = split.turns; a.parts = split.parts; a.chunk = split.chunk;
+  const int es = ctx->esize();
+  const bool vec = dh * es % 16 == 0 && al16(k, page_stride * es) && al16(v) && al16(q, ldq * es);
+  const Split split = attention_split(ctx, pages, T, Hs, a.max_len, seq != nullptr, vec);
+  a.turns = split.turns; a.run = split.run; a.places = split.places; a.parts = split.parts; a.chunk = split.chunk;
   a.ml_parts = scratch;
   a.acc_parts = need ? scratch + (size_t)T * Hs * a.parts * 2 : nullptr;
   a.scale = 1.44269504089f / sqrtf((float)dh);
-  const int es = ctx->esize();
-  const bool vec = dh * es % 16 == 0 && al16(k, page_stride * es) && al16(v) && al16(q, ldq * es);
-  if (split.turns && vec) {
-    launch_attention_tile(ctx->stream, a);
+  if (split.turns) {
+    launch_attention_tile(ctx->d.dtype == TWIST_BF16, ctx->stream, a);
     TW_HIP(ctx, hipGetLastError());
     return TWIST_OK;
   }

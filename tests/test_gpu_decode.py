@@ -345,13 +345,68 @@ def test_attention_of_a_long_prompt(lib, dtype):
             assert ((lse[rows].double().t() - wl).abs() <= (dh + 4) * E24 * mag + 2.0 ** -22 + (n + 8) * E24 + wl.abs() * 2.0 ** -23).all()
 
 
-def test_attention_of_values_that_are_no_numbers(lib):
+def _tiled(lens, seq, Hs, dh, max_len):
+    """The rows, and as many unused ones behind them as make a call large enough for tiles of 16 rows (2^25 products of a score, 256 tokens)."""
+    more = max(0, -(-2 ** 25 // (Hs * dh * max_len)) - len(lens))
+    return lens + [-1] * more, seq + [(-1, 0, 99)[i // 5 % 3] for i in range(more)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hs,dh,page", [(2, 128, 16), (3, 64, 16), (2, 32, 8), (1, 256, 16), (3, 40, 32), (2, 80, 16), (1, 96, 64), (2, 24, 8), (4, 8, 1), (1, 160, 16), (1, 192, 16), (1, 224, 16),
+                                        (9, 16, 4), (2, 112, 128)])
+def test_attention_in_tiles_of_rows(lib, dtype, Hs, dh, page):
+    """Runs of rows of one sequence that start and end anywhere, in any order of lengths, beside rows of their own and unused ones; NaN behind each sequence."""
+    check = lambda lens, seq, n_seqs, **kw: _check_attention(lib, dtype, Hs, dh, page, *_tiled(lens, seq, Hs, dh, 300), n_seqs=n_seqs, max_len=300, max_pages=-(-300 // page), **kw)  # noqa: E731
+    check([97, 98, 99, 100, 1, 2, 3, 40, 41, 0, 50, 50, -1], [0, 0, 0, 0, 2, 2, 2, 1, 1, 1, 7, -1, 0], 3)
+    check(list(range(1, 71)), [0] * 70, 1)                                                   # a whole prompt at once
+    check(list(range(230, 195, -1)) + [-1, 0, 3, 299, 300], [1] * 40, 2)
+    check([20, 33, 4, 290], [0, -1, 0, 0], 1, holes=[(0, 0), (0, 200 // page)])
+    check([1, 64, 65, 200, 0, 31, 32, 33, 16, 17, 300], list(range(11)), 11)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hs,dh,top", [(1, 128, 5000), (2, 64, 4503), (1, 40, 9000), (1, 256, 3001)])
+def test_attention_in_tiles_over_long_sequences(lib, dtype, Hs, dh, top):
+    """Sequences cut into parts, the last of which only some rows of a tile reach, missing pages among them."""
+    lens, seq = [top - 3, top - 2, top - 1, top, 2048, 2049, 1, 0, -1, 700, 2500, 2501], [0] * 9 + [1] * 3
+    check = lambda **kw: _check_attention(lib, dtype, Hs, dh, 16, *_tiled(lens, seq, Hs, dh, top), n_seqs=2, max_len=top, **kw)  # noqa: E731
+    check()
+    check(holes=[(0, 3), (1, 0), (1, 156)] + [(0, i) for i in range(64, 160)])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_in_tiles_of_values_that_are_no_numbers(lib, dtype):
     """An infinity reaches the rows that see it and no others, also where their scores leave nothing of a term of its weight."""
-    ctx, g, dh = _ctx(lib, BF, 64), _gen(8), 64
-    k, v = _pools(g, 8, 1, 16, dh, BF)
+    ctx, g, dh = _ctx(lib, dtype, 64), _gen(8), 64
+    k, v = _pools(g, 20, 1, 16, dh, dtype)
+    table = torch.arange(20, dtype=torch.int32, device="cuda").view(1, -1)
+    cache = lib.PagedCache(k, v, table)
+    lens, seq = _tiled([40, 41, 100, 320], [0, 0, 0, 0], 1, dh, 320)
+    q = torch.zeros((len(lens), dh), dtype=_dt(dtype), device="cuda")
+    lens, seq = _i32(*lens), _i32(*seq)
+    base = ctx.twist_cache_attention_raw(cache, q, lens, 320, seq=seq)[0][:4].clone()
+    v[2, 0, 8, 5] = INF                                    # token 40: the last of row 1, none of row 0
+    v[6, 0, 2, 7] = -INF                                   # token 98
+    v[16, 0, 5, 9] = NAN                                   # token 261: row 3 only
+    o = ctx.twist_cache_attention_raw(cache, q, lens, 320, seq=seq)[0][:4]
+    torch.cuda.synchronize()
+    assert torch.equal(o[0], base[0])
+    assert (o[1:, 5] == INF).all() and torch.isfinite(o[1, 7]) and (o[2:, 7] == -INF).all()
+    assert torch.isfinite(o[:3, 9]).all() and torch.isnan(o[3, 9])
+    rest = [e for e in range(dh) if e not in (5, 7, 9)]
+    # (such tokens go another way through the kernel: equal up to the 2^-16 of the weights' bf16 terms, or 320 + 8 roundings, and one rounding of the output)
+    top = v[torch.isfinite(v)].float().abs().max()
+    assert ((o - base).float().abs()[:, rest] <= 2 * U[dtype] * base.float().abs()[:, rest] + (2.0 ** -15 if dtype == BF else 328 * E24) * top).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_attention_of_values_that_are_no_numbers(lib, dtype):
+    """An infinity reaches the rows that see it and no others, also where their scores leave nothing of a term of its weight."""
+    ctx, g, dh = _ctx(lib, dtype, 64), _gen(8), 64
+    k, v = _pools(g, 8, 1, 16, dh, dtype)
     table = torch.arange(8, dtype=torch.int32, device="cuda").view(1, -1)
     cache = lib.PagedCache(k, v, table)
-    q = torch.zeros((4, dh), dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros((4, dh), dtype=_dt(dtype), device="cuda")
     lens, seq = _i32(40, 41, 100, 128), _i32(0, 0, 0, 0)
     base, _ = ctx.twist_cache_attention_raw(cache, q, lens, 128, seq=seq)
     v[2, 0, 8, 5] = INF                                    # token 40: the last of row 1, none of row 0
@@ -363,8 +418,8 @@ def test_attention_of_values_that_are_no_numbers(lib):
     assert (o[1:, 5] == INF).all() and torch.isfinite(o[1, 7]) and (o[2:, 7] == -INF).all()
     assert torch.isfinite(o[:3, 9]).all() and torch.isnan(o[3, 9])
     rest = [e for e in range(dh) if e not in (5, 7, 9)]
-    # (such tokens go another way through the kernel: equal up to the 2^-16 of the weights' terms and one rounding)
-    assert ((o - base).float().abs()[:, rest] <= 2.0 ** -7 * base.float().abs()[:, rest] + 2.0 ** -15).all()
+    # (such tokens go another way through the kernel: equal up to the 2^-16 of the weights' bf16 terms, or 128 + 8 roundings, and one rounding of the output)
+    assert ((o - base).float().abs()[:, rest] <= 2 * U[dtype] * base.float().abs()[:, rest] + (2.0 ** -15 if dtype == BF else 136 * E24 * v[torch.isfinite(v)].abs().max())).all()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
