@@ -243,7 +243,8 @@ typedef struct {
  *   cache    (dev, 256-byte aligned, >= twist_cache_bytes) the pools of all layers, caller-owned, need not be cleared: what is beyond a sequence's
  *            length is never used.  Valid for this subnet's widths and this n_pages and page_tokens.
  *   max_len  (host) the longest length of this call, at most desc.max_seq; kernels and workspace (dev, 256-byte aligned, >=
- *            twist_decode_workspace_bytes) are chosen by it and T alone, so a captured step serves all shorter lengths.
+ *            twist_decode_workspace_bytes) are chosen by it, T and the table's shape alone, so a captured step serves all shorter lengths.  The
+ *            workspace carries nothing from call to call; calls that may run at the same time need one each.
  * No loss, no gradients, any storage mode.  TWIST_ESHAPE without a vocabulary, and as twist_subnet_forward. */
 TWIST_API twist_status twist_cache_bytes(twist_ctx *ctx, const twist_subnet *sub, const twist_pages *pages, size_t *bytes);
 TWIST_API twist_status twist_decode_workspace_bytes(twist_ctx *ctx, const twist_subnet *sub, const twist_pages *pages, int32_t T, int32_t max_len, size_t *bytes);
@@ -401,7 +402,8 @@ TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32
  *                            sees no token gives o = 0, lse = -infinity; one with lens[t] < 0 or a seq[t] outside [0, n_seqs) is left as it was.  What lies
  *                            in the pools beyond lens[t] is never used.  max_len (host): no row sees more than its first max_len tokens; kernels are
  *                            chosen, and scratch of twist_cache_attention_floats floats is sized, by it, so a captured call serves all shorter lengths.
- *                            scratch need not be cleared; it may be NULL where 0 floats are asked for.  fp32 scores, softmax and sums.
+ *                            scratch need not be cleared; it may be NULL where 0 floats are asked for; calls that may run at the same time need one
+ *                            each.  fp32 scores, softmax and sums.
  * TWIST_ESHAPE if d_head exceeds 256, strides overlap, page_tokens is none of the above or a buffer is too small. */
 TWIST_API twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages *pages, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld,
                                               int32_t T, int32_t Hs, const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq);
@@ -417,7 +419,7 @@ typedef struct {
   int32_t hist_cap;
   const int32_t *n_history; /* dev [T]: ids in row t (NULL: hist_cap), capped to hist_cap */
   const int32_t *n_prompt;  /* dev [T]: how many of them, from the start, are the prompt's (NULL: none) */
-  const float *repetition;  /* dev [T], > 0: a token that is in the history has its logit divided by it if positive, multiplied otherwise */
+  const float *repetition;  /* dev [T], 2^-126 to 2^126: a token that is in the history has its logit divided by it if positive, multiplied otherwise */
   const float *frequency;   /* dev [T]: times the number of times that the token was generated is taken off */
   const float *presence;    /* dev [T]: taken off if the token was generated at all */
   const int32_t *bias_ids;  /* dev [T] rows of bias_cap token ids, ld_bias apart, and what is added to their logits; an id named twice takes its last */
