@@ -203,12 +203,12 @@ class Context:
         if status:
             _check(status, self.h)
 
-    def _empty(self, shape, dtype, result=True):
+    def _empty(self, dtype, *shape, result=True):
         """Memory that the context's stream may write at once, whatever the current stream is; `result`: and that the current one may read until it is dropped."""
         if torch._C._cuda_getCurrentRawStream(self.gpu) == self.raw_stream:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+            return torch.empty(*shape, dtype=dtype, device=self.device)
         with torch.cuda.stream(self.stream):
-            t = torch.empty(shape, dtype=dtype, device=self.device)
+            t = torch.empty(*shape, dtype=dtype, device=self.device)
         if result:
             t.record_stream(torch.cuda.current_stream(self.device))
         return t
@@ -299,7 +299,7 @@ class Context:
         and values go to the cache (storage of twist_cache_bytes).  See include/twist.h."""
         T, V = tokens.shape[0], self.desc.vocab
         if logits is None:      # rows that start at multiples of 16 bytes
-            logits = self._empty((T, (V + 7) // 8 * 8), self.torch_dtype)[:, :V]
+            logits = self._empty(self.torch_dtype, T, (V + 7) // 8 * 8)[:, :V]
         ldl = self._rows(logits, T, V, "logits", self.torch_dtype)
         if pages.gpu != self.gpu or cache.get_device() != self.gpu or workspace.get_device() != self.gpu:
             _refuse(f"table, cache and workspace: need to be on {self.device}")
@@ -502,11 +502,11 @@ class Context:
         T, HD = q.shape[0], cache.Hs * cache.d_head
         ldq = self._rows(q, T, HD, "q", self.torch_dtype)
         if out is None:
-            out, ldo = self._empty((T, HD), self.torch_dtype), HD
+            out, ldo = self._empty(self.torch_dtype, T, HD), HD
         else:
             ldo = self._rows(out, T, HD, "out", self.torch_dtype)
         if lse is None:
-            lse = self._empty((T, cache.Hs), torch.float32)
+            lse = self._empty(torch.float32, T, cache.Hs)
         elif self._rows(lse, T, cache.Hs, "lse", torch.float32) != cache.Hs:
             _refuse("lse: needs rows without padding")
         n = cache.floats.get((T, max_len))
@@ -514,7 +514,7 @@ class Context:
             if len(cache.floats) > 999:
                 cache.floats.clear()
             n = cache.floats[T, max_len] = self.twist_cache_attention_floats(cache, T, max_len)
-        scratch = self._empty(n, torch.float32, result=False) if n else None
+        scratch = self._empty(torch.float32, n, result=False) if n else None
         self._call(lib.twist_cache_attention_raw, cache.pages.ref, cache.k_addr, cache.v_addr, cache.page_stride, q.data_ptr(), ldq, T, cache.Hs,
                    _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len, out.data_ptr(), ldo, lse.data_ptr(), _addr(scratch), n)
         return out, lse
@@ -526,7 +526,7 @@ class Context:
         if not (rules.T in (None, T) and rules.gpu in (None, self.gpu) and (rules.words is None or rules.words * 32 >= V)):
             _refuse(f"rules: need {T} rows on {self.device}, and a mask of {(V + 31) // 32} words a row")
         if out is None:
-            out, ldo = self._empty((T, V), torch.float32), V
+            out, ldo = self._empty(torch.float32, T, V), V
         else:
             ldo = self._rows(out, T, V, "out", torch.float32)
         self._call(lib.twist_logits_raw, logits.data_ptr(), ld, T, rules.ref, out.data_ptr(), ldo)
