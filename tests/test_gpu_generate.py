@@ -1,4 +1,4 @@
-"""Generating tokens with a deployed subnet: twist_subnet_decode against the checker's forward pass, and the steps of generation as they are used
+"""Generating tokens with a deployed subnet: twist_subnet_decode against the oracle's forward pass, and the steps of generation as they are used
 together (prompts, single tokens, rules on logits, pages handed out on the way, captured steps).
 
 Bounds of the logits (relative Frobenius error over all of them): fp32 1e-4, the repository's bound of an fp32 path.  bf16: a logit has 9 rounding points of
@@ -74,7 +74,7 @@ class Deployed:
         return self.ctx.twist_subnet_decode(self.sub, tokens, lens, max_len, self.pages, self.cache, self.ws[key], seq=seq, logits=logits)
 
     def want(self, ids):
-        """The checker's logits [N, vocab] of one sequence of ids."""
+        """The oracle's logits [N, vocab] of one sequence of ids."""
         kept = []
 
         def hook(tag, a):
@@ -87,7 +87,7 @@ class Deployed:
 
 
 @pytest.mark.parametrize("name", list(MODELS))
-def test_prompt_then_single_tokens_give_the_checkers_logits(lib, name):
+def test_prompt_then_single_tokens_give_the_oracles_logits(lib, name):
     """Sequences of different lengths: prompts together in one call, then a token each, then a few drafted ones each."""
     cfg = MODELS[name][0]
     top = min(cfg.max_seq, 70)
@@ -174,7 +174,7 @@ def test_what_a_workspace_held_changes_nothing(lib, name, listed):
 @pytest.mark.parametrize("name", ["llama_f32_um", "gpt_bf16", "llama_bf16_um"])
 def test_generation_as_it_is_used(lib, name):
     """Prompts of their own lengths, then 20 captured steps of three sequences: decode, rules on the logits, choice, bookkeeping on the device, with pages
-    handed to the sequences as they grow.  What the steps computed is checked against the checker on the finished sequences."""
+    handed to the sequences as they grow.  What the steps computed is checked against the oracle on the finished sequences."""
     cfg = MODELS[name][0]
     V, S, top, page, steps = cfg.vocab, 3, 64, 8, 20
     start = [4, 30, 15]
