@@ -392,10 +392,11 @@ TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32
  * by the caller, "dtype" means desc.dtype, d_head and rotary positions come from the ctx's model description.
  *
  * twist_cache_append_raw     T new tokens, rows of qkv [T, 3*Hs*d_head] (q | k | v, dtype, rows ld elements apart): row t is token lens[t] - 1 of sequence
- *                            seq[t] (t itself with seq NULL).  Its v, and its k turned by the rotary embedding of that position (desc.use_rope; angles in
- *                            fp64, one rounding), go to their place in the pools; its q, turned likewise, to row t of q_out (rows ldq apart; q_out may be
+ *                            seq[t] (t itself with seq NULL).  Its v, and its k turned by the rotary embedding of that position (desc.use_rope; angles brought
+ *                            below a turn in fp64), go to their place in the pools; its q, turned likewise, to row t of q_out (rows ldq apart; q_out may be
  *                            the q part of qkv itself, or NULL: queries are not asked for).  Rows with lens[t] < 1 or a seq[t] outside [0, n_seqs) are
- *                            unused ones of the batch: nothing is written for them.  Where two rows name the same token, it holds values of either.
+ *                            unused ones of the batch: nothing is written for them.  Where two rows name the same place, by one token or by pages that
+ *                            several sequences share, each value there is one of theirs.
  * twist_cache_attention_raw  for row t of q [T, Hs*d_head] (dtype, rows ldq apart) and every head, with the scale 1/sqrt(d_head): softmax attention over
  *                            tokens 0 .. lens[t] - 1 of sequence seq[t] (t itself with seq NULL), those on pages that it has; several rows may share a
  *                            sequence.  o [T, Hs*d_head] (dtype, rows ldo apart), lse [T, Hs] fp32 (log-sum-exp of the scaled scores; may be NULL).  A row that
@@ -403,7 +404,8 @@ TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32
  *                            in the pools beyond lens[t] is never used.  max_len (host): no row sees more than its first max_len tokens; kernels are
  *                            chosen, and scratch of twist_cache_attention_floats floats is sized, by it, so a captured call serves all shorter lengths.
  *                            scratch need not be cleared; it may be NULL where 0 floats are asked for; calls that may run at the same time need one
- *                            each.  fp32 scores, softmax and sums.
+ *                            each.  Scores, softmax and sums in fp32 (bf16, rows that share a sequence: the weights that values are multiplied by to
+ *                            2^-16).  Sequences may share pages.
  * TWIST_ESHAPE if d_head exceeds 256, strides overlap, page_tokens is none of the above or a buffer is too small. */
 TWIST_API twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages *pages, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld,
                                               int32_t T, int32_t Hs, const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq);

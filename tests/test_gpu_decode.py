@@ -439,6 +439,32 @@ def test_attention_without_pages(lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+def test_pages_that_sequences_share(lib, dtype):
+    """A common beginning of three sequences, read by all; one place written by two rows holds, value by value, one of theirs."""
+    Hs, dh, page = 3, 64, 16
+    ctx, g = _ctx(lib, dtype, dh), _gen(12)
+    k, v = _pools(g, 8, Hs, page, dh, dtype)
+    table = torch.tensor([[5, 2, 7, 0], [5, 2, 1, -1], [5, 5, 5, 3]], dtype=torch.int32, device="cuda")
+    cache = lib.PagedCache(k, v, table)
+    qkv, lens = _randn(g, 3, 3 * Hs * dh, dtype=dtype), _i32(50, 40, 64)
+    ctx.twist_cache_append_raw(cache, qkv, lens)
+    for seq in (None, _i32(2, 0, 0)):
+        o, lse = ctx.twist_cache_attention_raw(cache, qkv[:, : Hs * dh], lens, 64, seq=seq)
+        torch.cuda.synchronize()
+        wo, wl, eo, el = _attention_want(k, v, table, qkv[:, : Hs * dh], lens, seq, 64, Hs, dh)
+        _close(o, wo, eo, U[dtype])
+        assert ((lse.double().cpu() - wl).abs() <= el).all()
+    before = k.clone(), v.clone()
+    ctx.twist_cache_append_raw(cache, qkv, _i32(4, 4, 36))              # places 3 of page 5, three times
+    torch.cuda.synchronize()
+    for i, (pool, old) in enumerate(zip((k, v), before), 1):
+        theirs = qkv[:, i * Hs * dh : (i + 1) * Hs * dh].view(3, Hs, dh)
+        assert (pool[5, :, 3] == theirs).any(0).all()
+        old[5, :, 3] = pool[5, :, 3]
+        assert torch.equal(pool, old)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("dh,n", [(64, 50), (64, 2000), (20, 50)])
 def test_attention_of_extreme_scores(lib, dtype, dh, n):
     """One key far above the others, far below them, scores of -infinity beside finite ones; an infinite or undefined one gives no number."""
