@@ -351,10 +351,10 @@ typedef short s16x4v __attribute__((ext_vector_type(4)));
 typedef short s16x8v __attribute__((ext_vector_type(8)));
 typedef float f32x4v __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2v __attribute__((ext_vector_type(2)));
-constexpr int kTile = 16;  // rows of a group
+constexpr int kTile = 16;  // rows of a tile
 
-// Rows of the batch that follow each other and share a sequence (prompts, drafted tokens), up to kTile of them from a multiple of kTile on, read its keys
-// once: their scores are the 16 columns of v_mfma_f32_16x16x32_bf16.  S^T = K Q^T for two tiles of 16 tokens, the keys' fragments straight from memory: lane
+// Rows of the batch that follow each other and share a sequence (prompts, drafted tokens), up to RC tiles of kTile of them from a multiple of that on, read its
+// keys once: a tile's scores are the 16 columns of v_mfma_f32_16x16x32_bf16.  S^T = K Q^T for two tiles of 16 tokens, the keys' fragments straight from memory: lane
 // (j = lane / 16, c = lane % 16) holds 16 bytes of token c and gets the scores of tokens 4 j .. 4 j + 3 of either tile for row c.  These eight
 // are the eight contraction indices that the lane has in O^T += V^T P^T, so the weights stay where they are; the values pass through LDS (a tile
 // of the wave's own, no barrier) and come back transposed in the same order of tokens.  Weights go in as two bf16 terms, cut off and rounded: at most 2^-16 of
@@ -362,7 +362,7 @@ constexpr int kTile = 16;  // rows of a group
 // fp32: v_mfma_f32_16x16x4_f32, of which an instruction takes one of the four numbers in a lane's 16 bytes of a key; four tokens of values are 4 x 256
 // bytes as they lie, lane (j, c) with elements 4 c .. 4 c + 3 of token 4 j + e: number i of them belongs to an accumulator of elements 4 k + i, so that
 // nothing passes through LDS.  Loads and products of a wave take turns: 45 to 60 % of the read rate, where one row a sequence reaches 75 to 93.
-template <int BF, int KS, int NW>
+template <int BF, int KS, int NW, int RC>
 __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(AttentionArgs A) {
   constexpr int ES = BF ? 2 : 4, N = 16 / ES, VB = (KS + 3) / 4, MT = BF ? 2 * KS : 4 * VB;
   constexpr int RB = 64 * KS + 32, LDR = 16 * MT + 4;  // bytes of a row of values in LDS, floats of one of results (the padding spreads the banks)
@@ -373,27 +373,34 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
   __shared__ float s_m[NW][kTile], s_l[NW][kTile];
   __shared__ int s_seen[NW][kTile];
   const int units = A.places / A.turns, unit = blockIdx.x % units, turn = blockIdx.x / units, part = blockIdx.y;
-  const int h = unit % A.Hs, t0 = unit / A.Hs * kTile, dh = A.dh;
+  const int h = unit % A.Hs, t0 = (RC > 1 ? units / A.Hs - 1 - unit / A.Hs : unit / A.Hs) * (RC * kTile), dh = A.dh;  // (a prompt's last rows, the longest, first)
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane >> 4, c = lane & 15;
-  // the first rows of the groups among rows t0 .. t0 + 15, of which every A.turns-th is this workgroup's
-  const int own = t0 + c < A.T ? A.seq[t0 + c] : -1, prev = __shfl_up(own, 1, 64);
-  uint32_t starts = (uint32_t)__ballot(t0 + c < A.T && (c == 0 || own != prev)) & 0xffffu;
+  // the first rows of the groups among rows t0 .. t0 + 16 RC - 1, of which every A.turns-th is this workgroup's
+  const bool mine = lane < RC * kTile && t0 + lane < A.T;
+  const int own = mine ? A.seq[t0 + lane] : -1, prev = __shfl_up(own, 1, 64);
+  uint32_t starts = (uint32_t)__ballot(mine && (lane == 0 || own != prev));
   for (int n = 0; starts; ++n) {
     const int r0 = __builtin_ctz(starts), t = t0 + r0;
     starts &= starts - 1;
     if (n % A.turns != turn) continue;
-    const int rows = (starts ? __builtin_ctz(starts) : min(kTile, A.T - t0)) - r0;
+    const int rows = (starts ? __builtin_ctz(starts) : min(RC * kTile, A.T - t0)) - r0;
     const int s = __builtin_amdgcn_readfirstlane(__shfl(own, r0, 64));
     if ((unsigned)s >= (unsigned)A.pg.n_seqs) continue;
-    const int given = c < rows ? A.lens[t + c] : -1, len = min(given, A.max_len);
-    int longest = len, shortest = c < rows ? len : INT32_MAX;
+    int len[RC], top_len[RC], longest = -1, shortest = INT32_MAX;  // of the lane's row of each tile, of the tile
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) {
-      longest = max(longest, __shfl_xor(longest, o, 64));
-      shortest = min(shortest, __shfl_xor(shortest, o, 64));
+    for (int b = 0; b < RC; ++b) {
+      const bool in = b * kTile + c < rows;
+      len[b] = in ? min(A.lens[t + b * kTile + c], A.max_len) : -1;
+      int hi = len[b], lo = in ? len[b] : INT32_MAX;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1) {
+        hi = max(hi, __shfl_xor(hi, o, 64));
+        lo = min(lo, __shfl_xor(lo, o, 64));
+      }
+      top_len[b] = __builtin_amdgcn_readfirstlane(hi);
+      longest = max(longest, top_len[b]);
+      shortest = min(shortest, __builtin_amdgcn_readfirstlane(lo));
     }
-    longest = __builtin_amdgcn_readfirstlane(longest);
-    shortest = __builtin_amdgcn_readfirstlane(shortest);
     const int p0 = part * A.chunk, p1 = min(p0 + A.chunk, longest);
     if (longest < 0 || (part && p0 >= longest)) continue;
     const int shift = A.pg.shift, first = p0 >> shift, n_ids = p1 > p0 ? ((p1 - 1) >> shift) - first + 1 : 0;
@@ -402,15 +409,21 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
       ids[i] = (unsigned)page < (unsigned)A.pg.n_pages ? page * A.page_stride + (((int64_t)h << shift)) * dh : -1;
     }
     const u32x4v none = {0u, 0u, 0u, 0u};
-    const char *q = static_cast<const char *>(A.q) + ((t + min(c, rows - 1)) * A.ldq + (int64_t)h * dh) * ES;
-    u32x4v qf[KS];
+    u32x4v qf[RC][KS];
+    f32x4v acc[RC][MT];
+    float m[RC], l[RC];  // of the lane's row: the maximum of all scores, the sum of this lane's weights
+    bool seen[RC];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) qf[k] = (4 * k + j) * N < dh ? *reinterpret_cast<const u32x4v *>(q + 64 * k + 16 * j) : none;
-    f32x4v acc[MT];
+    for (int b = 0; b < RC; ++b) {
+      const char *q = static_cast<const char *>(A.q) + ((t + min(b * kTile + c, rows - 1)) * A.ldq + (int64_t)h * dh) * ES;
 #pragma unroll
-    for (int m = 0; m < MT; ++m) acc[m] = f32x4v{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f;  // of row c: the maximum of all scores, the sum of this lane's weights
-    bool seen = false;
+      for (int k = 0; k < KS; ++k) qf[b][k] = (4 * k + j) * N < dh ? *reinterpret_cast<const u32x4v *>(q + 64 * k + 16 * j) : none;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) acc[b][i] = f32x4v{0.f, 0.f, 0.f, 0.f};
+      m[b] = -INFINITY;
+      l[b] = 0.f;
+      seen[b] = false;
+    }
     char *tile = tiles[wave];
     const int wr = c * RB + 16 * j, rd = (4 * j + (c >> 2)) * RB + (c & 3) * 8;  // where the lane's values go, and what it reads of 4 x 16 of them
     __syncthreads();
@@ -442,61 +455,71 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
             const bool ok = tok < p1 && base >= 0;
             const char *vp = static_cast<const char *>(A.v) + (ok ? base + (int64_t)(tok & ((1 << shift) - 1)) * dh : 0) * 4 + 16 * c;
 #pragma unroll
-            for (int b = 0; b < VB; ++b) vf[i][4 * b + e] = 64 * b + 4 * c < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 256 * b) : none;
+            for (int k = 0; k < VB; ++k) vf[i][4 * k + e] = 64 * k + 4 * c < dh && ok ? *reinterpret_cast<const u32x4v *>(vp + 256 * k) : none;
           }
       }
       __builtin_amdgcn_sched_barrier(0);  // (all loads before the first product)
-      f32x4v sc[2] = {f32x4v{0.f, 0.f, 0.f, 0.f}, f32x4v{0.f, 0.f, 0.f, 0.f}};
+      float p[RC][8];
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int b = 0; b < RC; ++b) {
+        if (RC > 1 && tok0 >= top_len[b]) {  // (rows of a prompt that end before these tokens)
 #pragma unroll
-        for (int k = 0; k < KS; ++k) {
-          if constexpr (BF) {
-            sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[i][k]), __builtin_bit_cast(bf16x8v, qf[k]), sc[i], 0, 0, 0);
-          } else {
+          for (int e = 0; e < 8; ++e) p[b][e] = 0.f;
+          continue;
+        }
+        f32x4v sc[2] = {f32x4v{0.f, 0.f, 0.f, 0.f}, f32x4v{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][k][e]), __uint_as_float(qf[k][e]), sc[i], 0, 0, 0);
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            if constexpr (BF) {
+              sc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v, kf[i][k]), __builtin_bit_cast(bf16x8v, qf[b][k]), sc[i], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) sc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[i][k][e]), __uint_as_float(qf[b][k][e]), sc[i], 0, 0, 0);
+            }
+          }
+        const bool whole = there == 0xffffffffu && tok0 + 32 <= shortest;
+        uint32_t on = 0xffu;  // which of the lane's eight tokens its row sees
+        if (!whole) {
+          on = 0;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int tok = 16 * (e >> 2) + 4 * j + (e & 3);
+            if ((there >> tok & 1) && tok0 + tok < len[b]) on |= 1u << e;
+            else sc[e >> 2][e & 3] = -INFINITY;
           }
         }
-      const bool whole = there == 0xffffffffu && tok0 + 32 <= shortest;
-      uint32_t on = 0xffu;  // which of the lane's eight tokens its row sees
-      if (!whole) {
-        on = 0;
+        seen[b] |= on != 0;
+        float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
+        mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float mn = fmaxf(m[b], mx), ref = mn == -INFINITY ? 0.f : mn;
+        if (__any(mn > m[b])) {
+          const float alpha = __builtin_amdgcn_exp2f((m[b] - ref) * A.scale);
+          l[b] *= alpha;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[b][i] *= alpha;
+          m[b] = mn;
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int tok = 16 * (e >> 2) + 4 * j + (e & 3);
-          if ((there >> tok & 1) && tok0 + tok < len) on |= 1u << e;
-          else sc[e >> 2][e & 3] = -INFINITY;
+          p[b][e] = __builtin_amdgcn_exp2f((sc[e >> 2][e & 3] - ref) * A.scale);
+          l[b] += p[b][e];
         }
-      }
-      seen |= on != 0;
-      float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      const float mn = fmaxf(m, mx), ref = mn == -INFINITY ? 0.f : mn;
-      if (__any(mn > m)) {
-        const float alpha = __builtin_amdgcn_exp2f((m - ref) * A.scale);
-        l *= alpha;
-#pragma unroll
-        for (int i = 0; i < MT; ++i) acc[i] *= alpha;
-        m = mn;
-      }
-      float p[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f((sc[e >> 2][e & 3] - ref) * A.scale);
-        l += p[e];
       }
       if constexpr (BF) {
-        u32x4v hi, lo;
+        u32x4v hi[RC], lo[RC];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t a = __float_as_uint(p[2 * e]), b = __float_as_uint(p[2 * e + 1]);
-          hi[e] = __builtin_amdgcn_perm(b, a, 0x07060302u);  // the upper halves
-          typedef float f32x2 __attribute__((ext_vector_type(2)));
-          const f32x2 rest = {p[2 * e] - __uint_as_float(a & 0xffff0000u), p[2 * e + 1] - __uint_as_float(b & 0xffff0000u)};
-          lo[e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
-        }
+        for (int b = 0; b < RC; ++b)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t x = __float_as_uint(p[b][2 * e]), y = __float_as_uint(p[b][2 * e + 1]);
+            hi[b][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);  // the upper halves
+            typedef float f32x2 __attribute__((ext_vector_type(2)));
+            const f32x2 rest = {p[b][2 * e] - __uint_as_float(x & 0xffff0000u), p[b][2 * e + 1] - __uint_as_float(y & 0xffff0000u)};
+            lo[b][e] = __builtin_bit_cast(uint32_t, __builtin_convertvector(rest, bf16x2v));
+          }
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
         u16x2 top = {0, 0};  // largest magnitude among the values
 #pragma unroll
@@ -514,26 +537,32 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
             typedef s16x4v __attribute__((address_space(3))) * lds_ptr;
             const s16x4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + rd + 32 * i)), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(tile + 16 * RB + rd + 32 * i));
             const bf16x8v vt = __builtin_bit_cast(bf16x8v, s16x8v{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]});
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, hi), acc[i], 0, 0, 0);
-            acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, lo), acc[i], 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < RC; ++b) {
+              if (RC > 1 && tok0 >= top_len[b]) continue;
+              acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, hi[b]), acc[b][i], 0, 0, 0);
+              acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8v, lo[b]), acc[b][i], 0, 0, 0);
+            }
           }
         } else {  // infinities and NaNs, which times the zero of a term or of a hidden token are no number: one by one, for the rows that see them
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-#pragma unroll 1
-            for (int x = 0; x < 4; ++x) {
-              const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
-              const float w = __shfl(p[e], 16 * x + c, 64);
-              if (!(there >> tok & 1) || tok0 + tok >= len) continue;
+          for (int b = 0; b < RC; ++b)
 #pragma unroll
-              for (int i = 0; i < MT; ++i) {
-                const u32x2v u = *reinterpret_cast<const u32x2v *>(tile + tok * RB + 32 * i + 8 * j);
-                acc[i][0] = fmaf(w, __uint_as_float(u.x << 16), acc[i][0]);
-                acc[i][1] = fmaf(w, __uint_as_float(u.x & 0xffff0000u), acc[i][1]);
-                acc[i][2] = fmaf(w, __uint_as_float(u.y << 16), acc[i][2]);
-                acc[i][3] = fmaf(w, __uint_as_float(u.y & 0xffff0000u), acc[i][3]);
+            for (int e = 0; e < 8; ++e)
+#pragma unroll 1
+              for (int x = 0; x < 4; ++x) {
+                const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
+                const float w = __shfl(p[b][e], 16 * x + c, 64);
+                if (!(there >> tok & 1) || tok0 + tok >= len[b]) continue;
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                  const u32x2v u = *reinterpret_cast<const u32x2v *>(tile + tok * RB + 32 * i + 8 * j);
+                  acc[b][i][0] = fmaf(w, __uint_as_float(u.x << 16), acc[b][i][0]);
+                  acc[b][i][1] = fmaf(w, __uint_as_float(u.x & 0xffff0000u), acc[b][i][1]);
+                  acc[b][i][2] = fmaf(w, __uint_as_float(u.y << 16), acc[b][i][2]);
+                  acc[b][i][3] = fmaf(w, __uint_as_float(u.y & 0xffff0000u), acc[b][i][3]);
+                }
               }
-            }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // the next tokens' values take the place of these
       } else {
@@ -541,72 +570,81 @@ __global__ __launch_bounds__(64 * NW) void cache_attention_tile_kernel(Attention
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-          for (int b = 0; b < 4 * VB; ++b)
+          for (int k = 0; k < 4 * VB; ++k)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) top = max(top, vf[i][b][e] & 0x7fffffffu);
-        if (!__any(top >= 0x7f800000u)) {
+            for (int e = 0; e < 4; ++e) top = max(top, vf[i][k][e] & 0x7fffffffu);
+        const bool finite = !__any(top >= 0x7f800000u);
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+        for (int b = 0; b < RC; ++b) {
+          if (RC > 1 && tok0 >= top_len[b]) continue;
+          if (finite) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-              acc[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[e >> 2][(i & ~3) + (e & 3)][i & 3]), p[e], acc[i], 0, 0, 0);
-        } else {  // as above; the values from memory again
+            for (int e = 0; e < 8; ++e)
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+              for (int i = 0; i < MT; ++i)
+                acc[b][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[e >> 2][(i & ~3) + (e & 3)][i & 3]), p[b][e], acc[b][i], 0, 0, 0);
+          } else {  // as above; the values from memory again
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
 #pragma unroll 1
-            for (int x = 0; x < 4; ++x) {
-              const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
-              const float w = __shfl(p[e], 16 * x + c, 64);
-              if (!(there >> tok & 1) || tok0 + tok >= len) continue;
-              const float *vp = static_cast<const float *>(A.v) + ids[((tok0 + tok) >> shift) - first] + (int64_t)((tok0 + tok) & ((1 << shift) - 1)) * dh;
+              for (int x = 0; x < 4; ++x) {
+                const int tok = 16 * (e >> 2) + 4 * x + (e & 3);
+                const float w = __shfl(p[b][e], 16 * x + c, 64);
+                if (!(there >> tok & 1) || tok0 + tok >= len[b]) continue;
+                const float *vp = static_cast<const float *>(A.v) + ids[((tok0 + tok) >> shift) - first] + (int64_t)((tok0 + tok) & ((1 << shift) - 1)) * dh;
 #pragma unroll
-              for (int b = 0; b < VB; ++b)
+                for (int k = 0; k < VB; ++k)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                  const int el = 64 * b + 16 * j + 4 * r;
-                  if (el < dh) {
-                    const f32x4v u = *reinterpret_cast<const f32x4v *>(vp + el);
+                  for (int r = 0; r < 4; ++r) {
+                    const int el = 64 * k + 16 * j + 4 * r;
+                    if (el < dh) {
+                      const f32x4v u = *reinterpret_cast<const f32x4v *>(vp + el);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[4 * b + i][r] = fmaf(w, u[i], acc[4 * b + i][r]);
+                      for (int i = 0; i < 4; ++i) acc[b][4 * k + i][r] = fmaf(w, u[i], acc[b][4 * k + i][r]);
+                    }
                   }
-                }
-            }
+              }
+          }
         }
       }
     }
-    l += __shfl_xor(l, 16, 64);
-    l += __shfl_xor(l, 32, 64);
-    const uint64_t any = __ballot(seen);
     float *res = reinterpret_cast<float *>(tile);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      if constexpr (BF) {
-        *reinterpret_cast<f32x4v *>(res + c * LDR + 16 * i + 4 * j) = acc[i];
-      } else {  // (elements 4 k + i % 4 of its 64)
-        const int b = i >> 2, r = i & 3;
-        *reinterpret_cast<f32x4v *>(res + c * LDR + 64 * b + 16 * j + 4 * r) = f32x4v{acc[4 * b][r], acc[4 * b + 1][r], acc[4 * b + 2][r], acc[4 * b + 3][r]};
-      }
-    }
-    if (j == 0) { s_m[wave][c] = m; s_l[wave][c] = l; s_seen[wave][c] = (any >> c | any >> (c + 16) | any >> (c + 32) | any >> (c + 48)) & 1; }
-    __syncthreads();
-    for (int i = tid; i < rows * dh; i += 64 * NW) {
-      const int r = i / dh, e = i - r * dh, row_len = A.lens[t + r];
-      if (row_len < 0 || (part && p0 >= min(row_len, A.max_len))) continue;
-      float M = s_m[0][r];
-      bool some = s_seen[0][r];
+    for (int b = 0; b < RC; ++b) {
+      if (RC > 1 && b * kTile >= rows) break;
+      l[b] += __shfl_xor(l[b], 16, 64);
+      l[b] += __shfl_xor(l[b], 32, 64);
+      const uint64_t any = __ballot(seen[b]);
 #pragma unroll
-      for (int w = 1; w < NW; ++w) { M = fmaxf(M, s_m[w][r]); some |= s_seen[w][r]; }
-      const float ref = M == -INFINITY ? 0.f : M;
-      float L = 0.f, a = 0.f;
-#pragma unroll
-      for (int w = 0; w < NW; ++w) {
-        const float x = __builtin_amdgcn_exp2f((s_m[w][r] - ref) * A.scale);
-        L += x * s_l[w][r];
-        a += x * reinterpret_cast<const float *>(tiles[w])[r * LDR + e];
+      for (int i = 0; i < MT; ++i) {
+        if constexpr (BF) {
+          *reinterpret_cast<f32x4v *>(res + c * LDR + 16 * i + 4 * j) = acc[b][i];
+        } else {  // (elements 4 k + i % 4 of its 64)
+          const int k = i >> 2, r = i & 3;
+          *reinterpret_cast<f32x4v *>(res + c * LDR + 64 * k + 16 * j + 4 * r) = f32x4v{acc[b][4 * k][r], acc[b][4 * k + 1][r], acc[b][4 * k + 2][r], acc[b][4 * k + 3][r]};
+        }
       }
-      leave<BF>(A, (int64_t)(t + r) * A.Hs + h, part, t + r, h, e, a, M * A.scale, L, some);
+      if (j == 0) { s_m[wave][c] = m[b]; s_l[wave][c] = l[b]; s_seen[wave][c] = (any >> c | any >> (c + 16) | any >> (c + 32) | any >> (c + 48)) & 1; }
+      __syncthreads();
+      for (int i = tid; i < min(rows - b * kTile, kTile) * dh; i += 64 * NW) {
+        const int r = i / dh, e = i - r * dh, row = t + b * kTile + r, row_len = A.lens[row];
+        if (row_len < 0 || (part && p0 >= min(row_len, A.max_len))) continue;
+        float M = s_m[0][r];
+        bool some = s_seen[0][r];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) { M = fmaxf(M, s_m[w][r]); some |= s_seen[w][r]; }
+        const float ref = M == -INFINITY ? 0.f : M;
+        float L = 0.f, a = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+          const float x = __builtin_amdgcn_exp2f((s_m[w][r] - ref) * A.scale);
+          L += x * s_l[w][r];
+          a += x * reinterpret_cast<const float *>(tiles[w])[r * LDR + e];
+        }
+        leave<BF>(A, (int64_t)row * A.Hs + h, part, row, h, e, a, M * A.scale, L, some);
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -669,10 +707,13 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 //  - Tiles (turns > 0; a workgroup takes every turns-th group among 16 rows): where sequences have several rows each on average, the more the shorter they may be
 //    (rows beyond 16 a sequence fill no more of a tile), and enough of both to fill the chip.  bf16, (heads x sequences) x tokens, r rows each, rows / tiles: (16 x 16) x 64, 16 rows 12.5 / 7.1,
 //    (16 x 64) x 64, 8 rows 23.8 / 27.1, x 250 47 / 37.7, (12 x 32) of 64 x 100, 5 rows 8.8 / 10.9, x 300 15.8 / 15.6, (19 x 19) x 926, 8 rows 83 / 34.8, a prompt of 1000,
-//    8 heads 173 / 36; few rows: (8 x 6) x 1172, 2 rows 12.6 / 17.3, (15 x 4) x 343, 8 rows 9.6 / 11.8, (30 x 2) of 64 x 1299, 8 rows 14.7 / 15.6.
+//    8 heads 173 / 31; few rows: (8 x 6) x 1172, 2 rows 12.6 / 17.3, (15 x 4) x 343, 8 rows 9.6 / 11.8, (30 x 2) of 64 x 1299, 8 rows 14.7 / 15.6.
 //    fp32, whose matrix instruction has a sixteenth of the rate: (12 x 32) of 64 x 400, 5 rows 19.3 / 26, (16 x 16) of 64 x 128, 16 rows 13.5 / 9.6,
 //    (29 x 24) of 96 x 1512, 8 rows 547 / 138, (12 x 8) of 64 x 1003, 4 rows 14.3 / 19, (16 x 4) x 4170, 3 rows 64 / 54, (12 x 40) of 64 x 2133, 2 rows 77 / 89; a prompt
-//    of 2000, 16 heads 1089 / 342.
+//    of 2000, 16 heads 1089 / 308.
+//    Two tiles in the registers of a workgroup, for heads that leave room for them (33 to 128), where sequences have 32 rows on average and many tokens.  One / two:
+//    a prompt of 4096, 32 heads 1106 / 653, of 2000, 16 heads 169 / 116, of 1024, 8 heads 33.1 / 30.9, of 512 17.6 / 23.2, 200 rows behind 7800, 8 heads 77.6 / 50.4, 4
+//    prompts of 300 28.9 / 32.2; fp32, 12 heads of 64, 2 of 1000 90.7 / 77.1, 1 of 500 20.9 / 23.5; heads of 32, 16 x 2 of 1000 30.1 / 35.3, of 256, 4 x 2 67.6 / 74.9.
 //  - Up to 384 KB of keys and values a head are read by one workgroup; where heads and rows are at most half the CUs, longer sequences are cut so that there are
 //    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
 //    8 x 4096 22 / 10.5 / 11, 32 x 2048 17 / 12.6 / 12.5, 32 x 8192 - / 30.5 / 32.5, 16 x 32768 - / 53.4 / 55.2;
@@ -681,13 +722,16 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 //    196 / 189, (32 x 16) x 16384 511 / 478, (8 x 32) x 6000 107 / 108.5; on the other side (8 x 32) x 4096 74.7 / 79.3, (12 x 16) x 4096 60.6 / 65.7, (16 x 128) x 2048 238 / 246.
 //  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
 //    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.
-struct Split { int waves, parts, chunk, turns, run, places; };
+struct Split { int waves, parts, chunk, tiles, turns, run, places; };
 Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int dh, int es, bool listed, bool tiles) {
   Split s;
-  const int64_t blocks = (T + kTile - 1) / kTile, row_bytes = dh * es, pair = 2 * row_bytes;
+  const int64_t row_bytes = dh * es, pair = 2 * row_bytes;
   tiles = tiles && T >= (es == 2 ? 2 : 3) * (int64_t)n_seqs && std::min<int64_t>(16 * (int64_t)n_seqs, T) * max_len >= (es == 2 ? 1024 : 2048) * (int64_t)n_seqs &&
           (T * Hs >= 2048 || (int64_t)T * Hs * dh >= ((1 << 25) + max_len - 1) / max_len);
-  s.turns = tiles ? std::min({8, T, (int)(((int64_t)kTile * n_seqs + T - 1) / T)}) : 0;
+  s.tiles = tiles ? T >= 32 * (int64_t)n_seqs && max_len >= 768 && dh > 32 && dh <= 128 ? 2 : 1 : 0;
+  const int rows = kTile * std::max(1, s.tiles);
+  const int64_t blocks = (T + rows - 1) / rows;
+  s.turns = tiles ? std::min({8, T, (int)(((int64_t)rows * n_seqs + T - 1) / T)}) : 0;
   s.run = listed && T >= 2 * (int64_t)n_seqs && Hs % 8 ? std::min(T, 8) : 1;
   s.places = (int)(tiles ? blocks * s.turns * Hs : s.run > 1 ? ((int64_t)(T + s.run - 1) / s.run * Hs + 7) / 8 * 8 * s.run : (int64_t)T * Hs);
   const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
@@ -760,33 +804,40 @@ void launch_attention_of(hipStream_t st, const AttentionArgs &a, int waves) {
 }
 
 template <int BF, int KS>
-void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a) {
-  constexpr int NW = KS > (BF ? 4 : 8) ? 4 : 8;
-  hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW>), dim3((unsigned)a.places, (unsigned)a.parts), dim3(64 * NW), 0, st, a);
+void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a, int tiles) {
+  constexpr int NW = KS > (BF ? 4 : 8) ? 4 : 8, NW2 = KS > 4 ? 4 : 8;  // (what their registers allow)
+  const dim3 grid((unsigned)a.places, (unsigned)a.parts);
+  if constexpr (BF ? KS > 1 && KS <= 4 : KS > 2 && KS <= 8) {
+    if (tiles == 2) {
+      hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW2, 2>), grid, dim3(64 * NW2), 0, st, a);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW, 1>), grid, dim3(64 * NW), 0, st, a);
 }
-void launch_attention_tile(int bf16, hipStream_t st, const AttentionArgs &a) {
+void launch_attention_tile(int bf16, hipStream_t st, const AttentionArgs &a, int tiles) {
   const int pieces = (a.dh * (bf16 ? 2 : 4) + 63) / 64;  // of 64 bytes
   if (bf16) {
     switch (pieces) {
-      case 1: launch_attention_tile_of<1, 1>(st, a); break;
-      case 2: launch_attention_tile_of<1, 2>(st, a); break;
-      case 3: launch_attention_tile_of<1, 3>(st, a); break;
-      case 4: launch_attention_tile_of<1, 4>(st, a); break;
-      case 5: launch_attention_tile_of<1, 5>(st, a); break;
-      case 6: launch_attention_tile_of<1, 6>(st, a); break;
-      case 7: launch_attention_tile_of<1, 7>(st, a); break;
-      default: launch_attention_tile_of<1, 8>(st, a); break;
+      case 1: launch_attention_tile_of<1, 1>(st, a, tiles); break;
+      case 2: launch_attention_tile_of<1, 2>(st, a, tiles); break;
+      case 3: launch_attention_tile_of<1, 3>(st, a, tiles); break;
+      case 4: launch_attention_tile_of<1, 4>(st, a, tiles); break;
+      case 5: launch_attention_tile_of<1, 5>(st, a, tiles); break;
+      case 6: launch_attention_tile_of<1, 6>(st, a, tiles); break;
+      case 7: launch_attention_tile_of<1, 7>(st, a, tiles); break;
+      default: launch_attention_tile_of<1, 8>(st, a, tiles); break;
     }
   } else if (pieces <= 2) {
-    launch_attention_tile_of<0, 2>(st, a);
+    launch_attention_tile_of<0, 2>(st, a, tiles);
   } else if (pieces <= 4) {
-    launch_attention_tile_of<0, 4>(st, a);
+    launch_attention_tile_of<0, 4>(st, a, tiles);
   } else if (pieces <= 8) {
-    launch_attention_tile_of<0, 8>(st, a);
+    launch_attention_tile_of<0, 8>(st, a, tiles);
   } else if (pieces <= 12) {
-    launch_attention_tile_of<0, 12>(st, a);
+    launch_attention_tile_of<0, 12>(st, a, tiles);
   } else {
-    launch_attention_tile_of<0, 16>(st, a);
+    launch_attention_tile_of<0, 16>(st, a, tiles);
   }
   if (a.parts > 1) launch_attention_join(bf16, st, a);
 }
@@ -877,7 +928,7 @@ extern "C" twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pa
   a.acc_parts = need ? scratch + (size_t)T * Hs * a.parts * 2 : nullptr;
   a.scale = 1.44269504089f / sqrtf((float)dh);
   if (split.turns) {
-    launch_attention_tile(ctx->d.dtype == TWIST_BF16, ctx->stream, a);
+    launch_attention_tile(ctx->d.dtype == TWIST_BF16, ctx->stream, a, split.tiles);
     TW_HIP(ctx, hipGetLastError());
     return TWIST_OK;
   }

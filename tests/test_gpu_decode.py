@@ -365,6 +365,16 @@ def test_attention_in_tiles_of_rows(lib, dtype, Hs, dh, page):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("Hs,dh,page", [(2, 128, 16), (3, 64, 16), (1, 40, 32), (2, 80, 1), (1, 96, 64), (2, 120, 16), (1, 36, 8), (4, 72, 512)])
+def test_attention_in_pairs_of_tiles(lib, dtype, Hs, dh, page):
+    """Prompts: more than 32 rows a sequence and room for 768 tokens; runs that start and end anywhere, rows that end long before others of their tiles."""
+    check = lambda lens, seq, n_seqs, **kw: _check_attention(lib, dtype, Hs, dh, page, *_tiled(lens, seq, Hs, dh, 800), n_seqs=n_seqs, max_len=800, max_pages=-(-800 // page), **kw)  # noqa: E731
+    check(list(range(1, 71)) + [790, 5, 0, -1, 300], [0] * 75, 1)
+    check(list(range(60, 0, -1)) + list(range(500, 520)) + [800], [1] * 60 + [0] * 21, 2)
+    check([30, 31] + [700] * 17 + list(range(300, 340)), [0] * 2 + [2] * 17 + [1] * 40, 3, holes=[(2, 0), (1, 300 // page), (0, 0)])
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("Hs,dh,top", [(1, 128, 5000), (2, 64, 4503), (1, 40, 9000), (1, 256, 3001)])
 def test_attention_in_tiles_over_long_sequences(lib, dtype, Hs, dh, top):
     """Sequences cut into parts, the last of which only some rows of a tile reach, missing pages among them."""
@@ -375,20 +385,21 @@ def test_attention_in_tiles_over_long_sequences(lib, dtype, Hs, dh, top):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
-def test_attention_in_tiles_of_values_that_are_no_numbers(lib, dtype):
+@pytest.mark.parametrize("room", [320, 800])
+def test_attention_in_tiles_of_values_that_are_no_numbers(lib, dtype, room):
     """An infinity reaches the rows that see it and no others, also where their scores leave nothing of a term of its weight."""
     ctx, g, dh = _ctx(lib, dtype, 64), _gen(8), 64
-    k, v = _pools(g, 20, 1, 16, dh, dtype)
-    table = torch.arange(20, dtype=torch.int32, device="cuda").view(1, -1)
+    k, v = _pools(g, room // 16, 1, 16, dh, dtype)
+    table = torch.arange(room // 16, dtype=torch.int32, device="cuda").view(1, -1)
     cache = lib.PagedCache(k, v, table)
-    lens, seq = _tiled([40, 41, 100, 320], [0, 0, 0, 0], 1, dh, 320)
+    lens, seq = _tiled([40, 41, 100, 320], [0, 0, 0, 0], 1, dh, room)
     q = torch.zeros((len(lens), dh), dtype=_dt(dtype), device="cuda")
     lens, seq = _i32(*lens), _i32(*seq)
-    base = ctx.twist_cache_attention_raw(cache, q, lens, 320, seq=seq)[0][:4].clone()
+    base = ctx.twist_cache_attention_raw(cache, q, lens, room, seq=seq)[0][:4].clone()
     v[2, 0, 8, 5] = INF                                    # token 40: the last of row 1, none of row 0
     v[6, 0, 2, 7] = -INF                                   # token 98
     v[16, 0, 5, 9] = NAN                                   # token 261: row 3 only
-    o = ctx.twist_cache_attention_raw(cache, q, lens, 320, seq=seq)[0][:4]
+    o = ctx.twist_cache_attention_raw(cache, q, lens, room, seq=seq)[0][:4]
     torch.cuda.synchronize()
     assert torch.equal(o[0], base[0])
     assert (o[1:, 5] == INF).all() and torch.isfinite(o[1, 7]) and (o[2:, 7] == -INF).all()
