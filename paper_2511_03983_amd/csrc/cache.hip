@@ -718,10 +718,13 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 //    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
 //    8 x 4096 22 / 10.5 / 11, 32 x 2048 17 / 12.6 / 12.5, 32 x 8192 - / 30.5 / 32.5, 16 x 32768 - / 53.4 / 55.2;
 //    beyond that half, 12 heads of 64 x 16 in fp32 x 2000 32 / 35 / -.  Tiles, whose waves take 32 tokens at a time: 256 KB (16 heads x 4096, 8 rows: parts of 256 / 512 / 1024 22.9 / 18.5 / 25).
-//  - From 2.5 MB on parts of 1 MB even out rows of different lengths: uncut / cut (8 x 20) x 6000 82.5 / 76.5, x 8000 107 / 90, (12 x 16) x 6000 89.7 / 82.4, (16 x 32) x 6000
+//  - From 2.5 MB on (tiles: 2 MB, (3 x 36) of 64 x 9059, 5 rows 68.9 / 53.4) parts of 1 MB even out rows of different lengths: uncut / cut (8 x 20) x 6000 82.5 / 76.5, x 8000 107 / 90, (12 x 16) x 6000 89.7 / 82.4, (16 x 32) x 6000
 //    196 / 189, (32 x 16) x 16384 511 / 478, (8 x 32) x 6000 107 / 108.5; on the other side (8 x 32) x 4096 74.7 / 79.3, (12 x 16) x 4096 60.6 / 65.7, (16 x 128) x 2048 238 / 246.
 //  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
-//    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.
+//    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.  Tiles have 8
+//    waves (what registers allow), or 4 where parts are short and workgroups more than CUs, 8 / 4: (16 x 64) x 250, 8 rows 37.5 / 29.2, (19 x 19) x 926, 8 rows 35.5 / 32.7,
+//    (21 x 18) x 933, 2 rows 37.8 / 33.6, (16 x 8) of 64, prompts of 100 21.3 / 13.1; (16 x 8) x 1000, 16 rows 21.3 / 24.9, (30 x 10) x 1800, 8 rows 50 / 55.5; fp32 (16 x 64) x
+//    300, 8 rows 70.5 / 78.9.
 struct Split { int waves, parts, chunk, tiles, turns, run, places; };
 Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int dh, int es, bool listed, bool tiles) {
   Split s;
@@ -737,10 +740,11 @@ Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int dh, in
   const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
   int64_t c = max_len;
   if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
-  if (max_len * pair >= 2560 << 10) c = std::min<int64_t>(c, (1 << 20) / pair);
+  if (max_len * pair >= (s.turns ? 2048 : 2560) << 10) c = std::min<int64_t>(c, (1 << 20) / pair);
   c = std::max<int64_t>(c, (max_len + kMaxParts - 1) / kMaxParts);
   c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)(kMaxIds - 1) << shift);  // (one page more where it begins inside one)
-  s.waves = c * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
+  if (tiles) s.waves = es == 2 && units > 256 && c * row_bytes <= 256 << 10 ? 4 : 8;
+  else s.waves = c * row_bytes > (units <= 256 ? 32 << 10 : 128 << 10) ? 16 : 4;
   s.chunk = (int)c;
   s.parts = (int)((max_len + c - 1) / c);
   return s;
@@ -804,40 +808,46 @@ void launch_attention_of(hipStream_t st, const AttentionArgs &a, int waves) {
 }
 
 template <int BF, int KS>
-void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a, int tiles) {
+void launch_attention_tile_of(hipStream_t st, const AttentionArgs &a, const Split &split) {
   constexpr int NW = KS > (BF ? 4 : 8) ? 4 : 8, NW2 = KS > 4 ? 4 : 8;  // (what their registers allow)
   const dim3 grid((unsigned)a.places, (unsigned)a.parts);
   if constexpr (BF ? KS > 1 && KS <= 4 : KS > 2 && KS <= 8) {
-    if (tiles == 2) {
+    if (split.tiles == 2) {
       hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW2, 2>), grid, dim3(64 * NW2), 0, st, a);
+      return;
+    }
+  }
+  if constexpr (BF && NW == 8) {
+    if (split.waves == 4) {
+      hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, 4, 1>), grid, dim3(256), 0, st, a);
       return;
     }
   }
   hipLaunchKernelGGL((cache_attention_tile_kernel<BF, KS, NW, 1>), grid, dim3(64 * NW), 0, st, a);
 }
-void launch_attention_tile(int bf16, hipStream_t st, const AttentionArgs &a, int tiles) {
+void launch_attention_tile(int bf16, hipStream_t st, const AttentionArgs &a, const Split &split) {
   const int pieces = (a.dh * (bf16 ? 2 : 4) + 63) / 64;  // of 64 bytes
   if (bf16) {
     switch (pieces) {
-      case 1: launch_attention_tile_of<1, 1>(st, a, tiles); break;
-      case 2: launch_attention_tile_of<1, 2>(st, a, tiles); break;
-      case 3: launch_attention_tile_of<1, 3>(st, a, tiles); break;
-      case 4: launch_attention_tile_of<1, 4>(st, a, tiles); break;
-      case 5: launch_attention_tile_of<1, 5>(st, a, tiles); break;
-      case 6: launch_attention_tile_of<1, 6>(st, a, tiles); break;
-      case 7: launch_attention_tile_of<1, 7>(st, a, tiles); break;
-      default: launch_attention_tile_of<1, 8>(st, a, tiles); break;
+      case 1: launch_attention_tile_of<1, 1>(st, a, split); break;
+      case 2: launch_attention_tile_of<1, 2>(st, a, split); break;
+      case 3: launch_attention_tile_of<1, 3>(st, a, split); break;
+      case 4: launch_attention_tile_of<1, 4>(st, a, split); break;
+      case 5: launch_attention_tile_of<1, 5>(st, a, split); break;
+      case 6: launch_attention_tile_of<1, 6>(st, a, split); break;
+      case 7: launch_attention_tile_of<1, 7>(st, a, split); break;
+      default: launch_attention_tile_of<1, 8>(st, a, split); break;
     }
   } else if (pieces <= 2) {
-    launch_attention_tile_of<0, 2>(st, a, tiles);
+    launch_attention_tile_of<0, 2>(st, a, split);
   } else if (pieces <= 4) {
-    launch_attention_tile_of<0, 4>(st, a, tiles);
+    launch_attention_tile_of<0, 4>(st, a, split);
   } else if (pieces <= 8) {
-    launch_attention_tile_of<0, 8>(st, a, tiles);
+    launch_attention_tile_of<0, 8>(st, a, split);
   } else if (pieces <= 12) {
-    launch_attention_tile_of<0, 12>(st, a, tiles);
+    launch_attention_tile_of<0, 12>(st, a, split);
   } else {
-    launch_attention_tile_of<0, 16>(st, a, tiles);
+    launch_attention_tile_of<0, 16>(st, a, split);
   }
   if (a.parts > 1) launch_attention_join(bf16, st, a);
 }
@@ -928,7 +938,7 @@ extern "C" twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pa
   a.acc_parts = need ? scratch + (size_t)T * Hs * a.parts * 2 : nullptr;
   a.scale = 1.44269504089f / sqrtf((float)dh);
   if (split.turns) {
-    launch_attention_tile(ctx->d.dtype == TWIST_BF16, ctx->stream, a, split.tiles);
+    launch_attention_tile(ctx->d.dtype == TWIST_BF16, ctx->stream, a, split);
     TW_HIP(ctx, hipGetLastError());
     return TWIST_OK;
   }
