@@ -168,6 +168,13 @@ def _ints(t, n, what, index):
     return t.data_ptr()
 
 
+def _storage(t, what, index):
+    """Address and bytes of a buffer on GPU `index` that is one run of memory, as the library takes it."""
+    if not t.is_contiguous() or t.get_device() != index:
+        _refuse(f"{what}: needs contiguous memory on GPU {index}")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
 def _check(status, ctx=None):
     if status != 0:
         raise TwistError(status, (lib.twist_last_error(ctx) or b"").decode())
@@ -301,11 +308,10 @@ class Context:
         if logits is None:      # rows that start at multiples of 16 bytes
             logits = self._empty(self.torch_dtype, T, (V + 7) // 8 * 8)[:, :V]
         ldl = self._rows(logits, T, V, "logits", self.torch_dtype)
-        if pages.gpu != self.gpu or cache.get_device() != self.gpu or workspace.get_device() != self.gpu:
-            _refuse(f"table, cache and workspace: need to be on {self.device}")
+        if pages.gpu != self.gpu:
+            _refuse(f"table: needs to be on {self.device}")
         self._call(lib.twist_subnet_decode, sub.h, _ints(tokens, T, "tokens", self.gpu), T, _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len,
-                   pages.ref, cache.data_ptr(), cache.numel() * cache.element_size(), workspace.data_ptr(), workspace.numel() * workspace.element_size(),
-                   logits.data_ptr(), ldl)
+                   pages.ref, *_storage(cache, "cache", self.gpu), *_storage(workspace, "workspace", self.gpu), logits.data_ptr(), ldl)
         return logits
 
     def twist_subnet_step(self, sub: "Subnet", kind=OPT_SGD, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) -> None:
