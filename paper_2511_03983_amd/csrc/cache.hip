@@ -718,8 +718,13 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 //    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
 //    8 x 4096 22 / 10.5 / 11, 32 x 2048 17 / 12.6 / 12.5, 32 x 8192 - / 30.5 / 32.5, 16 x 32768 - / 53.4 / 55.2;
 //    beyond that half, 12 heads of 64 x 16 in fp32 x 2000 32 / 35 / -.  Tiles, whose waves take 32 tokens at a time: 256 KB (16 heads x 4096, 8 rows: parts of 256 / 512 / 1024 22.9 / 18.5 / 25).
-//  - From 2.5 MB on (tiles: 2 MB, (3 x 36) of 64 x 9059, 5 rows 68.9 / 53.4) parts of 1 MB even out rows of different lengths: uncut / cut (8 x 20) x 6000 82.5 / 76.5, x 8000 107 / 90, (12 x 16) x 6000 89.7 / 82.4, (16 x 32) x 6000
-//    196 / 189, (32 x 16) x 16384 511 / 478, (8 x 32) x 6000 107 / 108.5; on the other side (8 x 32) x 4096 74.7 / 79.3, (12 x 16) x 4096 60.6 / 65.7, (16 x 128) x 2048 238 / 246.
+//  - Where workgroups are few enough that the longest row of all decides, parts of 1 MB even out rows of different lengths.  Rows, from 2.5 MB on, up to 1024 workgroups: uncut / cut (8 x 20) x
+//    6000 82.5 / 76.5, x 8000 107 / 90, (12 x 16) x 6000 89.7 / 82.4, (16 x 32) x 6000 196 / 189, (32 x 16) x 16384 493 / 478, (16 x 64) x 8192 495 / 481, (8 x 32) x 6000 107 / 108.5;
+//    on the other side (8 x 32) x 4096 74.7 / 79.3, (12 x 16) x 4096 60.6 / 65.7, (16 x 128) x 2048 238 / 246, x 6000 685 / 690, (32 x 128) x 6000 1351 / 1353.  Tiles, from 2 MB on, between 128
+//    (below, what is said above) and 512: (7 x 20) x 12000, 2 rows 187 / 131, (5 x 36) x 9059, 5 rows 147 / 143, (8 x 36) 260 / 225, (20 x 8) x 8192, 8 rows 133 / 103,
+//    (40 x 8) 208 / 194, (16 x 16) x 6000, 16 rows 117 / 129; on the other side (16 x 8) x 8192, 8 rows 83 / 92, (16 x 32) 277 / 286, (32 x 64) x 6000, 4 rows 703 / 747.  Prompts, whose
+//    rows are many or whose tiles differ by less than they hold, are never cut for it: 4096 tokens, 32 heads 655 / 904, 8 heads 172 / 235, 8192, 2 heads 150 / 230, 1000 behind 6000, 8
+//    heads 118 / 162, fp32 64 wide 176 / 205, bf16 4 heads of 256 217 / 311, 2000 behind 14000, 2 heads of 32 70 / 70.
 //  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
 //    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.  Tiles have 8
 //    waves (what registers allow), or 4 where parts are short and workgroups more than CUs, 8 / 4: (16 x 64) x 250, 8 rows 37.5 / 29.2, (19 x 19) x 926, 8 rows 35.5 / 32.7,
@@ -740,7 +745,8 @@ Split choose_split(int T, int n_seqs, int Hs, int max_len, int shift, int dh, in
   const int64_t units = (s.turns ? std::min(blocks * s.turns, n_seqs + blocks - 1) : T) * Hs;
   int64_t c = max_len;
   if (units <= 128 && max_len * pair > 384 << 10) c = std::max<int64_t>((s.turns ? 256 << 10 : 64 << 10) / pair, max_len / (256 / units));
-  if (max_len * pair >= (s.turns ? 2048 : 2560) << 10) c = std::min<int64_t>(c, (1 << 20) / pair);
+  const bool even_out = s.turns ? max_len * pair >= 2048 << 10 && units > 128 && units < 512 && T < 32 * (int64_t)n_seqs : max_len * pair >= 2560 << 10 && units <= 1024;
+  if (even_out) c = std::min<int64_t>(c, (1 << 20) / pair);
   c = std::max<int64_t>(c, (max_len + kMaxParts - 1) / kMaxParts);
   c = std::min<int64_t>((c + 63) / 64 * 64, (int64_t)(kMaxIds - 1) << shift);  // (one page more where it begins inside one)
   if (tiles) s.waves = es == 2 && units > 256 && c * row_bytes <= 256 << 10 ? 4 : 8;
