@@ -406,7 +406,8 @@ TWIST_API twist_status twist_embed_raw(twist_ctx *ctx, const int32_t *tok, int32
  *                            scratch need not be cleared; it may be NULL where 0 floats are asked for; calls that may run at the same time need one
  *                            each.  Scores, softmax and sums in fp32 (bf16, rows that share a sequence: the weights that values are multiplied by to
  *                            2^-16).  Sequences may share pages.
- * TWIST_ESHAPE if d_head exceeds 256, strides overlap, page_tokens is none of the above or a buffer is too small. */
+ * TWIST_ESHAPE if d_head exceeds 256, strides overlap, page_tokens is none of the above, a buffer is too small, T * Hs reaches 2^22, or an attention's
+ * workgroups do (one for every row and head, or for 16 rows and a head where rows share sequences, and for every 2047 pages of a sequence). */
 TWIST_API twist_status twist_cache_append_raw(twist_ctx *ctx, const twist_pages *pages, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld,
                                               int32_t T, int32_t Hs, const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq);
 TWIST_API twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist_pages *pages, int32_t T, int32_t Hs, int32_t max_len, size_t *floats);

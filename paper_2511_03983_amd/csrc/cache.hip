@@ -787,6 +787,8 @@ Split attention_split(const twist_ctx *ctx, const twist_pages *p, int T, int Hs,
   max_len = (int)std::min<int64_t>(max_len, (int64_t)p->max_pages * p->page_tokens);
   return choose_split(T, p->n_seqs, Hs, max_len, __builtin_ctz((unsigned)p->page_tokens), ctx->d.d_head, ctx->esize(), listed, listed && vec);
 }
+// whether it can be launched: workgroups of up to 1024 threads, of which a launch has less than 2^32, and parts that can be joined
+bool launchable(const Split &s) { return s.parts <= kMaxParts && (int64_t)s.places * s.parts < (int64_t)1 << 22; }
 
 void launch_attention_join(int bf16, hipStream_t st, const AttentionArgs &a) {
   int dlog = 0;
@@ -905,14 +907,23 @@ extern "C" twist_status twist_cache_attention_floats(twist_ctx *ctx, const twist
   TW_TRY(check_cache(ctx, who, pages, (int64_t)Hs * ctx->d.d_head * pages->page_tokens, T, Hs));
   if (max_len < 1) TW_FAIL(ctx, TWIST_EINVAL, "%s: max_len=%d", who, max_len);
   size_t need = 0;
-  for (int form = 0; form < 3; ++form) {  // whether the caller's rows may share sequences, and how they are aligned, is not known here
+  bool any = false;
+  for (int form = 0; form < 3; ++form) {  // whether the caller's rows may share sequences, and how they are aligned, is not known here: the most of what can run
     int most = max_len;
     const Split s = attention_split(ctx, pages, T, Hs, most, form > 0, form > 1 && ctx->d.d_head * ctx->esize() % 16 == 0);
-    if (s.parts > kMaxParts || (int64_t)s.places * s.parts >= (int64_t)1 << 22)  // (workgroups of 1024 threads, of which a launch has less than 2^32)
-      TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
+    if (!launchable(s)) continue;
+    any = true;
     if (s.parts > 1) need = std::max(need, (size_t)T * Hs * s.parts * (ctx->d.d_head + 2));
   }
+  if (!any) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
   *floats = need;
+  return TWIST_OK;
+}
+
+twist_status twist_cache_attention_check(twist_ctx *ctx, const char *who, const twist_pages *pages, int T, int Hs, int max_len, bool listed) {
+  int most = max_len;
+  if (!launchable(attention_split(ctx, pages, T, Hs, most, listed, ctx->d.d_head * ctx->esize() % 16 == 0)))
+    TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
   return TWIST_OK;
 }
 
@@ -939,6 +950,7 @@ extern "C" twist_status twist_cache_attention_raw(twist_ctx *ctx, const twist_pa
   const int es = ctx->esize();
   const bool vec = dh * es % 16 == 0 && al16(k, page_stride * es) && al16(v) && al16(q, ldq * es);
   const Split split = attention_split(ctx, pages, T, Hs, a.max_len, seq != nullptr, vec);
+  if (!launchable(split)) TW_FAIL(ctx, TWIST_ESHAPE, "%s: %d rows of %d heads over %d tokens are too many for one call", who, T, Hs, max_len);
   a.turns = split.turns; a.run = split.run; a.places = split.places; a.parts = split.parts; a.chunk = split.chunk;
   a.ml_parts = scratch;
   a.acc_parts = need ? scratch + (size_t)T * Hs * a.parts * 2 : nullptr;

@@ -130,6 +130,8 @@ extern "C" twist_status twist_subnet_decode(twist_ctx *ctx, twist_subnet *sub, c
   const twist_model_desc &d = ctx->d;
   if (ldl < d.vocab) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows of logits overlap", who);
   if (reinterpret_cast<uintptr_t>(cache) % 256 || reinterpret_cast<uintptr_t>(workspace) % 256) TW_FAIL(ctx, TWIST_ESHAPE, "%s: cache and workspace must be 256-byte aligned", who);
+  const bool listed = seq || T > pages->n_seqs;  // (row t of sequence t needs no list)
+  for (int32_t heads : sub->plan->layout.heads_sub) TW_TRY(twist_cache_attention_check(ctx, who, pages, T, heads, max_len, listed));  // (before anything is appended)
   const size_t need = cache_size(ctx, sub, pages);
   if (cache_bytes < need) TW_FAIL(ctx, TWIST_ESHAPE, "%s: cache of %zu bytes is smaller than the %zu needed", who, cache_bytes, need);
   Workspace w;
@@ -153,7 +155,7 @@ extern "C" twist_status twist_subnet_decode(twist_ctx *ctx, twist_subnet *sub, c
   else hipLaunchKernelGGL((decode_embed_kernel<0>), grid, dim3(kT), 0, ctx->stream, tokens, seq, lens, T, pages->n_seqs, max_len, P(L.global[TWIST_TOK_EMBED]),
                           P(L.global[TWIST_POS_EMBED]), w.x[0], w.used, w.of, D, d.vocab);
   TW_HIP(ctx, hipGetLastError());
-  const int32_t *of = seq || T > pages->n_seqs ? w.of : nullptr;  // (row t of sequence t needs no list)
+  const int32_t *of = listed ? w.of : nullptr;
   char *k = static_cast<char *>(cache), *v;
   for (int l = 0; l < d.n_layers; ++l, k = v + pool_bytes(ctx, sub, pages, l - 1)) {
     const int Hs = L.heads_sub[l], HD = Hs * dh, F = L.ffn_sub[l] * d.ffn_granule;

@@ -153,6 +153,9 @@ twist_status twist_act_fwd(twist_ctx *ctx, int bf16, int act, const void *gu, vo
 twist_status twist_act_bwd(twist_ctx *ctx, int bf16, int act, const void *gu, const void *da, void *dgu, int T, int F, const int32_t *keep = nullptr,
                            int unit = 1, float *sums = nullptr);
 
+// whether twist_cache_attention_raw has a launch for these rows, with a list of sequences or without, over pools and queries that are aligned as heads allow
+twist_status twist_cache_attention_check(twist_ctx *ctx, const char *who, const twist_pages *pages, int T, int Hs, int max_len, bool listed);
+
 // logits [T,V] -> in place dlogits = (softmax - onehot)/T (grad) or left alone; row losses to rowloss[T]; then loss = mean
 twist_status twist_ce_fwd_bwd(twist_ctx *ctx, int bf16, void *logits, int64_t ld, const int32_t *targets, float *rowloss, float *loss, int T, int V, bool grad = true);
 // the same loss from the parts that a projection left (GemmEpilogue::targets); rowloss holds the target logits and receives the row losses
