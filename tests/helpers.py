@@ -56,3 +56,17 @@ def bf16_ulp_distance(a, b):
         u = np.asarray(x, np.float32).view(np.uint32).astype(np.int64) >> 16
         return np.where(u & 0x8000, 0x8000 - u, u)      # monotone integer order
     return np.abs(key(a) - key(b))
+
+
+def within(got, want, err, u):
+    """Every element of `got` within a rounding u of the 64-bit `want` and `err` beside it; one that is no number is within none."""
+    got, want = got.double().cpu(), want.cpu()
+    off = (got - want).abs()
+    ok = off <= u * want.abs() + err * (1 + u)
+    assert ok.all(), (int((~ok).sum()), float(off.max()))
+
+
+def rel_fro_of_numbers(a, b):
+    """rel_fro, which is NaN, and so compares with no bound, where either holds something that is no number: refused here."""
+    assert np.isfinite(a).all() and np.isfinite(b).all()
+    return rel_fro(a, b)

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 import test_gpu_decode as decode
+from helpers import within
 from test_gpu_generate import Deployed
 
 pytestmark = pytest.mark.gpu
@@ -21,12 +22,6 @@ def test_decode_refuses_storage_with_gaps(lib):
     assert (ws == 0xaa).all() and (big == 0xaa).all() and (d.cache == 0xff).all()
 
 
-def _within(got, want, err, u):
-    """Every element within its bound; what is no number is within none."""
-    got, want = got.double().cpu(), want.cpu()
-    assert ((got - want).abs() <= u * want.abs() + err * (1 + u)).all(), float((got - want).abs().max())
-
-
 def test_a_prompt_of_more_rows_and_parts_than_workgroups_of_a_launch(lib):
     """4096 rows of 104 heads over ten parts (pages of a token): tiles, where a workgroup a row would be 2^22 of them and more."""
     T, Hs, dh, top = 4096, 104, 8, 20470
@@ -42,6 +37,6 @@ def test_a_prompt_of_more_rows_and_parts_than_workgroups_of_a_launch(lib):
     torch.cuda.synchronize()
     rows = torch.tensor([0, 1500, 4095], device="cuda")
     wo, wl, eo, el = decode._attention_want(k, v, table, q[rows], lens[rows], seq[rows], top, Hs, dh)
-    _within(o[rows], wo, eo, decode.U[decode.BF])
+    within(o[rows], wo, eo, decode.U[decode.BF])
     assert ((lse[rows].double().cpu() - wl).abs() <= el).all()
     assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
