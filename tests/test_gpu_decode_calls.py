@@ -1,4 +1,5 @@
-"""Calls of token generation as a caller may make them, beside the kernels' own cases: buffers with gaps, prompts near the limits of a launch."""
+"""Calls of token generation as a caller may make them, beside the kernels' own cases: buffers with gaps, prompts near the limits of a launch, batches of
+sequences with a few rows each."""
 import pytest
 import torch
 
@@ -7,6 +8,11 @@ from helpers import within
 from test_gpu_generate import Deployed
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def numbers_only(monkeypatch):
+    monkeypatch.setattr(decode, "_close", within)
 
 
 def test_decode_refuses_storage_with_gaps(lib):
@@ -40,3 +46,41 @@ def test_a_prompt_of_more_rows_and_parts_than_workgroups_of_a_launch(lib):
     within(o[rows], wo, eo, decode.U[decode.BF])
     assert ((lse[rows].double().cpu() - wl).abs() <= el).all()
     assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+
+
+def _batch(S, r, top, order):
+    """Lengths and sequences of S times r rows, one length of each sequence near the top, and what a batch holds beside them."""
+    ends = [max(r, top - (top * s) // S) for s in range(S)]
+    rows = [(ends[s] - r + 1 + i, s) for s in range(S) for i in range(r)]
+    if order == "mixed":                                               # no two neighbours of one sequence: a tile holds 16 groups
+        rows = [rows[s * r + i] for i in range(r) for s in range(S)]
+    elif order == "ragged":                                            # runs of 1 to 2 r - 1 rows across the tiles, unused rows between them
+        rows = [x for i, x in enumerate(rows) if i % (2 * r) or i % 5]
+        for at in (3, 17, 40):
+            rows[at:at] = [(0, rows[at][1]), (-1, rows[at][1]), (5, -1), (7, S)]
+    return [n for n, _ in rows], [s for _, s in rows]
+
+
+@pytest.mark.parametrize("order", ["runs", "mixed", "ragged"])
+@pytest.mark.parametrize("Hs,dh,S,r,top", [(8, 128, 40, 2, 600), (8, 96, 40, 3, 500), (12, 64, 32, 5, 310), (16, 40, 40, 4, 300), (16, 80, 24, 4, 280), (16, 32, 30, 6, 300),  # workgroups of 4 waves
+                                           (8, 128, 24, 8, 250), (4, 64, 20, 7, 1000), (3, 40, 40, 4, 1800), (2, 96, 30, 12, 500), (1, 32, 36, 15, 2000), (4, 256, 20, 3, 600)])
+def test_attention_of_a_few_rows_of_many_sequences(lib, Hs, dh, S, r, top, order):
+    """bf16 tiles that several workgroups share, each taking every second to eighth group of their rows."""
+    lens, seq = _batch(S, r, top, order)
+    decode._check_attention(lib, decode.BF, Hs, dh, 16, lens, seq, n_seqs=S, max_len=top, max_pages=-(-top // 16), holes=[(1, 0), (2, 3), (S - 1, 1)])
+
+
+@pytest.mark.parametrize("order", ["runs", "mixed", "ragged"])
+@pytest.mark.parametrize("Hs,dh,S,r,top", [(8, 128, 20, 4, 520), (12, 64, 24, 3, 700), (12, 40, 24, 8, 400), (8, 80, 20, 6, 700), (4, 32, 40, 12, 800), (4, 256, 12, 5, 600)])
+def test_fp32_attention_of_a_few_rows_of_many_sequences(lib, Hs, dh, S, r, top, order):
+    lens, seq = _batch(S, r, top, order)
+    decode._check_attention(lib, decode.F32, Hs, dh, 16, lens, seq, n_seqs=S, max_len=top, max_pages=-(-top // 16), holes=[(1, 0), (2, 3), (S - 1, 1)])
+
+
+@pytest.mark.parametrize("dtype,dh", [(decode.BF, 128), (decode.F32, 64)])
+def test_attention_of_a_few_rows_of_many_long_sequences(lib, dtype, dh):
+    """The same where sequences are cut into parts, the last of which few of them reach."""
+    S, r, top = 40, 3, 4300
+    lens, seq = _batch(S, r, top, "runs")
+    lens = [n if s in (0, 1, 2, 20) else min(n, 90 + n % 7) for n, s in zip(lens, seq)]
+    decode._check_attention(lib, dtype, 4, dh, 64, lens, seq, n_seqs=S, max_len=top, max_pages=-(-top // 64), holes=[(1, 0), (0, 40)] + [(2, i) for i in range(16, 40)])
