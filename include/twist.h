@@ -226,7 +226,9 @@ TWIST_API twist_status twist_subnet_forward(twist_ctx *ctx, twist_subnet *sub, c
 /* A paged cache of keys and values: pools k and v (desc.dtype), each n_pages pages of [Hs][page_tokens][d_head] whose starts lie page_stride elements apart
  * (at least Hs * page_tokens * d_head), as many key/value heads as query heads.  Row s of the table names the pages of sequence s in order: token p of it
  * lies in page table[s][p / page_tokens], at place p % page_tokens.  Entries outside [0, n_pages) are pages that the sequence does not have: no key
- * is written there, and attention sees none.  A sequence holds max_pages * page_tokens tokens at most. */
+ * is written there, and attention sees none.  A sequence holds max_pages * page_tokens tokens at most.  The host does not know which of the n_seqs sequences the
+ * rows of a call belong to, and chooses kernels as if they were spread over all: rows of a few sequences, a prompt above all, are faster through a table of these
+ * alone (table + s * ld_table with n_seqs = 1, and 0 in seq), with the same results up to rounding. */
 typedef struct {
   const int32_t *table;  /* dev [n_seqs] rows of max_pages entries, ld_table apart */
   int64_t ld_table;

@@ -651,7 +651,8 @@ class Subnet:
 
 
 class Pages:
-    """A page table [n_seqs, max_pages] (int32, entries outside [0, n_pages): no page) over pools of n_pages pages of page_tokens tokens."""
+    """A page table [n_seqs, max_pages] (int32, entries outside [0, n_pages): no page) over pools of n_pages pages of page_tokens tokens.  Kernels are chosen as if a
+    call's rows were spread over all n_seqs: a prompt is faster through a table of its own row, Pages(table[s:s + 1], ...) with 0 in seq."""
 
     def __init__(self, table: torch.Tensor, n_pages: int, page_tokens: int):
         if not (table.is_cuda and table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1)):

@@ -703,7 +703,8 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
   finish<BF>(A, t, h, tid, a, M, L, any);
 }
 
-// Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens.  Figures are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
+// Kernel, waves of a workgroup, parts of a sequence and their length, for T rows of Hs heads over at most max_len tokens.  n_seqs, the table's rows, stands for the
+// sequences that the T rows are of (the host does not see whose they are; the caller may pass a table of those alone).  Figures are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
 //  - Tiles (turns > 0; a workgroup takes every turns-th group among 16 rows): where sequences have several rows each on average, the more the shorter they may be
 //    (rows beyond 16 a sequence fill no more of a tile), and enough of both to fill the chip.  bf16, (heads x sequences) x tokens, r rows each, rows / tiles: (16 x 16) x 64, 16 rows 12.5 / 7.1,
 //    (16 x 64) x 64, 8 rows 23.8 / 27.1, x 250 47 / 37.7, (12 x 32) of 64 x 100, 5 rows 8.8 / 10.9, x 300 15.8 / 15.6, (19 x 19) x 926, 8 rows 83 / 34.8, a prompt of 1000,

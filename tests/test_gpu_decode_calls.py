@@ -1,11 +1,13 @@
 """Calls of token generation as a caller may make them, beside the kernels' own cases: buffers with gaps, prompts near the limits of a launch, batches of
-sequences with a few rows each."""
+sequences with a few rows each, prompts in large tables."""
+import numpy as np
 import pytest
 import torch
 
+import synth_inputs as si
 import test_gpu_decode as decode
-from helpers import within
-from test_gpu_generate import Deployed
+from helpers import rel_fro_of_numbers, to_numpy, within
+from test_gpu_generate import Deployed, _bound
 
 pytestmark = pytest.mark.gpu
 
@@ -84,3 +86,43 @@ def test_attention_of_a_few_rows_of_many_long_sequences(lib, dtype, dh):
     lens, seq = _batch(S, r, top, "runs")
     lens = [n if s in (0, 1, 2, 20) else min(n, 90 + n % 7) for n, s in zip(lens, seq)]
     decode._check_attention(lib, dtype, 4, dh, 64, lens, seq, n_seqs=S, max_len=top, max_pages=-(-top // 64), holes=[(1, 0), (0, 40)] + [(2, i) for i in range(16, 40)])
+
+
+@pytest.mark.parametrize("dtype", [decode.BF, decode.F32])
+@pytest.mark.parametrize("n_seqs", [1, 8, 40, 200, 600])
+def test_a_prompt_in_a_table_of_any_size(lib, dtype, n_seqs):
+    """Kernels are chosen by the table's rows: one prompt of 400 rows through each form of them, and through its own row of the table alone."""
+    Hs, dh, T, top, page = 4, 64, 400, 800, 16
+    ctx, g = decode._ctx(lib, dtype, dh), decode._gen(31)
+    n_pages = top // page + 5
+    k, v = decode._pools(g, n_pages, Hs, page, dh, dtype)
+    at = n_seqs // 2
+    table = torch.full((n_seqs, top // page), -1, dtype=torch.int32, device="cuda")
+    table[at] = torch.randperm(n_pages, generator=g, device="cuda")[: top // page].to(torch.int32)
+    q = decode._randn(g, T, Hs * dh, dtype=dtype, scale=1.5)
+    lens = (torch.arange(T, device="cuda") + top - T + 1).to(torch.int32)
+    seq = torch.full((T,), at, dtype=torch.int32, device="cuda")
+    rows = torch.arange(0, T, 37, device="cuda")
+    for pages, which in ((table, seq), (table[at:at + 1], torch.zeros_like(seq))):
+        o, lse = ctx.twist_cache_attention_raw(lib.PagedCache(k, v, pages), q, lens, top, seq=which)
+        torch.cuda.synchronize()
+        wo, wl, eo, el = decode._attention_want(k, v, pages, q[rows], lens[rows], which[rows], top, Hs, dh)
+        within(o[rows], wo, eo, decode.U[dtype])
+        assert ((lse[rows].double().cpu() - wl).abs() <= el).all()
+        assert torch.isfinite(o.float()).all() and torch.isfinite(lse).all()
+
+
+@pytest.mark.parametrize("name", ["llama_f32_um", "llama_bf16", "gpt_bf16"])
+def test_a_prompt_through_its_own_row_of_the_table(lib, name):
+    """A prompt of one of 40 sequences through a table of that row alone, then tokens through the whole table: one cache, the oracle's logits."""
+    d = Deployed(lib, name, 40, 64)
+    ids = si.tokens_uniform(d.cfg.vocab, 1, 64, 5)[0][:52]
+    s, n = 23, 48
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()  # noqa: E731
+    own = lib.Pages(d.table[s:s + 1], d.pages.n_pages, d.page)
+    assert d.ctx.twist_cache_bytes(d.sub, own) == d.cache.numel()
+    ws = torch.full((d.ctx.twist_decode_workspace_bytes(d.sub, own, n, 64),), 0xff, dtype=torch.uint8, device="cuda")
+    got = list(to_numpy(d.ctx.twist_subnet_decode(d.sub, i32(ids[:n].tolist()), i32(list(range(1, n + 1))), 64, own, d.cache, ws, seq=i32([0] * n))))
+    for p in range(n, len(ids)):
+        got.append(to_numpy(d.step([3, int(ids[p])], [1, p + 1], [7, s], 64))[1])
+    assert rel_fro_of_numbers(np.stack(got), d.want(ids)) <= _bound(d.cfg)
