@@ -1,5 +1,5 @@
 """Calls of token generation as a caller may make them, beside the kernels' own cases: buffers with gaps, prompts near the limits of a launch, batches of
-sequences with a few rows each, prompts in large tables."""
+sequences with a few rows each, prompts in large tables, logits at any place, tables in others."""
 import numpy as np
 import pytest
 import torch
@@ -126,3 +126,48 @@ def test_a_prompt_through_its_own_row_of_the_table(lib, name):
     for p in range(n, len(ids)):
         got.append(to_numpy(d.step([3, int(ids[p])], [1, p + 1], [7, s], 64))[1])
     assert rel_fro_of_numbers(np.stack(got), d.want(ids)) <= _bound(d.cfg)
+
+
+@pytest.mark.parametrize("name", ["gpt_bf16", "llama_f32_um", "ragged_f32", "llama_bf16_um"])
+@pytest.mark.parametrize("T", [3, 40])
+def test_logits_at_any_place(lib, name, T):
+    """Rows of logits of any stride, from any element on: the same numbers up to rounding, nothing beside them."""
+    d = Deployed(lib, name, T, 16)
+    V, dt = d.cfg.vocab, d.ctx.torch_dtype
+    step = lambda out: d.step([t % V for t in range(T)], [1] * T, max_len=16, logits=out)  # noqa: E731
+    base = step(None).clone()
+    assert torch.isfinite(base.float()).all()
+    for ldl, at in ((V, 0), (V + 1, 1), (V + 5, 3), (V + 8 - V % 8, 2)):
+        buf = torch.full((T * ldl + 8,), 7.0, dtype=dt, device="cuda")
+        out = buf.as_strided((T, V), (ldl, 1), at)
+        step(out)
+        torch.cuda.synchronize()
+        assert rel_fro_of_numbers(to_numpy(out), to_numpy(base)) <= _bound(d.cfg)
+        out.fill_(7.0)
+        assert (buf == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [decode.BF, decode.F32])
+def test_tables_that_are_part_of_others(lib, dtype):
+    """A table whose rows lie further apart than they are long, or that begins inside one: what lies between is not the sequence's."""
+    Hs, dh, page, S = 3, 64, 16, 5
+    ctx, g = decode._ctx(lib, dtype, dh, rope=True), decode._gen(17)
+    k, v = decode._pools(g, 64, Hs, page, dh, dtype)
+    whole = torch.randint(0, 64, (S + 2, 12), generator=g, device="cuda", dtype=torch.int32)
+    whole[1:6, 2:10] = torch.randperm(64, generator=g, device="cuda")[:40].view(5, 8).to(torch.int32)
+    part = whole[1:6, 2:10]
+    qkv, lens = decode._randn(g, S, 3 * Hs * dh, dtype=dtype), decode._i32(1, 17, 100, 128, 129)       # the last: beyond its eight pages
+    q = torch.zeros((S, Hs * dh), dtype=k.dtype, device="cuda")
+    wq, wk, wv, eq, ek = decode._append_want(k, v, part, qkv, lens, None, q, Hs, dh, True, 10000.0)
+    cache = lib.PagedCache(k, v, part)
+    ctx.twist_cache_append_raw(cache, qkv, lens, q_out=q)
+    torch.cuda.synchronize()
+    within(q, wq, eq, decode.U[dtype])
+    within(k, wk, ek, torch.where(ek > 0, decode.U[dtype], 0.0))
+    assert torch.equal(v.double().cpu(), wv)
+    for seq in (None, decode._i32(4, 4, 3, 2, 2)):
+        o, lse = ctx.twist_cache_attention_raw(cache, q, lens, 200, seq=seq)
+        torch.cuda.synchronize()
+        wo, wl, eo, el = decode._attention_want(k, v, part, q, lens, seq, 200, Hs, dh)
+        within(o, wo, eo, decode.U[dtype])
+        assert ((lse.double().cpu() - wl).abs() <= el).all()
