@@ -439,6 +439,49 @@ typedef struct {
  * [T, vocab] fp32, rows ldo apart, receives the result; columns beyond vocab are left as they were.  fp32 models: out may be the logits themselves. */
 TWIST_API twist_status twist_logits_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t T, const twist_logit_rules *rules, float *out, int64_t ldo);
 
+/* What a draw keeps of a row's distribution.  Any pointer may be NULL: the rule is not applied. */
+typedef struct {
+  const float *temperature; /* dev [T]: logits are divided by it; where it is not above 0 the largest logit is taken (NULL: 1) */
+  const int32_t *top_k;     /* dev [T]: the top_k largest logits are kept (below 1: all) */
+  const float *top_p;       /* dev [T]: of these, largest first, as few as have top_p of their probability together, one at least (1 and above: all) */
+  const float *min_p;       /* dev [T]: of these, those at least min_p times as probable as the most probable one */
+} twist_draw_rules;
+/* Draws a token for each of T rows of logits [T, vocab] (rows ld apart; fp32 where logits_f32 is not 0, as twist_logits_raw leaves them, else dtype) with the random
+ * number uniform[t] (dev, in [0, 1); numbers outside count as the nearest inside) and the rules (NULL: none).  A row's columns are ordered by logit, largest first, equal ones by column;
+ * the token is the first at which the probabilities of the kept columns, summed in this order, exceed uniform[t] times their sum.  tokens [T] (dev) receives its column, logprobs [T]
+ * (fp32, may be NULL) the logarithm of its probability among the kept columns, kept [T] (int32, may be NULL) their number.  Columns at -infinity, and those that hold no
+ * number, are never kept; a row without any other gives token -1, -infinity and 0.  Of a row with +infinity only such columns have a probability.  Probabilities and their sums are whole
+ * multiples of 2^-42 of the largest (2^-46 up to 2^16 columns), so that no order of summation changes a token.
+ *
+ * twist_top_logits_raw: the k largest (1 <= k <= 1024) of each of T rows of logits in the same order: ids [T, k] (int32) and values [T, k] (fp32; rows of both ldk apart), and rest
+ * [T] (fp32, may be NULL), the log-sum-exp of the row's other logits divided by the temperature (> 0): -infinity where there are none.  Columns that hold no number count as
+ * -infinity.  Entries beyond the vocabulary: id -1, value -infinity.
+ * TWIST_ESHAPE without a vocabulary, for rows that overlap, 2^22 rows and more, a vocabulary of 2^20 and more. */
+TWIST_API twist_status twist_draw_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t logits_f32, int32_t T, const float *uniform, const twist_draw_rules *rules,
+                                      int32_t *tokens, float *logprobs, int32_t *kept);
+TWIST_API twist_status twist_top_logits_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t logits_f32, int32_t T, int32_t k, float temperature, int32_t *ids,
+                                            float *values, int64_t ldk, float *rest);
+
+/* What a teacher says about T tokens: k of its logits each (1 <= k <= 1024; ids outside the vocabulary are entries that are not there, of one that is named twice the
+ * probabilities add up), and optionally the log-sum-exp of its other logits divided by the temperature: what twist_top_logits_raw gives. */
+typedef struct {
+  const int32_t *ids;   /* dev [T] rows of k, ld apart */
+  const float *values;  /* dev, likewise */
+  const float *rest;    /* dev [T]; NULL: the entries are the whole of its distribution */
+  int64_t ld;
+  int32_t k;
+  float temperature;    /* > 0: teacher's and student's logits are divided by it */
+  float weight;         /* 0 to 1: the teacher's share of the loss; the targets have the others */
+} twist_teacher;
+/* The loss of T rows of a student's logits [T, vocab] (dtype, rows ld apart) and its gradient.  With the teacher's probabilities q of its entries, and of all its other tokens together (rest), and
+ * the student's p of the same, both at the temperature, row t counts
+ *     weight * temperature^2 * sum q (log q - log p)  +  (1 - weight) * cross-entropy(logits, targets[t])
+ * A row without an entry or rest has no teacher, one with a target outside the vocabulary no target: that part of it is 0.  targets (dev [T]) may be NULL where weight is 1.  loss (fp32
+ * scalar) receives the mean over all T rows, rowloss [T] (fp32) the rows', grad [T, vocab] (dtype, rows ldg apart; the logits themselves, ldg = ld, or memory apart from them) the mean's
+ * gradient; columns beyond vocab are left as they were.  Errors as twist_top_logits_raw. */
+TWIST_API twist_status twist_distill_raw(twist_ctx *ctx, const void *logits, int64_t ld, const int32_t *targets, int32_t T, const twist_teacher *teacher, void *grad, int64_t ldg,
+                                         float *rowloss, float *loss);
+
 /* Measurement aid for benchmarks (not part of the method): while enabled, every projection (GEMM) launch on
  * this ctx is bracketed by two HIP events on the ctx's stream.  twist_profile_gemm_read synchronises the
  * stream, returns the number of launches, their summed duration in milliseconds and their summed algorithmic

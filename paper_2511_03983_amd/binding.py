@@ -11,6 +11,7 @@ __all__ = [
     "TwistError", "ModelDesc", "SampleDesc", "OptDesc", "lib", "Context", "Plan", "Subnet", "FullWeights",
     "LAYER_TENSORS", "GLOBAL_TENSORS", "F32", "BF16", "KIND_HEAD", "KIND_FFN", "STORE_PARAMS", "STORE_GRADS",
     "STORE_ADAMW", "OPT_SGD", "OPT_ADAMW", "SCALE_NONE", "SCALE_SQRT_RATIO", "desc_from_cfg", "Pages", "PagedCache", "LogitRules",
+    "DrawRules", "Teacher",
 ]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -83,6 +84,14 @@ class LogitRulesC(C.Structure):
                 ("ld_bias", C.c_int64), ("bias_cap", C.c_int32), ("n_bias", C.c_void_p), ("allowed", C.c_void_p), ("ld_allowed", C.c_int64)]
 
 
+class DrawRulesC(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
+class TeacherC(C.Structure):
+    _fields_ = [("ids", C.c_void_p), ("values", C.c_void_p), ("rest", C.c_void_p), ("ld", C.c_int64), ("k", C.c_int32), ("temperature", C.c_float), ("weight", C.c_float)]
+
+
 _vp, _i32, _sz = C.c_void_p, C.c_int32, C.c_size_t
 _PI32 = C.POINTER(C.c_int32)
 _SIGS = {
@@ -132,6 +141,9 @@ _SIGS = {
     "twist_cache_attention_floats": ([_vp, C.POINTER(PagesC), _i32, _i32, _i32, C.POINTER(_sz)], _i32),
     "twist_cache_attention_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _i32, _vp, C.c_int64, _vp, _vp, _sz], _i32),
     "twist_logits_raw": ([_vp, _vp, C.c_int64, _i32, C.POINTER(LogitRulesC), _vp, C.c_int64], _i32),
+    "twist_draw_raw": ([_vp, _vp, C.c_int64, _i32, _i32, _vp, C.POINTER(DrawRulesC), _vp, _vp, _vp], _i32),
+    "twist_top_logits_raw": ([_vp, _vp, C.c_int64, _i32, _i32, _i32, C.c_float, _vp, _vp, C.c_int64, _vp], _i32),
+    "twist_distill_raw": ([_vp, _vp, C.c_int64, _vp, _i32, C.POINTER(TeacherC), _vp, C.c_int64, _vp, _vp], _i32),
     "twist_set_kernel_choice": ([_vp, _i32, _i32, _i32], _i32),
     "twist_profile_gemm": ([_vp, _i32], _i32),
     "twist_set_overlap": ([_vp, _i32], _i32),
@@ -159,12 +171,12 @@ def _refuse(message):
     raise TwistError(1, message)
 
 
-def _ints(t, n, what, index):
-    """Address of an int32 vector of n on GPU `index` (None stays NULL)."""
+def _ints(t, n, what, index, dtype=torch.int32):
+    """Address of a vector of n (int32, or another type) on GPU `index` (None stays NULL)."""
     if t is None:
         return None
-    if t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != index:
-        _refuse(f"{what}: needs a contiguous int32 vector of {n} on GPU {index}")
+    if t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous() or t.get_device() != index:
+        _refuse(f"{what}: needs a contiguous {str(dtype)[6:]} vector of {n} on GPU {index}")
     return t.data_ptr()
 
 
@@ -538,6 +550,62 @@ class Context:
         self._call(lib.twist_logits_raw, logits.data_ptr(), ld, T, rules.ref, out.data_ptr(), ldo)
         return out
 
+    def _logits(self, logits: torch.Tensor):
+        """(rows, row stride, whether fp32) of logits [T, vocab] in the model's type or fp32."""
+        f32 = logits.dtype is torch.float32
+        T = logits.shape[0]
+        return T, self._rows(logits, T, self.desc.vocab, "logits", torch.float32 if f32 else self.torch_dtype), int(f32)
+
+    def twist_draw_raw(self, logits: torch.Tensor, uniform: torch.Tensor, rules: "DrawRules | None" = None, tokens: torch.Tensor | None = None,
+                       logprobs: torch.Tensor | None = None, kept: torch.Tensor | None = None):
+        """(tokens, logprobs, kept) [T] drawn from logits [T, vocab] (fp32 or the model's type) with the random numbers uniform [T] (fp32).  Vectors that are given
+        receive the results.  See include/twist.h."""
+        T, ld, f32 = self._logits(logits)
+        if rules is not None and not (rules.T in (None, T) and rules.gpu in (None, self.gpu)):
+            _refuse(f"rules: need {T} rows on {self.device}")
+        tokens = self._empty(torch.int32, T) if tokens is None else tokens
+        logprobs = self._empty(torch.float32, T) if logprobs is None else logprobs
+        kept = self._empty(torch.int32, T) if kept is None else kept
+        if uniform is None:
+            _refuse("uniform: a draw needs its random numbers")
+        self._call(lib.twist_draw_raw, logits.data_ptr(), ld, f32, T, _ints(uniform, T, "uniform", self.gpu, torch.float32), None if rules is None else rules.ref,
+                   _ints(tokens, T, "tokens", self.gpu), _ints(logprobs, T, "logprobs", self.gpu, torch.float32), _ints(kept, T, "kept", self.gpu))
+        return tokens, logprobs, kept
+
+    def twist_top_logits_raw(self, logits: torch.Tensor, k: int, temperature: float = 1.0, ids: torch.Tensor | None = None, values: torch.Tensor | None = None,
+                             rest: torch.Tensor | None = None):
+        """(ids int32 [T, k], values fp32 [T, k], rest fp32 [T]): the k largest of logits [T, vocab] (fp32 or the model's type) in order, and the log-sum-exp of the
+        others over the temperature.  Tensors that are given receive the results (ids and values: one row stride).  See include/twist.h."""
+        T, ld, f32 = self._logits(logits)
+        if ids is None:
+            ids = self._empty(torch.int32, T, k)
+        if values is None:
+            values = self._empty(torch.float32, T, k)
+        if rest is None:
+            rest = self._empty(torch.float32, T)
+        ldk = self._rows(ids, T, k, "ids", torch.int32)
+        if self._rows(values, T, k, "values", torch.float32) != ldk:
+            _refuse("ids and values: need one row stride")
+        self._call(lib.twist_top_logits_raw, logits.data_ptr(), ld, f32, T, k, temperature, ids.data_ptr(), values.data_ptr(), ldk,
+                   _ints(rest, T, "rest", self.gpu, torch.float32))
+        return ids, values, rest
+
+    def twist_distill_raw(self, logits: torch.Tensor, targets: torch.Tensor | None, teacher: "Teacher", grad: torch.Tensor | None = None):
+        """(loss fp32 scalar, rowloss fp32 [T], grad [T, vocab]) of a student's logits [T, vocab] against the teacher's and the targets (int32 [T]; None with weight 1).
+        grad, where given, receives the gradient; it may be the logits.  See include/twist.h."""
+        T, V = logits.shape[0], self.desc.vocab
+        ld = self._rows(logits, T, V, "logits", self.torch_dtype)
+        if teacher.T != T or teacher.gpu != self.gpu:
+            _refuse(f"teacher: needs {T} rows on {self.device}")
+        if grad is None:
+            grad, ldg = self._empty(self.torch_dtype, T, V), V
+        else:
+            ldg = self._rows(grad, T, V, "grad", self.torch_dtype)
+        rowloss, loss = self._empty(torch.float32, T), self._empty(torch.float32, ())
+        self._call(lib.twist_distill_raw, logits.data_ptr(), ld, _ints(targets, T, "targets", self.gpu), T, teacher.ref, grad.data_ptr(), ldg, rowloss.data_ptr(),
+                   loss.data_ptr())
+        return loss, rowloss, grad
+
     def twist_set_kernel_choice(self, gemm_tile: int = 0, plain_only: bool = False, staged_attention: bool = False) -> None:
         _check(lib.twist_set_kernel_choice(self.h, gemm_tile, int(plain_only), int(staged_attention)), self.h)
 
@@ -707,6 +775,44 @@ class LogitRules:
         self.words = None if allowed is None else allowed.shape[1]
         self.c = LogitRulesC(_addr(history), ld(history), cap(history), _addr(n_history), _addr(n_prompt), _addr(repetition), _addr(frequency), _addr(presence),
                              _addr(bias_ids), _addr(bias_values), ld(bias_ids), cap(bias_ids), _addr(n_bias), _addr(allowed), ld(allowed))
+        self.ref = C.pointer(self.c)
+
+
+class DrawRules:
+    """What twist_draw_raw keeps of each of T rows, in this order (every tensor optional): temperature (fp32 [T]; 0: the largest logit), top_k (int32 [T]), top_p and
+    min_p (fp32 [T])."""
+
+    def __init__(self, temperature=None, top_k=None, top_p=None, min_p=None):
+        self.keep = dict(temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+        self.T = self.gpu = None
+        for name, t in self.keep.items():
+            if t is None:
+                continue
+            if not (t.is_cuda and t.dtype == (torch.int32 if name == "top_k" else torch.float32) and t.dim() == 1 and t.is_contiguous()):
+                _refuse(f"{name}: needs CUDA {'int32' if name == 'top_k' else 'fp32'} values, contiguous")
+            if self.T not in (None, t.shape[0]) or self.gpu not in (None, t.get_device()):
+                _refuse(f"{name}: another number of rows or GPU than the others")
+            self.T, self.gpu = t.shape[0], t.get_device()
+        self.c = DrawRulesC(*map(_addr, (temperature, top_k, top_p, min_p)))
+        self.ref = C.pointer(self.c)
+
+
+class Teacher:
+    """A teacher's top logits as twist_top_logits_raw gives them, ids (int32) and values (fp32) [T, k] of one row stride and rest (fp32 [T], optional), with the temperature
+    and the teacher's weight in the loss."""
+
+    def __init__(self, ids: torch.Tensor, values: torch.Tensor, rest: torch.Tensor | None = None, temperature: float = 1.0, weight: float = 1.0):
+        if not (ids.is_cuda and ids.dim() == 2 and ids.dtype == torch.int32 and values.dtype == torch.float32 and ids.shape == values.shape
+                and ids.device == values.device and (ids.shape[1] < 2 or ids.stride(1) == values.stride(1) == 1)):
+            _refuse("ids and values: need CUDA int32 and fp32 [T, k] with contiguous rows")
+        self.T, k = ids.shape
+        ld = [t.stride(0) if self.T > 1 else max(t.stride(0), k) for t in (ids, values)]
+        if ld[0] != ld[1]:
+            _refuse("ids and values: need one row stride")
+        self.gpu = ids.get_device()
+        _ints(rest, self.T, "rest", self.gpu, torch.float32)
+        self.keep = (ids, values, rest)
+        self.c = TeacherC(ids.data_ptr(), values.data_ptr(), _addr(rest), ld[0], k, temperature, weight)
         self.ref = C.pointer(self.c)
 
 

@@ -1367,6 +1367,12 @@ twist_status twist_ce_parts(twist_ctx *ctx, const float *parts, int blocks, floa
   return TWIST_OK;
 }
 
+twist_status twist_mean(twist_ctx *ctx, const float *v, int64_t n, float scale, float *out) {
+  hipLaunchKernelGGL(mean_kernel, dim3(1), dim3(kT), 0, ctx->stream, v, n, scale, out);
+  TW_HIP(ctx, hipGetLastError());
+  return TWIST_OK;
+}
+
 twist_status twist_mse_fwd_bwd(twist_ctx *ctx, int bf16, const float *x, const void *y, float *dx, void *dxb, float *partial, float *loss, int64_t n) {
   const int blocks = (int)std::min<int64_t>((n + kT - 1) / kT, 1024);
   LAUNCH_BF(mse_kernel, bf16, dim3(blocks), dim3(kT), x, y, dx, dxb, partial, n, 2.f / (float)n);

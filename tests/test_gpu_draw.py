@@ -1,0 +1,261 @@
+"""Drawing tokens from logits and taking the largest of them, each against the formula in 64 bits.
+
+What is drawn, kept or listed is compared as it is: whole numbers.  Floating results, with u = 2^-24:
+  logprobs  a rounding, and the quantum of the probabilities' sums: V 2^-(bits + 1) of the largest, bits of them as the header has it;
+  rest      m / tau, the logarithm and their sum: a rounding of each; the sum of exponentials is off, relative to itself, by u times
+            2 E[d] (the rounding of an exponent d against the largest, and of its division: E[d] <= ln V, since the entropy of the distribution is
+            ln sum + E[d] <= ln V), 4 (two steps of the exponential) and the additions in one chain (V / 256 + 16).
+"""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import synth_inputs as si
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+def _ctx(lib, V, dtype="f32", stream=None):
+    return lib.Context(lib.desc_from_cfg(si.ModelCfg(arch="llama", d_model=64, n_heads=1, d_head=64, d_ff=8, vocab=V, max_seq=1, act="swiglu", norm="rms", has_bias=False,
+                                                     tied_head=False, rope=True, dtype=dtype)), stream)
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _order(x):
+    """(columns, logits) of a row, largest first, equal ones by column; what holds no number counts as -infinity."""
+    x = np.where(np.isnan(x), -np.inf, x)
+    at = np.lexsort((np.arange(len(x)), -x))
+    return at, x[at]
+
+
+def _draw_want(x, u, temp=None, k=None, p=None, m=None):
+    """(token, logprob, kept) of one row in 64 bits."""
+    at, z = _order(x)
+    n = int((z > -np.inf).sum())
+    if n == 0:
+        return -1, -math.inf, 0
+    if temp is not None and not temp > 0:
+        return int(at[0]), 0.0, 1
+    with np.errstate(invalid="ignore"):
+        d = np.where(z[:n] == z[0], 0.0, z[:n] - z[0]) / (1.0 if temp is None else temp)
+    w = np.exp(np.where(np.isnan(d), -np.inf, d))
+    if k is not None and k > 0:
+        n = min(n, k)
+    if p is not None and p < 1:
+        s = np.cumsum(w[:n])
+        n = min(n, 1 + int((s[:-1] < p * s[-1]).sum()))
+    if m is not None and m > 0:
+        n = min(n, int((w[:n] >= min(m, 1.0)).sum()))
+    s = np.cumsum(w[:n])
+    j = min(int((s <= max(u if u == u else 0.0, 0.0) * s[-1]).sum()), int((w[:n] > 0).sum()) - 1)
+    return int(at[j]), float(d[j] - math.log(s[-1])), n
+
+
+def _check(ctx, lib, x, u, temperature=None, top_k=None, top_p=None, min_p=None, rows=None, **kw):
+    T, V = x.shape
+    rules = None if all(r is None for r in (temperature, top_k, top_p, min_p)) else lib.DrawRules(temperature, top_k, top_p, min_p)
+    tokens, logprobs, kept = ctx.twist_draw_raw(x, u, rules, **kw)
+    xs, us = x.double().cpu().numpy(), u.double().tolist()
+    of = [None if r is None else r.tolist() for r in (temperature, top_k, top_p, min_p)]
+    bits = max(42, min(51, 62 - math.ceil(math.log2(V))))
+    for t in range(T) if rows is None else rows:
+        token, logprob, n = _draw_want(xs[t], us[t], *(None if r is None else r[t] for r in of))
+        got = (int(tokens[t]), int(kept[t]))
+        assert got == (token, n), (t, got, (token, n), [None if r is None else r[t] for r in of], us[t])
+        lp = float(logprobs[t])
+        assert lp == logprob or abs(lp - logprob) <= U * abs(logprob) + V * 2.0 ** -(bits + 1) + 1e-12, (t, lp, logprob)
+    return tokens, logprobs, kept
+
+
+def _logits(g, T, V, kind="model"):
+    x = 2.0 * torch.randn((T, V), generator=g, device="cuda")
+    if kind == "model":
+        n = min(V, 40)
+        at = torch.randint(0, V // n, (T, n), generator=g, device="cuda") + torch.arange(n, device="cuda") * (V // n)
+        x.scatter_(1, at, 6.0 + 3.0 * torch.randn((T, n), generator=g, device="cuda"))
+    elif kind == "flat":
+        x *= 0.05
+    elif kind == "steps":                   # few different values
+        x = x.round()
+    elif kind == "masked":
+        x = torch.where(torch.rand((T, V), generator=g, device="cuda") < 0.03, x, -math.inf)
+    elif kind == "wide":
+        x = x * 40
+    return x
+
+
+def _rules(g, T, V, which):
+    r = lambda: torch.rand(T, generator=g, device="cuda")  # noqa: E731
+    pick = lambda *v: torch.tensor(v, device="cuda")[torch.randint(0, len(v), (T,), generator=g, device="cuda")]  # noqa: E731
+    return dict(temperature=pick(0.0, 0.1, 0.7, 1.0, 1.3, 5.0, -1.0) if "t" in which else None,
+                top_k=pick(0, 1, 2, 5, 50, 300, 1024, 1500, 5000, V - 1, V, V + 7, -4).to(torch.int32) if "k" in which else None,
+                top_p=pick(0.0, 0.05, 0.5, 0.9, 0.95, 0.999, 1.0, 1.5) if "p" in which else None,
+                min_p=torch.where(r() < 0.5, 10.0 ** (-6 * r()), pick(0.0, 1.0, 0.05, -1.0, 2.0)) if "m" in which else None)
+
+
+DTYPES = {"f32": (torch.float32, "f32"), "bf16": (torch.bfloat16, "bf16"), "f32_of_bf16": (torch.float32, "bf16")}
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 257, 1003, 4099, 16389, 32000, 50257, 65536, 70001, 131072])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_draw(lib, dtype, V):
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(V)
+    for i, kind in enumerate(("model", "flat", "steps", "masked", "wide")):
+        for which in ("", "k", "p", "m", "tkpm", "tkp"):
+            T = 7 if V < 40000 else 3
+            x = _logits(g, T, V, kind).to(dt)
+            _check(ctx, lib, x, torch.rand(T, generator=g, device="cuda"), **_rules(g, T, V, which))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [5, 1000, 9001, 66000])
+def test_draw_borders(lib, dtype, V):
+    """Random numbers at and beyond their ends, rows of one value, rows with one column or none to draw, infinities, columns that hold no number, zeros of both signs."""
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(3 + V)
+    u = torch.tensor([0.0, 1.0 - 2.0 ** -24, 1.0, 7.0, -1.0, math.nan, 2.0 ** -24, 0.5], device="cuda")
+    T = len(u)
+    rows = [torch.zeros((T, V)), torch.full((T, V), -math.inf), torch.full((T, V), math.nan), torch.full((T, V), -3e38), torch.full((T, V), math.inf),
+            torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0).expand(T, V)]
+    one = torch.full((T, V), -math.inf)
+    one[:, V // 2] = -100.0
+    some = _logits(g, T, V).cpu()
+    some[:, ::3] = math.nan
+    some[:, 1::3] = -math.inf
+    tops = _logits(g, T, V).cpu()
+    tops[:, [1, V - 1]] = math.inf
+    far = torch.full((T, V), -2000.0)       # the others are next to impossible
+    far[:, V - 1] = 0.0
+    for x in rows + [one, some, tops, far]:
+        x = x.to(dt).cuda().contiguous()
+        _check(ctx, lib, x, u)
+        for which in ("k", "p", "m", "tkpm"):
+            _check(ctx, lib, x, u, **_rules(g, T, V, which))
+        _check(ctx, lib, x, u, top_k=torch.full((T,), 3, dtype=torch.int32, device="cuda"), top_p=torch.full((T,), 0.5, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_draw_strides_and_places(lib, dtype):
+    """Rows at any distance from any element on; what lies between them is not read as theirs, results go where they are asked for."""
+    dt, model = DTYPES[dtype]
+    for V, pad, first in ((1003, 0, 1), (1003, 5, 0), (4100, 4, 3), (50257, 7, 2), (70003, 1, 5)):
+        ctx, g = _ctx(lib, V, model), _gen(V + pad)
+        T = 4
+        whole = torch.full((T * (V + pad) + first + 3,), math.inf, dtype=dt, device="cuda")
+        x = whole[first: first + T * (V + pad)].view(T, V + pad)[:, :V]
+        x.copy_(_logits(g, T, V))
+        out = [torch.full((T + 2,), -7, dtype=d, device="cuda") for d in (torch.int32, torch.float32, torch.int32)]
+        got = _check(ctx, lib, x, torch.rand(T, generator=g, device="cuda"), **_rules(g, T, V, "kp"), tokens=out[0][1:-1], logprobs=out[1][1:-1], kept=out[2][1:-1])
+        assert all((o[[0, -1]] == -7).all() and (o[1:-1] == r).all() for o, r in zip(out, got))
+
+
+def test_draw_many_rows(lib):
+    V, T = 300, 5000
+    ctx, g = _ctx(lib, V), _gen(9)
+    x = _logits(g, T, V)
+    rules = _rules(g, T, V, "tkpm")
+    first = _check(ctx, lib, x, torch.rand(T, generator=g, device="cuda"), rows=range(0, T, 97), **rules)
+    assert ((first[0] >= 0) & (first[0] < V)).all()
+
+
+def test_draws_follow_the_distribution(lib):
+    """Evenly spaced random numbers draw every column as often as its probability says, but for one at each of its two ends."""
+    V, T = 50, 8192
+    ctx, g = _ctx(lib, V), _gen(1)
+    x = torch.randn((1, V), generator=g, device="cuda")
+    tokens, _, kept = ctx.twist_draw_raw(x.expand(T, V).contiguous(), (torch.arange(T, device="cuda") + 0.5) / T)
+    n = torch.bincount(tokens.long(), minlength=V).double()
+    assert (n - T * torch.softmax(x[0].double(), 0)).abs().max() <= 1.0 + 1e-6 and (kept == V).all()
+
+
+def test_draw_refuses_what_does_not_fit(lib):
+    V, T = 100, 4
+    ctx = _ctx(lib, V, "bf16")
+    x, u = torch.zeros((T, V), dtype=torch.bfloat16, device="cuda"), torch.zeros(T, device="cuda")
+    i32 = torch.zeros(T, dtype=torch.int32, device="cuda")
+    bad = [lambda: ctx.twist_draw_raw(x.half(), u), lambda: ctx.twist_draw_raw(x[:, :99], u), lambda: ctx.twist_draw_raw(x.cpu(), u), lambda: ctx.twist_draw_raw(x.t().contiguous().t(), u),
+           lambda: ctx.twist_draw_raw(x, u[:3]), lambda: ctx.twist_draw_raw(x, u.double()), lambda: ctx.twist_draw_raw(x, u.cpu()), lambda: ctx.twist_draw_raw(x, None),
+           lambda: ctx.twist_draw_raw(x, u, lib.DrawRules(top_p=u[:3].clone())), lambda: ctx.twist_draw_raw(x, u, tokens=i32[:3]), lambda: ctx.twist_draw_raw(x, u, tokens=u),
+           lambda: ctx.twist_draw_raw(x, u, kept=torch.zeros(2 * T, dtype=torch.int32, device="cuda")[::2]), lambda: lib.DrawRules(top_k=u), lambda: lib.DrawRules(top_p=i32),
+           lambda: lib.DrawRules(temperature=u, top_p=u[:2].clone()), lambda: ctx.twist_top_logits_raw(x, 0), lambda: ctx.twist_top_logits_raw(x, 1025),
+           lambda: ctx.twist_top_logits_raw(x, 5, temperature=0.0), lambda: ctx.twist_top_logits_raw(x, 5, ids=torch.zeros((T, 6), dtype=torch.int32, device="cuda")),
+           lambda: ctx.twist_top_logits_raw(x, 5, ids=torch.zeros((T, 6), dtype=torch.int32, device="cuda")[:, :5]),
+           lambda: ctx.twist_top_logits_raw(x, 5, rest=i32)]
+    for call in bad:
+        with pytest.raises(lib.TwistError):
+            call()
+
+
+# ------------------------------------------------------------------------------------------------ the largest logits
+def _check_top(ctx, x, k, tau=1.0, rows=None, **kw):
+    T, V = x.shape
+    ids, values, rest = ctx.twist_top_logits_raw(x, k, temperature=tau, **kw)
+    xs, tau = x.double().cpu().numpy(), float(np.float32(tau))
+    ids_, values_, rest_ = ids.cpu().numpy(), values.double().cpu().numpy(), rest.double().cpu().numpy()
+    n = min(k, V)
+    for t in range(T) if rows is None else rows:
+        at, z = _order(xs[t])
+        assert (ids_[t, :n] == at[:n]).all() and (values_[t, :n] == z[:n]).all(), t
+        assert (ids_[t, n:] == -1).all() and (values_[t, n:] == -np.inf).all()
+        m = z[n] if n < V else -np.inf
+        if not np.isfinite(m):
+            assert rest_[t] == m, (t, rest_[t], m)
+            continue
+        want = m / tau + math.log(np.exp((z[n:] - m) / tau).sum())
+        off = U * (2 * math.log(V) + 4 + V / 256 + 16 + 2 * abs(m / tau) + 2 * abs(want - m / tau) + abs(want))
+        assert abs(rest_[t] - want) <= off, (t, rest_[t], want, off)
+    return ids, values, rest
+
+
+@pytest.mark.parametrize("V", [1, 3, 65, 1003, 4099, 16389, 32000, 50257, 65536, 70001, 131072])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_top_logits(lib, dtype, V):
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(V + 1)
+    for kind in ("model", "flat", "steps", "masked", "wide"):
+        for k, tau in ((1, 1.0), (17, 2.0), (64, 0.5), (200, 1.0), (1000, 3.3), (1024, 1.0)):
+            _check_top(ctx, _logits(g, 3, V, kind).to(dt), k, tau)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [5, 1000, 9001, 66000])
+def test_top_logits_borders(lib, dtype, V):
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(5)
+    some = _logits(g, 2, V).cpu()
+    some[:, ::2] = math.nan
+    tops = _logits(g, 2, V).cpu()
+    tops[:, [0, V // 2, V - 1]] = math.inf
+    zeros = torch.where(torch.arange(V) % 2 == 0, 0.0, -0.0).expand(2, V)
+    far = torch.full((2, V), -3e38)
+    far[:, V // 3] = 3e38
+    for x in (torch.zeros((2, V)), torch.full((2, V), -math.inf), torch.full((2, V), math.nan), some, tops, zeros, far, torch.arange(2 * V).view(2, V).float()):
+        for k in (1, 2, 40, 1024):
+            _check_top(ctx, x.to(dt).cuda().contiguous(), k)
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_top_logits_strides_and_places(lib, dtype):
+    dt, model = DTYPES[dtype]
+    for V, pad, first, k in ((1003, 0, 1, 30), (1003, 5, 0, 7), (4100, 4, 3, 100), (50257, 7, 2, 20), (70003, 1, 5, 20)):
+        ctx, g = _ctx(lib, V, model), _gen(V + pad)
+        T = 4
+        whole = torch.full((T * (V + pad) + first + 3,), math.inf, dtype=dt, device="cuda")
+        x = whole[first: first + T * (V + pad)].view(T, V + pad)[:, :V]
+        x.copy_(_logits(g, T, V))
+        ids, values = (torch.full((T, k + 3), -7, dtype=d, device="cuda") for d in (torch.int32, torch.float32))
+        _check_top(ctx, x, k, ids=ids[:, 1: k + 1], values=values[:, 1: k + 1])
+        assert all((o[:, 0] == -7).all() and (o[:, k + 1:] == -7).all() for o in (ids, values))
+
+
+def test_top_logits_many_rows(lib):
+    V, T = 1003, 3000
+    ctx, g = _ctx(lib, V, "bf16"), _gen(2)
+    _check_top(ctx, _logits(g, T, V).bfloat16(), 12, rows=range(0, T, 61))
