@@ -3,32 +3,84 @@
 
 namespace {
 
-constexpr int kT = 256;
 constexpr int kTop = 1024;  // the longest list
+constexpr float kLog2e = 1.44269504f;
 
-template <int BF> __device__ __forceinline__ float load1(const void *p, int64_t i) {
-  return BF ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16) : static_cast<const float *>(p)[i];
+typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+
+// Sixteen bytes of a row, from any element on, as floats: eight of bf16, four of fp32.
+template <int BF> struct Piece {
+  static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
+  u32x4v u;
+  __device__ __forceinline__ void load(const char *row, int v, int V) {
+    if ((v + 1) * N <= V) __builtin_memcpy(&u, row + (int64_t)v * 16, 16);
+    else {
+      u = none();
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (v * N + e >= V) continue;
+        if (BF) u[e / 2] = (u[e / 2] & (e % 2 ? 0xffffu : 0xffff0000u)) | (uint32_t) reinterpret_cast<const uint16_t *>(row)[v * N + e] << (e % 2 * 16);
+        else u[e % 4] = reinterpret_cast<const uint32_t *>(row)[v * N + e];
+      }
+    }
+  }
+  static __device__ __forceinline__ u32x4v none() {  // -infinity throughout
+    const uint32_t n = BF ? 0xff80ff80u : 0xff800000u;
+    return u32x4v{n, n, n, n};
+  }
+  __device__ __forceinline__ float operator[](int e) const {
+    if (!BF) return __uint_as_float(u[e % 4]);
+    return __uint_as_float(e % 2 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+  }
+  __device__ __forceinline__ void clear(uint32_t bits) {  // -infinity where a bit is set
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (bits >> e & 1) {
+        if (BF) u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | 0xff800000u : (u[e / 2] & 0xffff0000u) | 0xff80u;
+        else u[e % 4] = 0xff800000u;
+      }
+  }
+};
+template <int BF> __device__ __forceinline__ float load1(const char *row, int c) {
+  return BF ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[c] << 16) : reinterpret_cast<const float *>(row)[c];
 }
-template <int BF> __device__ __forceinline__ void store1(void *p, int64_t i, float v) {
-  if (BF) static_cast<__bf16 *>(p)[i] = (__bf16)v;  // round to nearest even
-  else static_cast<float *>(p)[i] = v;
+template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, float v) {
+  if (BF) reinterpret_cast<__bf16 *>(row)[c] = (__bf16)v;  // round to nearest even
+  else reinterpret_cast<float *>(row)[c] = v;
+}
+template <int BF> __device__ __forceinline__ void store_piece(char *row, int v, int V, const float *g) {
+  constexpr int N = Piece<BF>::N;
+  if ((v + 1) * N <= V) {
+    u32x4v u;
+    if (BF) {
+      typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+      typedef float f2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f2 p = {g[2 * i % N], g[(2 * i + 1) % N]};
+        u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, b2));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(g[i]);
+    }
+    __builtin_memcpy(row + (int64_t)v * 16, &u, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (v * N + e < V) store1<BF>(row, v * N + e, g[e]);
+  }
 }
 
-template <class T> __device__ __forceinline__ T block_add(T v, T *sh) {
+template <class T> __device__ __forceinline__ T wave_add(T v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
+  return v;
 }
-__device__ __forceinline__ float block_max(float v, float *sh) {
+__device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return fmaxf(fmaxf(sh[0], sh[1]), fmaxf(sh[2], sh[3]));
+  return v;
 }
 
 // Natural logarithm of a / (a + b), near 1 as exact as far from it.
@@ -36,123 +88,220 @@ __device__ __forceinline__ double log_share(double a, double b) { return b < a ?
 
 // A row a workgroup.  The row's tokens are the teacher's (the set) and the others, whose share of the distribution is formed from themselves and not as what the set leaves: it may be
 // next to nothing, or all but everything.  With tau the temperature, p and q over the set and over the others together (P, Q of them), the gradient of
-// KL(q || p) is (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.  WORDS: 32 tokens each, of the table of which are in the set.
-template <int BF, int WORDS>
-__global__ __launch_bounds__(kT) void distill_kernel(const void *x, int64_t ld, const int32_t *targets, int V, twist_teacher te, void *grad, int64_t ldg, int64_t pad, float inv_T,
+// KL(q || p) is (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.
+// Bound by memory: the row is read once and its gradient written once.  It stays in registers as it came (NV pieces of 16 bytes a thread; rows that NT threads cannot hold, NV = 0, are read
+// three times), the set's columns as -infinity, so that they weigh nothing in the others' sums; their own gradients, a thread each and in 64 bits where they meet a logarithm, are stored over
+// the others' behind a barrier.
+template <int BF, int NT, int NV>
+__global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int64_t ld, const int32_t *targets, int V, twist_teacher te, char *grads, int64_t ldg, int64_t pad, float inv_T,
                                                      float *rowloss) {
-  __shared__ uint32_t in_set[WORDS];
+  using P16 = Piece<BF>;
+  constexpr int N = P16::N, NW = NT / 64, WORDS = NV ? NV * NT * N / 32 : 1 << 15;
+  __shared__ uint32_t in_set[WORDS];  // a bit a column
   __shared__ int32_t id[kTop];
   __shared__ float logit[kTop];
   __shared__ double weight[kTop];
-  __shared__ double shd[4];
-  __shared__ float shf[4];
+  __shared__ float most[3][NW], sums[2][NW];
+  __shared__ double set_sums[3][NW], kls[NW];
   __shared__ int twice;
-  const int t = blockIdx.x, tid = threadIdx.x, k = te.k;
-  const int64_t row = t * ld, out = t * ldg;
+  const int t = blockIdx.x, tid = threadIdx.x, k = te.k, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const char *row = logits + (int64_t)t * ld * P16::ES;
+  char *out = grads + (int64_t)t * ldg * P16::ES;
   const float tau = te.temperature, inv_tau = 1.f / tau;
-  for (int i = tid; i < (V + 31) / 32; i += kT) in_set[i] = 0;
+  const int pieces = (V + N - 1) / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
+  P16 x[NV ? NV : 1];
+#pragma unroll
+  for (int u = 0; u < NV; ++u) {
+    x[u].u = P16::none();
+    if (u * NT < mine && u * NT + tid < pieces) x[u].load(row, u * NT + tid, V);
+  }
+  const int tgt = te.weight < 1.f ? targets[t] : -1;
+  const bool aimed = (unsigned)tgt < (unsigned)V;
+  const float rest = te.rest ? te.rest[t] : -INFINITY, aim = aimed ? load1<BF>(row, tgt) : 0.f;
+  for (int i = tid; i < (V + 31) / 32; i += NT) in_set[i] = 0;
   if (tid == 0) twice = 0;
   __syncthreads();
-  float mt = te.rest ? te.rest[t] : -INFINITY;
-  const float rest = mt;
-  float mine = -INFINITY, other = -INFINITY;  // largest logits of the set and of the others
-  for (int j = tid; j < k; j += kT) {
+  float top_t = rest, top_set = -INFINITY;  // largest of the teacher's, and of the student's in the set
+  for (int j = tid; j < k; j += NT) {
     const int c = te.ids[t * te.ld + j];
     const bool on = (unsigned)c < (unsigned)V;
     id[j] = on ? c : -1;
     if (!on) continue;
     if (atomicOr(&in_set[c / 32], 1u << (c & 31)) >> (c & 31) & 1) twice = 1;
-    logit[j] = load1<BF>(x, row + c);
-    mine = fmaxf(mine, logit[j]);
-    mt = fmaxf(mt, te.values[t * te.ld + j] * inv_tau);
+    logit[j] = load1<BF>(row, c);
+    top_set = fmaxf(top_set, logit[j]);
+    top_t = fmaxf(top_t, te.values[t * te.ld + j] * inv_tau);
   }
-  mt = block_max(mt, shf);
-  const int tgt = te.weight < 1.f ? targets[t] : -1;
-  const bool taught = te.weight > 0.f && mt > -INFINITY, aimed = (unsigned)tgt < (unsigned)V;
+  top_t = wave_max(top_t);
+  top_set = wave_max(top_set);
+  if (lane == 0) { most[0][wave] = top_t; most[1][wave] = top_set; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) { top_t = fmaxf(top_t, most[0][w]); top_set = fmaxf(top_set, most[1][w]); }
+  const bool taught = te.weight > 0.f && top_t > -INFINITY;
   if (!taught && !aimed) {
-    for (int c = tid; c < pad; c += kT) store1<BF>(grad, out + c, 0.f);
+    const float zeros[N] = {};
+    for (int v = tid; v < pieces; v += NT) store_piece<BF>(out, v, V, zeros);
+    for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
     if (tid == 0) rowloss[t] = 0.f;
     return;
   }
+  auto bits_of = [&](int v) {  // of a piece's columns in the set
+    const uint32_t b = reinterpret_cast<const uint8_t *>(in_set)[N == 8 ? v : v / 2];
+    return N == 8 ? b : b >> (v % 2 * 4) & 15u;
+  };
+  // f(piece, its number) for all of the thread's pieces of the row, the set's columns -infinity
+  auto each = [&](auto f) {
+    if (NV) {
+#pragma unroll
+      for (int u = 0; u < NV; ++u)
+        if (u * NT < mine) f(x[u], u * NT + tid);
+    } else {
+      for (int v = tid; v < pieces; v += NT) {
+        P16 y;
+        y.load(row, v, V);
+        y.clear(bits_of(v));
+        f(y, v);
+      }
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < NV; ++u)
+    if (u * NT < mine) {
+      const uint32_t b = bits_of(u * NT + tid);
+      if (b) x[u].clear(b);
+    }
+  float other = -INFINITY;
+  each([&](const P16 &y, int) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) other = fmaxf(other, y[e]);
+  });
+  other = wave_max(other);
+  if (lane == 0) most[2][wave] = other;
   // the teacher's weights against its largest; of a token that is named twice the first entry takes the others'
-  for (int j = tid; j < k; j += kT)
-    if (id[j] >= 0) weight[j] = taught ? exp((double)te.values[t * te.ld + j] / tau - (double)mt) : 0.0;
-  const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - (double)mt) : 0.0;
+  for (int j = tid; j < k; j += NT)
+    if (id[j] >= 0) weight[j] = taught ? exp((double)te.values[t * te.ld + j] / tau - (double)top_t) : 0.0;
+  const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - (double)top_t) : 0.0;
   __syncthreads();
+#pragma unroll
+  for (int w = 0; w < NW; ++w) other = fmaxf(other, most[2][w]);
   if (twice) {
-    double sum[kTop / kT];
-    bool first[kTop / kT];
-    for (int j = tid, u = 0; j < k; j += kT, ++u) {
+    constexpr int M = (kTop + NT - 1) / NT;
+    double sum[M];
+    bool first[M];
+#pragma unroll
+    for (int u = 0; u < M; ++u) {
+      const int j = u * NT + tid;
       sum[u] = 0.0;
-      first[u] = id[j] >= 0;
-      for (int i = 0; i < k; ++i)
-        if (id[i] == id[j]) {
-          sum[u] += weight[i];
-          first[u] = first[u] && i >= j;
-        }
+      first[u] = j < k && id[j] >= 0;
+      if (first[u])
+        for (int i = 0; i < k; ++i)
+          if (id[i] == id[j]) {
+            sum[u] += weight[i];
+            first[u] = first[u] && i >= j;
+          }
     }
     __syncthreads();
-    for (int j = tid, u = 0; j < k; j += kT, ++u) {
-      if (!first[u]) id[j] = -1;
-      else weight[j] = sum[u];
+#pragma unroll
+    for (int u = 0; u < M; ++u) {
+      const int j = u * NT + tid;
+      if (j < k && !first[u]) id[j] = -1;
+      else if (j < k) weight[j] = sum[u];
     }
   }
-  auto outside = [&](int c) { return !(in_set[c / 32] >> (c & 31) & 1); };
-  for (int c = tid; c < V; c += kT) other = fmaxf(other, outside(c) ? load1<BF>(x, row + c) : -INFINITY);
-  mine = block_max(mine, shf);
-  other = block_max(other, shf);
-  const float m = fmaxf(mine, other);
+  const float ref = other > -INFINITY ? other : 0.f, m = fmaxf(top_set, other);
+  // sums over the others against their largest, and over the set against the row's
+  const float c1 = kLog2e, ct = kLog2e * inv_tau;
   float s1 = 0.f, st = 0.f;
-  for (int c = tid; c < V; c += kT)
-    if (outside(c) && other > -INFINITY) {
-      const float d = load1<BF>(x, row + c) - other;
-      s1 += __expf(d);
-      st += __expf(d * inv_tau);
+  each([&](const P16 &y, int) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float d = y[e] - ref;
+      if (aimed) s1 += __builtin_amdgcn_exp2f(d * c1);
+      if (taught) st += __builtin_amdgcn_exp2f(d * ct);
     }
-  // sums over the others, brought to the row's largest, and over the set
-  const double down = other > -INFINITY ? (double)other - m : 0.0;
-  const double others1 = block_add((double)s1, shd) * exp(down), others = block_add((double)st, shd), others_m = others * exp(down / tau);
+  });
   double set1 = 0.0, set = 0.0, qs = 0.0;
-  for (int j = tid; j < k; j += kT)
+  for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
       const double d = (double)logit[j] - m;
       set1 += exp(d);
       set += exp(d / tau);
       qs += weight[j];
     }
-  set1 = block_add(set1, shd);
-  set = block_add(set, shd);
-  qs = block_add(qs, shd);
-  const double z1 = others1 + set1, z = others_m + set, zq = qs + rest_weight;
-  const double log_z = log(z), log_zq = log(zq);
-  const double log_others = others_m > 0.0 ? log_share(others_m, set) : down / tau + (others > 0.0 ? log(others) : -INFINITY) - log_z;
-  double kl = 0.0;
-  if (taught)
-    for (int j = tid; j < k; j += kT)
-      if (id[j] >= 0 && weight[j] != 0.0) kl += weight[j] / zq * ((log(weight[j]) - log_zq) - (((double)logit[j] - m) / tau - log_z));
-  kl = block_add(kl, shd);
+  s1 = wave_add(s1);
+  st = wave_add(st);
+  if (64 * wave < k) { set1 = wave_add(set1); set = wave_add(set); qs = wave_add(qs); }
+  if (lane == 0) {
+    sums[0][wave] = s1; sums[1][wave] = st;
+    set_sums[0][wave] = set1; set_sums[1][wave] = set; set_sums[2][wave] = qs;
+  }
+  __syncthreads();
+  double others1 = 0.0, others = 0.0;
+  set1 = set = qs = 0.0;
+#pragma unroll
+  for (int w = 0; w < NW; ++w) {
+    others1 += sums[0][w]; others += sums[1][w];
+    set1 += set_sums[0][w]; set += set_sums[1][w]; qs += set_sums[2][w];
+  }
+  const double down = other > -INFINITY ? (double)other - m : 0.0, others_m = others * exp(down / tau);
+  const double z1 = others1 * exp(down) + set1, z = others_m + set, zq = qs + rest_weight;
   const double Q = taught ? rest_weight / zq : 0.0, P = others_m / z;
-  if (rest_weight != 0.0) kl += Q * (log_share(rest_weight, qs) - log_others);
   // the others' gradient is their share of each other times P - Q, which is what the set's probabilities differ by
   const double more = Q < 0.5 ? P - Q : qs / zq - set / z;
-  const float a1 = aimed ? (float)((1.0 - (double)te.weight) / z1 * inv_T) : 0.f, at = taught && others > 0.0 ? (float)((double)te.weight * tau * more / others * inv_T) : 0.f;
-  for (int c = tid; c < V; c += kT) {
-    const float v = load1<BF>(x, row + c);
-    float g = at != 0.f ? __expf((v - other) * inv_tau) * at : 0.f;
-    if (aimed) g += __expf(v - m) * a1 - (c == tgt ? (1.f - te.weight) * inv_T : 0.f);
-    if (c == tgt && tid == c % kT) rowloss[t] = (float)((double)te.weight * tau * tau * kl + (1.0 - (double)te.weight) * (log(z1) - ((double)v - m)));
-    store1<BF>(grad, out + c, g);
+  const float a1 = aimed ? (float)((1.0 - (double)te.weight) * exp(down) / z1 * inv_T) : 0.f, at = taught && others > 0.0 ? (float)((double)te.weight * tau * more / others * inv_T) : 0.f;
+  each([&](const P16 &y, int v) {
+    float g[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      const float d = y[e] - ref;
+      g[e] = 0.f;
+      if (aimed) g[e] = __builtin_amdgcn_exp2f(d * c1) * a1;
+      if (taught) g[e] = fmaf(__builtin_amdgcn_exp2f(d * ct), at, g[e]);
+    }
+    if (v < pieces) store_piece<BF>(out, v, V, g);
+  });
+  for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
+  // the row's loss
+  double kl = 0.0;
+  if (taught && 64 * wave < k) {
+    const double log_z = log(z), log_zq = log(zq);
+    for (int j = tid; j < k; j += NT)
+      if (id[j] >= 0 && weight[j] != 0.0) kl += weight[j] / zq * ((log(weight[j]) - log_zq) - (((double)logit[j] - m) / tau - log_z));
+    kl = wave_add(kl);
   }
-  for (int64_t c = V + tid; c < pad; c += kT) store1<BF>(grad, out + c, 0.f);
-  if (!aimed && tid == 0) rowloss[t] = (float)((double)te.weight * tau * tau * kl);
-  __syncthreads();  // (the set's gradients take the places of what was written above)
-  for (int j = tid; j < k; j += kT)
+  if (lane == 0) kls[wave] = kl;
+  __syncthreads();  // (the set's gradients take the places of what was written above, and so does the target's)
+  const double wt = (double)te.weight * tau;
+  for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
       const double d = (double)logit[j] - m;
-      double g = taught ? (double)te.weight * tau * (exp(d / tau) / z - weight[j] / zq) : 0.0;
+      double g = taught ? wt * (exp(d / tau) / z - weight[j] / zq) : 0.0;
       if (aimed) g += (1.0 - (double)te.weight) * (exp(d) / z1 - (id[j] == tgt ? 1.0 : 0.0));
-      store1<BF>(grad, out + id[j], (float)(g * inv_T));
+      store1<BF>(out, id[j], (float)(g * inv_T));
     }
+  if (tid == 0) {
+    double loss = 0.0;
+    if (aimed) {
+      loss = (1.0 - (double)te.weight) * (log(z1) - ((double)aim - m));
+      if (!(in_set[tgt / 32] >> (tgt & 31) & 1)) {
+        const float d = aim - ref;
+        float g = fmaf(__builtin_amdgcn_exp2f(d * c1), a1, -(1.f - te.weight) * inv_T);
+        if (taught) g = fmaf(__builtin_amdgcn_exp2f(d * ct), at, g);
+        store1<BF>(out, tgt, g);
+      }
+    }
+    if (taught) {
+      kl = 0.0;
+      for (int w = 0; w < NW; ++w) kl += kls[w];
+      if (rest_weight != 0.0) {
+        const double log_others = others_m > 0.0 ? log_share(others_m, set) : down / tau + (others > 0.0 ? log(others) : -INFINITY) - log(z);
+        kl += Q * (log_share(rest_weight, qs) - log_others);
+      }
+      loss += wt * tau * kl;
+    }
+    rowloss[t] = (float)loss;
+  }
 }
 
 }  // namespace
@@ -174,10 +323,21 @@ twist_status twist_distill(twist_ctx *ctx, const char *who, int bf16, const void
                            int64_t pad, float *rowloss, float *loss) {
   TW_TRY(twist_check_teacher(ctx, who, te, T, V));
   const float inv_T = 1.f / (float)T;
-#define DISTILL(BF, WORDS) \
-  hipLaunchKernelGGL((distill_kernel<BF, WORDS>), dim3(T), dim3(kT), 0, ctx->stream, logits, ld, targets, V, *te, grad, ldg, pad, inv_T, rowloss)
-  if (V <= 1 << 16) { if (bf16) DISTILL(1, 1 << 11); else DISTILL(0, 1 << 11); }
-  else { if (bf16) DISTILL(1, 1 << 15); else DISTILL(0, 1 << 15); }
+  const char *x = static_cast<const char *>(logits);
+  char *g = static_cast<char *>(grad);
+#define DISTILL(BF, NT, NV) hipLaunchKernelGGL((distill_kernel<BF, NT, NV>), dim3(T), dim3(NT), 0, ctx->stream, x, ld, targets, V, *te, g, ldg, pad, inv_T, rowloss)
+  if (bf16) {
+    if (V <= 4 * 8 * 256) DISTILL(1, 256, 4);
+    else if (V <= 16 * 8 * 256) DISTILL(1, 256, 16);
+    else if (V <= 16 * 8 * 512) DISTILL(1, 512, 16);
+    else DISTILL(1, 1024, 0);
+  } else {
+    if (V <= 4 * 4 * 256) DISTILL(0, 256, 4);
+    else if (V <= 16 * 4 * 256) DISTILL(0, 256, 16);
+    else if (V <= 16 * 4 * 512) DISTILL(0, 512, 16);
+    else if (V <= 16 * 4 * 1024) DISTILL(0, 1024, 16);
+    else DISTILL(0, 1024, 0);
+  }
 #undef DISTILL
   return twist_mean(ctx, rowloss, T, inv_T, loss);
 }
