@@ -8,22 +8,11 @@ constexpr float kLog2e = 1.44269504f;
 
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
-// Sixteen bytes of a row, from any element on, as floats: eight of bf16, four of fp32.
+// Sixteen bytes of a row, from any element on, as floats: eight of bf16, four of fp32.  (Rows of an odd vocabulary start anywhere; loads and stores need no alignment.)
 template <int BF> struct Piece {
   static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
   u32x4v u;
-  __device__ __forceinline__ void load(const char *row, int v, int V) {
-    if ((v + 1) * N <= V) __builtin_memcpy(&u, row + (int64_t)v * 16, 16);
-    else {
-      u = none();
-#pragma unroll
-      for (int e = 0; e < N; ++e) {
-        if (v * N + e >= V) continue;
-        if (BF) u[e / 2] = (u[e / 2] & (e % 2 ? 0xffffu : 0xffff0000u)) | (uint32_t) reinterpret_cast<const uint16_t *>(row)[v * N + e] << (e % 2 * 16);
-        else u[e % 4] = reinterpret_cast<const uint32_t *>(row)[v * N + e];
-      }
-    }
-  }
+  __device__ __forceinline__ void load(const char *row, int v) { __builtin_memcpy(&u, row + (int64_t)v * 16, 16); }
   static __device__ __forceinline__ u32x4v none() {  // -infinity throughout
     const uint32_t n = BF ? 0xff80ff80u : 0xff800000u;
     return u32x4v{n, n, n, n};
@@ -48,28 +37,16 @@ template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, f
   if (BF) reinterpret_cast<__bf16 *>(row)[c] = (__bf16)v;  // round to nearest even
   else reinterpret_cast<float *>(row)[c] = v;
 }
-template <int BF> __device__ __forceinline__ void store_piece(char *row, int v, int V, const float *g) {
-  constexpr int N = Piece<BF>::N;
-  if ((v + 1) * N <= V) {
-    u32x4v u;
-    if (BF) {
-      typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-      typedef float f2 __attribute__((ext_vector_type(2)));
+template <int BF> __device__ __forceinline__ void store_piece(char *row, int v, const float *g) {
+  u32x4v u;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const f2 p = {g[2 * i % N], g[(2 * i + 1) % N]};
-        u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(p, b2));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) u[i] = __float_as_uint(g[i]);
-    }
-    __builtin_memcpy(row + (int64_t)v * 16, &u, 16);
-  } else {
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (v * N + e < V) store1<BF>(row, v * N + e, g[e]);
+  for (int i = 0; i < 4; ++i) {
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    if (BF) u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{g[2 * i % Piece<BF>::N], g[(2 * i + 1) % Piece<BF>::N]}), b2));
+    else u[i] = __float_as_uint(g[i]);
   }
+  __builtin_memcpy(row + (int64_t)v * 16, &u, 16);
 }
 
 template <class T> __device__ __forceinline__ T wave_add(T v) {
@@ -81,6 +58,14 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
   return v;
+}
+
+// exp(x) in 32 bits: the exponent's rounding, which a large one would multiply, taken care of
+__device__ __forceinline__ float exp_f32(double x) {
+  const double y = x * 1.4426950408889634;
+  if (y <= -200.0) return 0.f;
+  const float h = (float)y;
+  return __builtin_amdgcn_exp2f(h) * fmaf((float)(y - h), 0.69314718f, 1.f);
 }
 
 // Natural logarithm of a / (a + b), near 1 as exact as far from it.
@@ -100,21 +85,23 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   __shared__ uint32_t in_set[WORDS];  // a bit a column
   __shared__ int32_t id[kTop];
   __shared__ float logit[kTop];
-  __shared__ double weight[kTop];
+  __shared__ double weight[kTop], part[kTop];  // the teacher's weights against its largest, and their exponents
   __shared__ float most[3][NW], sums[2][NW];
   __shared__ double set_sums[3][NW], kls[NW];
   __shared__ int twice;
   const int t = blockIdx.x, tid = threadIdx.x, k = te.k, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const char *row = logits + (int64_t)t * ld * P16::ES;
   char *out = grads + (int64_t)t * ldg * P16::ES;
-  const float tau = te.temperature, inv_tau = 1.f / tau;
-  const int pieces = (V + N - 1) / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
+  const double tau = te.temperature, inv_tau = 1.0 / tau;
+  const int pieces = V / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
+  const int last = pieces * N + tid;                    // the row's last columns, fewer than a piece, a thread each
   P16 x[NV ? NV : 1];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     x[u].u = P16::none();
-    if (u * NT < mine && u * NT + tid < pieces) x[u].load(row, u * NT + tid, V);
+    if (u * NT + tid < pieces) x[u].load(row, u * NT + tid);
   }
+  float xl = last < V ? load1<BF>(row, last) : -INFINITY;
   const int tgt = te.weight < 1.f ? targets[t] : -1;
   const bool aimed = (unsigned)tgt < (unsigned)V;
   const float rest = te.rest ? te.rest[t] : -INFINITY, aim = aimed ? load1<BF>(row, tgt) : 0.f;
@@ -130,7 +117,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     if (atomicOr(&in_set[c / 32], 1u << (c & 31)) >> (c & 31) & 1) twice = 1;
     logit[j] = load1<BF>(row, c);
     top_set = fmaxf(top_set, logit[j]);
-    top_t = fmaxf(top_t, te.values[t * te.ld + j] * inv_tau);
+    top_t = fmaxf(top_t, (float)(te.values[t * te.ld + j] * inv_tau));
   }
   top_t = wave_max(top_t);
   top_set = wave_max(top_set);
@@ -141,8 +128,8 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   const bool taught = te.weight > 0.f && top_t > -INFINITY;
   if (!taught && !aimed) {
     const float zeros[N] = {};
-    for (int v = tid; v < pieces; v += NT) store_piece<BF>(out, v, V, zeros);
-    for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
+    for (int v = tid; v < pieces; v += NT) store_piece<BF>(out, v, zeros);
+    for (int64_t c = last; c < pad; c += NT) store1<BF>(out, c, 0.f);
     if (tid == 0) rowloss[t] = 0.f;
     return;
   }
@@ -150,16 +137,21 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     const uint32_t b = reinterpret_cast<const uint8_t *>(in_set)[N == 8 ? v : v / 2];
     return N == 8 ? b : b >> (v % 2 * 4) & 15u;
   };
-  // f(piece, its number) for all of the thread's pieces of the row, the set's columns -infinity
+  // f(piece, its number) for all of the thread's pieces of the row, those beyond it and the set's columns -infinity
   auto each = [&](auto f) {
     if (NV) {
+      int at = tid;
+      asm volatile("" : "+v"(at));  // (neither places nor what one pass makes of the pieces are kept for the next: registers)
 #pragma unroll
       for (int u = 0; u < NV; ++u)
-        if (u * NT < mine) f(x[u], u * NT + tid);
+        if (u * NT < mine) {
+          asm volatile("" : "+v"(x[u].u));
+          f(x[u], u * NT + at);
+        }
     } else {
       for (int v = tid; v < pieces; v += NT) {
         P16 y;
-        y.load(row, v, V);
+        y.load(row, v);
         y.clear(bits_of(v));
         f(y, v);
       }
@@ -171,7 +163,8 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
       const uint32_t b = bits_of(u * NT + tid);
       if (b) x[u].clear(b);
     }
-  float other = -INFINITY;
+  if (last < V && in_set[last / 32] >> (last & 31) & 1) xl = -INFINITY;
+  float other = xl;
   each([&](const P16 &y, int) {
 #pragma unroll
     for (int e = 0; e < N; ++e) other = fmaxf(other, y[e]);
@@ -180,7 +173,10 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   if (lane == 0) most[2][wave] = other;
   // the teacher's weights against its largest; of a token that is named twice the first entry takes the others'
   for (int j = tid; j < k; j += NT)
-    if (id[j] >= 0) weight[j] = taught ? exp((double)te.values[t * te.ld + j] / tau - (double)top_t) : 0.0;
+    if (id[j] >= 0) {
+      part[j] = te.values[t * te.ld + j] * inv_tau - top_t;
+      weight[j] = taught ? exp(part[j]) : 0.0;
+    }
   const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - (double)top_t) : 0.0;
   __syncthreads();
 #pragma unroll
@@ -206,13 +202,16 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     for (int u = 0; u < M; ++u) {
       const int j = u * NT + tid;
       if (j < k && !first[u]) id[j] = -1;
-      else if (j < k) weight[j] = sum[u];
+      else if (j < k && sum[u] != weight[j]) {
+        weight[j] = sum[u];
+        part[j] = log(sum[u]);
+      }
     }
   }
   const float ref = other > -INFINITY ? other : 0.f, m = fmaxf(top_set, other);
   // sums over the others against their largest, and over the set against the row's
-  const float c1 = kLog2e, ct = kLog2e * inv_tau;
-  float s1 = 0.f, st = 0.f;
+  const float c1 = kLog2e, ct = (float)(kLog2e * inv_tau);
+  float s1 = __builtin_amdgcn_exp2f((xl - ref) * c1), st = __builtin_amdgcn_exp2f((xl - ref) * ct);
   each([&](const P16 &y, int) {
 #pragma unroll
     for (int e = 0; e < N; ++e) {
@@ -225,8 +224,8 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
       const double d = (double)logit[j] - m;
-      set1 += exp(d);
-      set += exp(d / tau);
+      if (aimed) set1 += exp_f32(d);
+      if (taught) set += exp(d * inv_tau);
       qs += weight[j];
     }
   s1 = wave_add(s1);
@@ -239,17 +238,19 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   __syncthreads();
   double others1 = 0.0, others = 0.0;
   set1 = set = qs = 0.0;
-#pragma unroll
+#pragma unroll 4
   for (int w = 0; w < NW; ++w) {
     others1 += sums[0][w]; others += sums[1][w];
     set1 += set_sums[0][w]; set += set_sums[1][w]; qs += set_sums[2][w];
   }
-  const double down = other > -INFINITY ? (double)other - m : 0.0, others_m = others * exp(down / tau);
-  const double z1 = others1 * exp(down) + set1, z = others_m + set, zq = qs + rest_weight;
-  const double Q = taught ? rest_weight / zq : 0.0, P = others_m / z;
+  const double down = other > -INFINITY ? (double)other - m : 0.0;
+  const float down1 = __expf((float)down), others_m = (float)others * __builtin_amdgcn_exp2f((float)down * ct);
+  const float z1 = fmaf((float)others1, down1, (float)set1), z = others_m + (float)set, zq = (float)(qs + rest_weight);
+  const float iz1 = 1.f / z1, iz = 1.f / z, izq = 1.f / zq, Q = taught ? (float)rest_weight * izq : 0.f, P = others_m * iz;
   // the others' gradient is their share of each other times P - Q, which is what the set's probabilities differ by
-  const double more = Q < 0.5 ? P - Q : qs / zq - set / z;
-  const float a1 = aimed ? (float)((1.0 - (double)te.weight) * exp(down) / z1 * inv_T) : 0.f, at = taught && others > 0.0 ? (float)((double)te.weight * tau * more / others * inv_T) : 0.f;
+  const float more = Q < 0.5f ? P - Q : (float)qs * izq - (float)set * iz;
+  const float w1 = (1.f - te.weight) * inv_T, wt = te.weight * te.temperature * inv_T;
+  const float a1 = aimed ? w1 * down1 * iz1 : 0.f, at = taught && others > 0.0 ? wt * more / (float)others : 0.f;
   each([&](const P16 &y, int v) {
     float g[N];
 #pragma unroll
@@ -259,46 +260,46 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
       if (aimed) g[e] = __builtin_amdgcn_exp2f(d * c1) * a1;
       if (taught) g[e] = fmaf(__builtin_amdgcn_exp2f(d * ct), at, g[e]);
     }
-    if (v < pieces) store_piece<BF>(out, v, V, g);
+    if (v < pieces) store_piece<BF>(out, v, g);
   });
-  for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
-  // the row's loss
+  for (int64_t c = last; c < pad; c += NT)
+    store1<BF>(out, c, c == last && c < V ? (aimed ? __builtin_amdgcn_exp2f((xl - ref) * c1) * a1 : 0.f) + (taught ? __builtin_amdgcn_exp2f((xl - ref) * ct) * at : 0.f) : 0.f);
+  // the row's loss, in 64 bits
+  const double whole = others * exp(down * inv_tau) + set;
   double kl = 0.0;
   if (taught && 64 * wave < k) {
-    const double log_z = log(z), log_zq = log(zq);
+    const double shift = log(whole) - log(qs + rest_weight);
     for (int j = tid; j < k; j += NT)
-      if (id[j] >= 0 && weight[j] != 0.0) kl += weight[j] / zq * ((log(weight[j]) - log_zq) - (((double)logit[j] - m) / tau - log_z));
+      if (id[j] >= 0 && weight[j] != 0.0) kl += weight[j] * (part[j] - ((double)logit[j] - m) * inv_tau + shift);
     kl = wave_add(kl);
   }
   if (lane == 0) kls[wave] = kl;
   __syncthreads();  // (the set's gradients take the places of what was written above, and so does the target's)
-  const double wt = (double)te.weight * tau;
   for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
       const double d = (double)logit[j] - m;
-      double g = taught ? wt * (exp(d / tau) / z - weight[j] / zq) : 0.0;
-      if (aimed) g += (1.0 - (double)te.weight) * (exp(d) / z1 - (id[j] == tgt ? 1.0 : 0.0));
-      store1<BF>(out, id[j], (float)(g * inv_T));
+      float g = taught ? wt * (exp_f32(d * inv_tau) * iz - (float)weight[j] * izq) : 0.f;
+      if (aimed) g += w1 * (exp_f32(d) * iz1 - (id[j] == tgt ? 1.f : 0.f));
+      store1<BF>(out, id[j], g);
     }
   if (tid == 0) {
     double loss = 0.0;
     if (aimed) {
-      loss = (1.0 - (double)te.weight) * (log(z1) - ((double)aim - m));
+      loss = (1.0 - (double)te.weight) * (log(others1 * exp(down) + set1) - ((double)aim - m));
       if (!(in_set[tgt / 32] >> (tgt & 31) & 1)) {
         const float d = aim - ref;
-        float g = fmaf(__builtin_amdgcn_exp2f(d * c1), a1, -(1.f - te.weight) * inv_T);
-        if (taught) g = fmaf(__builtin_amdgcn_exp2f(d * ct), at, g);
-        store1<BF>(out, tgt, g);
+        store1<BF>(out, tgt, (__builtin_amdgcn_exp2f(d * c1) * a1 - w1) + (taught ? __builtin_amdgcn_exp2f(d * ct) * at : 0.f));
       }
     }
     if (taught) {
       kl = 0.0;
       for (int w = 0; w < NW; ++w) kl += kls[w];
+      kl /= qs + rest_weight;
       if (rest_weight != 0.0) {
-        const double log_others = others_m > 0.0 ? log_share(others_m, set) : down / tau + (others > 0.0 ? log(others) : -INFINITY) - log(z);
-        kl += Q * (log_share(rest_weight, qs) - log_others);
+        const double rm = others * exp(down * inv_tau), log_others = rm > 0.0 ? log_share(rm, set) : down * inv_tau + (others > 0.0 ? log(others) : -INFINITY) - log(whole);
+        kl += rest_weight / (qs + rest_weight) * (log_share(rest_weight, qs) - log_others);
       }
-      loss += wt * tau * kl;
+      loss += (double)te.weight * tau * tau * kl;
     }
     rowloss[t] = (float)loss;
   }
