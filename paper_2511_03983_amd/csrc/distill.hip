@@ -1,4 +1,6 @@
 // The loss of a student's logits against a teacher's top logits and the targets, with its gradient.
+#include <type_traits>
+
 #include "nn.h"
 
 namespace {
@@ -8,11 +10,11 @@ constexpr float kLog2e = 1.44269504f;
 
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
 
-// Sixteen bytes of a row, from any element on, as floats: eight of bf16, four of fp32.  (Rows of an odd vocabulary start anywhere; loads and stores need no alignment.)
+// Sixteen bytes of a row, as floats: eight of bf16, four of fp32.
 template <int BF> struct Piece {
   static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
   u32x4v u;
-  __device__ __forceinline__ void load(const char *row, int v) { __builtin_memcpy(&u, row + (int64_t)v * 16, 16); }
+  __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(&u, p, 16); }  // (from any element on)
   static __device__ __forceinline__ u32x4v none() {  // -infinity throughout
     const uint32_t n = BF ? 0xff80ff80u : 0xff800000u;
     return u32x4v{n, n, n, n};
@@ -37,7 +39,7 @@ template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, f
   if (BF) reinterpret_cast<__bf16 *>(row)[c] = (__bf16)v;  // round to nearest even
   else reinterpret_cast<float *>(row)[c] = v;
 }
-template <int BF> __device__ __forceinline__ void store_piece(char *row, int v, const float *g) {
+template <int BF> __device__ __forceinline__ void store_piece(char *p, const float *g) {
   u32x4v u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -46,7 +48,7 @@ template <int BF> __device__ __forceinline__ void store_piece(char *row, int v, 
     if (BF) u[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{g[2 * i % Piece<BF>::N], g[(2 * i + 1) % Piece<BF>::N]}), b2));
     else u[i] = __float_as_uint(g[i]);
   }
-  __builtin_memcpy(row + (int64_t)v * 16, &u, 16);
+  __builtin_memcpy(p, &u, 16);
 }
 
 template <class T> __device__ __forceinline__ T wave_add(T v) {
@@ -68,59 +70,71 @@ __device__ __forceinline__ float exp_f32(double x) {
   return __builtin_amdgcn_exp2f(h) * fmaf((float)(y - h), 0.69314718f, 1.f);
 }
 
-// Natural logarithm of a / (a + b), near 1 as exact as far from it.
-__device__ __forceinline__ double log_share(double a, double b) { return b < a ? -log1p(b / a) : log(a / (a + b)); }
-
 // A row a workgroup.  The row's tokens are the teacher's (the set) and the others, whose share of the distribution is formed from themselves and not as what the set leaves: it may be
 // next to nothing, or all but everything.  With tau the temperature, p and q over the set and over the others together (P, Q of them), the gradient of
 // KL(q || p) is (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.
 // Bound by memory: the row is read once and its gradient written once.  It stays in registers as it came (NV pieces of 16 bytes a thread; rows that NT threads cannot hold, NV = 0, are read
 // three times), the set's columns as -infinity, so that they weigh nothing in the others' sums; their own gradients, a thread each and in 64 bits where they meet a logarithm, are stored over
 // the others' behind a barrier.
+// Pieces begin where the gradient's row is aligned, which is where the logits' is as a rule (rows of an odd vocabulary start anywhere; 8192 x 50257 bf16 from any element on 554 us, all rows
+// aligned 440); the columns before and behind them are a thread's each.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int64_t ld, const int32_t *targets, int V, twist_teacher te, char *grads, int64_t ldg, int64_t pad, float inv_T,
-                                                     float *rowloss) {
+                                                        float *rowloss) {
   using P16 = Piece<BF>;
-  constexpr int N = P16::N, NW = NT / 64, WORDS = NV ? NV * NT * N / 32 : 1 << 15;
-  __shared__ uint32_t in_set[WORDS];  // a bit a column
+  constexpr int N = P16::N, ES = P16::ES, NW = NT / 64, WORDS = NV ? NV * NT * N / 32 + 1 : (1 << 15) + 1;
+  __shared__ uint32_t in_set[WORDS];  // a bit a column, the first of a piece on a byte (fp32: half a byte)
   __shared__ int32_t id[kTop];
   __shared__ float logit[kTop];
   __shared__ double weight[kTop], part[kTop];  // the teacher's weights against its largest, and their exponents
   __shared__ float most[3][NW], sums[2][NW];
-  __shared__ double set_sums[3][NW], kls[NW];
+  __shared__ double set_sums[4][NW];
   __shared__ int twice;
   const int t = blockIdx.x, tid = threadIdx.x, k = te.k, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const char *row = logits + (int64_t)t * ld * P16::ES;
-  char *out = grads + (int64_t)t * ldg * P16::ES;
-  const double tau = te.temperature, inv_tau = 1.0 / tau;
-  const int pieces = V / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
-  const int last = pieces * N + tid;                    // the row's last columns, fewer than a piece, a thread each
+  const char *row = logits + (int64_t)t * ld * ES;
+  char *out = grads + (int64_t)t * ldg * ES;
+  const int head = min(V, (int)(-(reinterpret_cast<uintptr_t>(out) / ES) & (N - 1)));
+  const int pieces = (V - head) / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
+  const int ends = V - pieces * N, end = tid < head ? tid : pieces * N + tid;  // columns that are in no piece, and the thread's
+  const char *first = row + head * ES;
+  char *first_out = out + head * ES;
+  // what the first of the list need, and the row
+  const int64_t list = t * te.ld;
+  const int id0 = tid < k ? te.ids[list + tid] : -1;
+  const float value0 = tid < k ? te.values[list + tid] : 0.f;
+  const int tgt = te.weight < 1.f ? targets[t] : -1;
+  const bool aimed = (unsigned)tgt < (unsigned)V;
+  const float rest = te.rest ? te.rest[t] : -INFINITY;
   P16 x[NV ? NV : 1];
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     x[u].u = P16::none();
-    if (u * NT + tid < pieces) x[u].load(row, u * NT + tid);
+    if (u * NT + tid < pieces) x[u].load(first + (int64_t)(u * NT + tid) * 16);
   }
-  float xl = last < V ? load1<BF>(row, last) : -INFINITY;
-  const int tgt = te.weight < 1.f ? targets[t] : -1;
-  const bool aimed = (unsigned)tgt < (unsigned)V;
-  const float rest = te.rest ? te.rest[t] : -INFINITY, aim = aimed ? load1<BF>(row, tgt) : 0.f;
-  for (int i = tid; i < (V + 31) / 32; i += NT) in_set[i] = 0;
+  float xl = tid < ends ? load1<BF>(row, end) : -INFINITY;
+  const float aim = aimed ? load1<BF>(row, tgt) : 0.f;
+  const double tau = te.temperature, inv_tau = 1.0 / tau;
+  for (int i = tid; i < V / 32 + 1; i += NT) in_set[i] = 0;
   if (tid == 0) twice = 0;
+  auto bit = [&](int c) { return c - head + N; };  // of a column, in the table
   __syncthreads();
   float top_t = rest, top_set = -INFINITY;  // largest of the teacher's, and of the student's in the set
   for (int j = tid; j < k; j += NT) {
-    const int c = te.ids[t * te.ld + j];
+    const int c = j == tid ? id0 : te.ids[list + j];
     const bool on = (unsigned)c < (unsigned)V;
     id[j] = on ? c : -1;
     if (!on) continue;
-    if (atomicOr(&in_set[c / 32], 1u << (c & 31)) >> (c & 31) & 1) twice = 1;
-    logit[j] = load1<BF>(row, c);
-    top_set = fmaxf(top_set, logit[j]);
-    top_t = fmaxf(top_t, (float)(te.values[t * te.ld + j] * inv_tau));
+    const float s = load1<BF>(row, c);
+    if (atomicOr(&in_set[bit(c) / 32], 1u << (bit(c) & 31)) >> (bit(c) & 31) & 1) twice = 1;
+    logit[j] = s;
+    top_set = fmaxf(top_set, s);
+    part[j] = (j == tid ? value0 : te.values[list + j]) * inv_tau;
+    top_t = fmaxf(top_t, (float)part[j]);
   }
-  top_t = wave_max(top_t);
-  top_set = wave_max(top_set);
+  if (64 * wave < k) {
+    top_t = wave_max(top_t);
+    top_set = wave_max(top_set);
+  }
   if (lane == 0) { most[0][wave] = top_t; most[1][wave] = top_set; }
   __syncthreads();
 #pragma unroll
@@ -128,14 +142,15 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   const bool taught = te.weight > 0.f && top_t > -INFINITY;
   if (!taught && !aimed) {
     const float zeros[N] = {};
-    for (int v = tid; v < pieces; v += NT) store_piece<BF>(out, v, zeros);
-    for (int64_t c = last; c < pad; c += NT) store1<BF>(out, c, 0.f);
+    for (int v = tid; v < pieces; v += NT) store_piece<BF>(first_out + (int64_t)v * 16, zeros);
+    if (tid < ends) store1<BF>(out, end, 0.f);
+    for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
     if (tid == 0) rowloss[t] = 0.f;
     return;
   }
   auto bits_of = [&](int v) {  // of a piece's columns in the set
-    const uint32_t b = reinterpret_cast<const uint8_t *>(in_set)[N == 8 ? v : v / 2];
-    return N == 8 ? b : b >> (v % 2 * 4) & 15u;
+    const uint32_t b = reinterpret_cast<const uint8_t *>(in_set)[N == 8 ? v + 1 : (v + 1) / 2];
+    return N == 8 ? b : b >> ((v + 1) % 2 * 4) & 15u;
   };
   // f(piece, its number) for all of the thread's pieces of the row, those beyond it and the set's columns -infinity
   auto each = [&](auto f) {
@@ -151,7 +166,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     } else {
       for (int v = tid; v < pieces; v += NT) {
         P16 y;
-        y.load(row, v);
+        y.load(first + (int64_t)v * 16);
         y.clear(bits_of(v));
         f(y, v);
       }
@@ -159,11 +174,11 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   };
 #pragma unroll
   for (int u = 0; u < NV; ++u)
-    if (u * NT < mine) {
+    if (u * NT + tid < pieces) {
       const uint32_t b = bits_of(u * NT + tid);
       if (b) x[u].clear(b);
     }
-  if (last < V && in_set[last / 32] >> (last & 31) & 1) xl = -INFINITY;
+  if (tid < ends && in_set[bit(end) / 32] >> (bit(end) & 31) & 1) xl = -INFINITY;
   float other = xl;
   each([&](const P16 &y, int) {
 #pragma unroll
@@ -174,7 +189,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   // the teacher's weights against its largest; of a token that is named twice the first entry takes the others'
   for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
-      part[j] = te.values[t * te.ld + j] * inv_tau - top_t;
+      part[j] -= top_t;
       weight[j] = taught ? exp(part[j]) : 0.0;
     }
   const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - (double)top_t) : 0.0;
@@ -184,24 +199,24 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   if (twice) {
     constexpr int M = (kTop + NT - 1) / NT;
     double sum[M];
-    bool first[M];
+    bool first_of[M];
 #pragma unroll
     for (int u = 0; u < M; ++u) {
       const int j = u * NT + tid;
       sum[u] = 0.0;
-      first[u] = j < k && id[j] >= 0;
-      if (first[u])
+      first_of[u] = j < k && id[j] >= 0;
+      if (first_of[u])
         for (int i = 0; i < k; ++i)
           if (id[i] == id[j]) {
             sum[u] += weight[i];
-            first[u] = first[u] && i >= j;
+            first_of[u] = first_of[u] && i >= j;
           }
     }
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < M; ++u) {
       const int j = u * NT + tid;
-      if (j < k && !first[u]) id[j] = -1;
+      if (j < k && !first_of[u]) id[j] = -1;
       else if (j < k && sum[u] != weight[j]) {
         weight[j] = sum[u];
         part[j] = log(sum[u]);
@@ -209,71 +224,95 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     }
   }
   const float ref = other > -INFINITY ? other : 0.f, m = fmaxf(top_set, other);
-  // sums over the others against their largest, and over the set against the row's
-  const float c1 = kLog2e, ct = (float)(kLog2e * inv_tau);
-  float s1 = __builtin_amdgcn_exp2f((xl - ref) * c1), st = __builtin_amdgcn_exp2f((xl - ref) * ct);
-  each([&](const P16 &y, int) {
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float d = y[e] - ref;
-      if (aimed) s1 += __builtin_amdgcn_exp2f(d * c1);
-      if (taught) st += __builtin_amdgcn_exp2f(d * ct);
-    }
-  });
-  double set1 = 0.0, set = 0.0, qs = 0.0;
-  for (int j = tid; j < k; j += NT)
-    if (id[j] >= 0) {
-      const double d = (double)logit[j] - m;
-      if (aimed) set1 += exp_f32(d);
-      if (taught) set += exp(d * inv_tau);
-      qs += weight[j];
-    }
-  s1 = wave_add(s1);
-  st = wave_add(st);
-  if (64 * wave < k) { set1 = wave_add(set1); set = wave_add(set); qs = wave_add(qs); }
-  if (lane == 0) {
-    sums[0][wave] = s1; sums[1][wave] = st;
-    set_sums[0][wave] = set1; set_sums[1][wave] = set; set_sums[2][wave] = qs;
-  }
-  __syncthreads();
-  double others1 = 0.0, others = 0.0;
-  set1 = set = qs = 0.0;
-#pragma unroll 4
-  for (int w = 0; w < NW; ++w) {
-    others1 += sums[0][w]; others += sums[1][w];
-    set1 += set_sums[0][w]; set += set_sums[1][w]; qs += set_sums[2][w];
-  }
+  // Sums over the others against their largest, and over the set against the row's.  Exponentials of (v - ref) / tau, and of v - ref: the same or only one of them asked for (mode 0), squares
+  // (temperature 2: 1; 4: 2), or an exponential each (3).  8192 x 50257 bf16 at temperature 2, both asked for: 372 us, with an exponential each and the choice made for every element 487; one of them alone 338
+  const float c1 = kLog2e, ct = (float)(kLog2e * inv_tau), c = taught ? ct : c1;
+  const int mode = !(taught && aimed) || te.temperature == 1.f ? 0 : te.temperature == 2.f ? 1 : te.temperature == 4.f ? 2 : 3;
+  auto exps = [&](auto how, float v, auto f) {  // f(first, second)
+    const float d = v - ref, a = __builtin_amdgcn_exp2f(d * c);
+    if (how == 0) f(a, a);
+    else if (how == 1) f(a, a * a);
+    else if (how == 2) f(a, (a * a) * (a * a));
+    else f(a, __builtin_amdgcn_exp2f(d * c1));
+  };
+  auto in_mode = [&](auto f) {
+    if (mode == 0) f(std::integral_constant<int, 0>{});
+    else if (mode == 1) f(std::integral_constant<int, 1>{});
+    else if (mode == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 3>{});
+  };
   const double down = other > -INFINITY ? (double)other - m : 0.0;
-  const float down1 = __expf((float)down), others_m = (float)others * __builtin_amdgcn_exp2f((float)down * ct);
-  const float z1 = fmaf((float)others1, down1, (float)set1), z = others_m + (float)set, zq = (float)(qs + rest_weight);
-  const float iz1 = 1.f / z1, iz = 1.f / z, izq = 1.f / zq, Q = taught ? (float)rest_weight * izq : 0.f, P = others_m * iz;
-  // the others' gradient is their share of each other times P - Q, which is what the set's probabilities differ by
-  const float more = Q < 0.5f ? P - Q : (float)qs * izq - (float)set * iz;
   const float w1 = (1.f - te.weight) * inv_T, wt = te.weight * te.temperature * inv_T;
-  const float a1 = aimed ? w1 * down1 * iz1 : 0.f, at = taught && others > 0.0 ? wt * more / (float)others : 0.f;
-  each([&](const P16 &y, int v) {
-    float g[N];
+  double others1 = 0.0, others = 0.0, set1 = 0.0, set = 0.0, qs = 0.0, kl = 0.0;
+  float iz1, iz, izq, a1, as;
+  auto slope = [&](auto how, float a, float b) { return how ? fmaf(b, a1, a * as) : a * as; };
+  in_mode([&](auto how) {
+    float s1 = 0.f, st = 0.f;
+    auto add = [&](float a, float b) {
+      st += a;
+      if (how) s1 += b;
+    };
+    exps(how, xl, add);
+    each([&](const P16 &y, int) {
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float d = y[e] - ref;
-      g[e] = 0.f;
-      if (aimed) g[e] = __builtin_amdgcn_exp2f(d * c1) * a1;
-      if (taught) g[e] = fmaf(__builtin_amdgcn_exp2f(d * ct), at, g[e]);
-    }
-    if (v < pieces) store_piece<BF>(out, v, g);
-  });
-  for (int64_t c = last; c < pad; c += NT)
-    store1<BF>(out, c, c == last && c < V ? (aimed ? __builtin_amdgcn_exp2f((xl - ref) * c1) * a1 : 0.f) + (taught ? __builtin_amdgcn_exp2f((xl - ref) * ct) * at : 0.f) : 0.f);
-  // the row's loss, in 64 bits
-  const double whole = others * exp(down * inv_tau) + set;
-  double kl = 0.0;
-  if (taught && 64 * wave < k) {
-    const double shift = log(whole) - log(qs + rest_weight);
+      for (int e = 0; e < N; ++e) exps(how, y[e], add);
+    });
     for (int j = tid; j < k; j += NT)
-      if (id[j] >= 0 && weight[j] != 0.0) kl += weight[j] * (part[j] - ((double)logit[j] - m) * inv_tau + shift);
-    kl = wave_add(kl);
+      if (id[j] >= 0) {
+        const double d = (double)logit[j] - m;
+        if (aimed) set1 += exp_f32(d);
+        if (taught) set += exp(d * inv_tau);
+        qs += weight[j];
+        if (weight[j] != 0.0) kl += weight[j] * (part[j] - d * inv_tau);
+      }
+    st = wave_add(st);
+    s1 = how ? wave_add(s1) : st;
+    if (64 * wave < k) { set1 = wave_add(set1); set = wave_add(set); qs = wave_add(qs); kl = wave_add(kl); }
+    if (lane == 0) {
+      sums[0][wave] = s1; sums[1][wave] = st;
+      set_sums[0][wave] = set1; set_sums[1][wave] = set; set_sums[2][wave] = qs; set_sums[3][wave] = kl;
+    }
+    __syncthreads();
+    set1 = set = qs = kl = 0.0;
+#pragma unroll 1
+    for (int w = 0; w < NW; ++w) {
+      others1 += sums[0][w]; others += sums[1][w];
+      if (64 * w < k) { set1 += set_sums[0][w]; set += set_sums[1][w]; qs += set_sums[2][w]; kl += set_sums[3][w]; }
+    }
+    const float down1 = __expf((float)down), others_m = (float)others * __builtin_amdgcn_exp2f((float)down * ct);
+    iz1 = 1.f / fmaf((float)others1, down1, (float)set1);
+    iz = 1.f / (others_m + (float)set);
+    izq = 1.f / (float)(qs + rest_weight);
+    const float Q = taught ? (float)rest_weight * izq : 0.f, P = others_m * iz;
+    // the others' gradient is their share of each other times P - Q, which is what the set's probabilities differ by
+    const float more = Q < 0.5f ? P - Q : (float)qs * izq - (float)set * iz, at = taught && others > 0.0 ? wt * more / (float)others : 0.f;
+    a1 = aimed ? w1 * down1 * iz1 : 0.f;
+    as = how ? at : a1 + at;
+    each([&](const P16 &y, int v) {
+      float g[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) exps(how, y[e], [&](float a, float b) { g[e] = slope(how, a, b); });
+      if (v < pieces) store_piece<BF>(first_out + (int64_t)v * 16, g);
+    });
+    if (tid < ends) exps(how, xl, [&](float a, float b) { store1<BF>(out, end, slope(how, a, b)); });
+  });
+  for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
+  if (wave == NW - 1) {
+    // the row's loss, in 64 bits: the share of one of two amounts is formed from their quotient, so that it is as exact near 1 as far from it.  A lane each for what would be one call behind the other.
+    auto of = [](double v, int from) { return __shfl(v, from, 64); };
+    const double e = exp(lane == 0 ? down * inv_tau : down), rm = others * of(e, 0), r1 = others1 * of(e, 1) + set1, whole = rm + set, qall = qs + rest_weight;
+    const double a = lane == 0 ? rm : rest_weight, b = lane == 0 ? set : qs, ratio = b < a ? b / a : a / b;  // (lanes 0 and 1)
+    const double l = log(lane == 0 ? whole : lane == 1 ? qall : lane == 2 ? r1 : lane == 3 ? others : lane == 4 ? rm / set : rest_weight / qs), l1 = log1p(ratio);
+    const double share = rm > 0.0 ? -of(l1, 0) + (set < rm ? 0.0 : of(l, 4)) : down * inv_tau + (others > 0.0 ? of(l, 3) : -INFINITY) - of(l, 0);
+    const double theirs = -of(l1, 1) + (qs < rest_weight ? 0.0 : of(l, 5));
+    double loss = aimed ? (1.0 - (double)te.weight) * (of(l, 2) - ((double)aim - m)) : 0.0;
+    if (taught) {
+      kl += qs != 0.0 ? qs * (of(l, 0) - of(l, 1)) : 0.0;
+      if (rest_weight != 0.0) kl += rest_weight * (theirs - share);
+      loss += (double)te.weight * tau * tau * (kl / qall);
+    }
+    if (lane == 0) rowloss[t] = (float)loss;
   }
-  if (lane == 0) kls[wave] = kl;
   __syncthreads();  // (the set's gradients take the places of what was written above, and so does the target's)
   for (int j = tid; j < k; j += NT)
     if (id[j] >= 0) {
@@ -282,27 +321,8 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
       if (aimed) g += w1 * (exp_f32(d) * iz1 - (id[j] == tgt ? 1.f : 0.f));
       store1<BF>(out, id[j], g);
     }
-  if (tid == 0) {
-    double loss = 0.0;
-    if (aimed) {
-      loss = (1.0 - (double)te.weight) * (log(others1 * exp(down) + set1) - ((double)aim - m));
-      if (!(in_set[tgt / 32] >> (tgt & 31) & 1)) {
-        const float d = aim - ref;
-        store1<BF>(out, tgt, (__builtin_amdgcn_exp2f(d * c1) * a1 - w1) + (taught ? __builtin_amdgcn_exp2f(d * ct) * at : 0.f));
-      }
-    }
-    if (taught) {
-      kl = 0.0;
-      for (int w = 0; w < NW; ++w) kl += kls[w];
-      kl /= qs + rest_weight;
-      if (rest_weight != 0.0) {
-        const double rm = others * exp(down * inv_tau), log_others = rm > 0.0 ? log_share(rm, set) : down * inv_tau + (others > 0.0 ? log(others) : -INFINITY) - log(whole);
-        kl += rest_weight / (qs + rest_weight) * (log_share(rest_weight, qs) - log_others);
-      }
-      loss += (double)te.weight * tau * tau * kl;
-    }
-    rowloss[t] = (float)loss;
-  }
+  if (tid == NT - 1 && aimed && !(in_set[bit(tgt) / 32] >> (bit(tgt) & 31) & 1))
+    in_mode([&](auto how) { exps(how, aim, [&](float a, float b) { store1<BF>(out, tgt, slope(how, a, b) - w1); }); });
 }
 
 }  // namespace
