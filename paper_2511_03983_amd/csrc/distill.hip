@@ -2,43 +2,13 @@
 #include <type_traits>
 
 #include "nn.h"
+#include "row.h"
 
 namespace {
 
 constexpr int kTop = 1024;  // the longest list
 constexpr float kLog2e = 1.44269504f;
 
-typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
-
-// Sixteen bytes of a row, as floats: eight of bf16, four of fp32.
-template <int BF> struct Piece {
-  static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
-  u32x4v u;
-  __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(&u, p, 16); }  // (from any element on)
-  static __device__ __forceinline__ u32x4v none() {  // -infinity throughout
-    const uint32_t n = BF ? 0xff80ff80u : 0xff800000u;
-    return u32x4v{n, n, n, n};
-  }
-  __device__ __forceinline__ float operator[](int e) const {
-    if (!BF) return __uint_as_float(u[e % 4]);
-    return __uint_as_float(e % 2 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
-  }
-  __device__ __forceinline__ void clear(uint32_t bits) {  // -infinity where a bit is set
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (bits >> e & 1) {
-        if (BF) u[e / 2] = e % 2 ? (u[e / 2] & 0xffffu) | 0xff800000u : (u[e / 2] & 0xffff0000u) | 0xff80u;
-        else u[e % 4] = 0xff800000u;
-      }
-  }
-};
-template <int BF> __device__ __forceinline__ float load1(const char *row, int c) {
-  return BF ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[c] << 16) : reinterpret_cast<const float *>(row)[c];
-}
-template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, float v) {
-  if (BF) reinterpret_cast<__bf16 *>(row)[c] = (__bf16)v;  // round to nearest even
-  else reinterpret_cast<float *>(row)[c] = v;
-}
 template <int BF> __device__ __forceinline__ void store_piece(char *p, const float *g) {
   u32x4v u;
 #pragma unroll
@@ -49,17 +19,6 @@ template <int BF> __device__ __forceinline__ void store_piece(char *p, const flo
     else u[i] = __float_as_uint(g[i]);
   }
   __builtin_memcpy(p, &u, 16);
-}
-
-template <class T> __device__ __forceinline__ T wave_add(T v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
 }
 
 // exp(x) in 32 bits: the exponent's rounding, which a large one would multiply, taken care of

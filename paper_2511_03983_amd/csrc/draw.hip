@@ -1,168 +1,566 @@
 // What is taken from a row of logits: a token drawn from it, or its k largest.  A row's columns have one order, larger logits first and equal ones by column; everything here is a
 // beginning of it.
 #include "nn.h"
+#include "row.h"
 
 namespace {
 
-constexpr int kT = 256;
-constexpr int kTop = 1024;  // the longest list
+constexpr int kTop = 1024;   // the longest list
+constexpr int kList = 1536;  // columns that are put in order by comparing them with each other
+constexpr int kBins = 1024;
+constexpr int kColumnBits = 20;
 
-template <int BF> __device__ __forceinline__ float load1(const void *p, int64_t i) {
-  const float v = BF ? __uint_as_float((uint32_t) static_cast<const uint16_t *>(p)[i] << 16) : static_cast<const float *>(p)[i];
-  return v == v ? v + 0.f : -INFINITY;  // no number: -infinity; -0 is 0
+// Unsigned numbers in the order of a row's columns: the logit's place in 32 bits, the column (turned over) below it.  Columns that hold no number count as -infinity, -0 is 0.
+__device__ __forceinline__ uint64_t place(float v, int c) {
+  const uint32_t b = __float_as_uint(v == v ? v + 0.f : -INFINITY);
+  return (uint64_t)(b ^ (b >> 31 ? 0xffffffffu : 0x80000000u)) << kColumnBits | ((1u << kColumnBits) - 1 - (uint32_t)c);
+}
+__device__ __forceinline__ float value_of(uint64_t p) {
+  const uint32_t k = (uint32_t)(p >> kColumnBits);
+  return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu));
+}
+__device__ __forceinline__ int column_of(uint64_t p) { return (1 << kColumnBits) - 1 - (int)(p & ((1u << kColumnBits) - 1)); }
+
+// 2^x in 64 bits for x <= 0 (below -200: 2^-200): 2^f, f of the fraction in -1/2 .. 1/2, by a Chebyshev polynomial of degree 10, 2^-51 off.
+__device__ __forceinline__ double power2(double x, int bits) {
+  x = fmax(x, -200.0);
+  const double n = rint(x), f = x - n;
+  double p = 7.074194562613105e-09;
+  p = fma(p, f, 1.020869083593037e-07);
+  p = fma(p, f, 1.3215432534254118e-06);
+  p = fma(p, f, 1.5252657257186041e-05);
+  p = fma(p, f, 0.00015403530463727982);
+  p = fma(p, f, 0.0013333558230170627);
+  p = fma(p, f, 0.009618129107587253);
+  p = fma(p, f, 0.05550410866444768);
+  p = fma(p, f, 0.24022650695910158);
+  p = fma(p, f, 0.69314718055995);
+  p = fma(p, f, 1.0);
+  return ldexp(p, (int)n + bits);
 }
 
-// Unsigned numbers in the order of the logits, and of a row's columns: the place in 32 bits, the column (turned over) below it.
-__device__ __forceinline__ uint32_t value_key(float v) {
-  const uint32_t b = __float_as_uint(v);
-  return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u);
-}
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
-__device__ __forceinline__ uint64_t place(float v, int c) { return (uint64_t)value_key(v) << 32 | (0xffffffffu - (uint32_t)c); }
+// What a workgroup shares while it searches a row
+template <int NT> struct Search {
+  union {
+    unsigned long long amount[kBins];
+    uint32_t count[kBins];
+  } bins;
+  unsigned long long list[kList];    // places that may be taken, in any order; then what the sorted ones weigh
+  unsigned long long sorted[kList];
+  unsigned long long found[2], wave_sum[NT / 64];
+  float most[NT / 64], least[NT / 64];
+  int n;
+};
 
-template <class T> __device__ __forceinline__ T block_add(T v, T *sh) {
+// A workgroup's steps over a row that it reads again for every pass: what is seldom needed, or takes long in any case.  Nothing here touches the row in registers.
+template <int BF, int NT> struct Finder {
+  using P16 = Piece<BF>;
+  static constexpr int N = P16::N, NW = NT / 64;
+  Search<NT> &sh;
+  const char *row, *first;
+  int V, head, pieces, tid, wave, lane;
+
+  __device__ __forceinline__ Finder(Search<NT> &s, const char *row_, int V_, int head_, int wave_) : sh(s), row(row_), V(V_), head(head_), tid(threadIdx.x), wave(wave_) {
+    lane = tid & 63;
+    pieces = (V - head) / N;
+    first = row + head * P16::ES;
+  }
+  // f(logit, column) of every column of the row
+  template <class F> __device__ __forceinline__ void columns(F f) const {
+#pragma unroll 1
+    for (int v = tid; v < pieces; v += NT) {
+      P16 y;
+      y.load(first + (int64_t)v * 16);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (sh[0] + sh[1]) + (sh[2] + sh[3]);
-}
-template <class T> __device__ __forceinline__ T block_most(T v, T *sh) {
+      for (int e = 0; e < N; ++e) f(y[e], head + v * N + e);
+    }
+    const int c = tid < head ? tid : pieces * N + tid;
+    if (c < V && tid < V - pieces * N) f(load1<BF>(row, c), c);
+  }
+  __device__ __forceinline__ unsigned long long block_add(unsigned long long v) const {
+    v = wave_add(v);
+    __syncthreads();
+    if (lane == 0) sh.wave_sum[wave] = v;
+    __syncthreads();
+    unsigned long long s = 0;
+#pragma unroll 4
+    for (int w = 0; w < NW; ++w) s += sh.wave_sum[w];
+    return s;
+  }
+  template <class T> __device__ __forceinline__ void clear(T *bins, int n) const {
+    for (int i = tid; i < n; i += NT) bins[i] = 0;
+  }
+  // The bin in which what lies in the bins up to it reaches `target` (n: none), and what lies before it.  n: a multiple of 64.
+  template <class T> __device__ __forceinline__ int find(const T *bins, int n, unsigned long long target, unsigned long long &before) const {
+    if (wave == 0) {
+      const int per = n / 64;
+      unsigned long long s = 0, upto;
+      for (int i = 0; i < per; ++i) s += bins[lane * per + i];
+      upto = s;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = max(v, (T)__shfl_xor(v, o, 64));
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned long long u = __shfl_up(upto, o, 64);
+        if (lane >= o) upto += u;
+      }
+      const uint64_t hit = __ballot(upto >= target);
+      if (hit == 0) {
+        if (lane == 63) { sh.found[0] = n; sh.found[1] = upto; }
+      } else if (lane == __builtin_ctzll(hit)) {
+        upto -= s;
+        int b = lane * per;
+        while (upto + bins[b] < target) upto += bins[b++];
+        sh.found[0] = b;
+        sh.found[1] = upto;
+      }
+    }
+    __syncthreads();
+    before = sh.found[1];
+    return (int)sh.found[0];
+  }
+
+  // The last place of the shortest beginning of the row whose columns' amounts add up to `target` (at least 1, at most the whole row's), a few bits of the places at a time.
+  template <class F> __device__ __forceinline__ uint64_t reach(unsigned long long target, F amount) const {
+    uint64_t prefix = 0;
+    int shift = 32 + kColumnBits;
+#pragma unroll 1
+    while (shift > 0) {
+      const int w = shift > 12 ? 10 : 6, bins = 1 << w, above = shift;
+      shift -= w;
+      __syncthreads();
+      clear(sh.bins.amount, bins);
+      __syncthreads();
+      columns([&](float v, int c) {
+        const uint64_t p = place(v, c);
+        if (p >> above != prefix) return;
+        const unsigned long long a = amount(v, p);
+        if (a) atomicAdd(&sh.bins.amount[bins - 1 - (int)(p >> shift & (bins - 1))], a);
+      });
+      __syncthreads();
+      unsigned long long before;
+      const int b = find(sh.bins.amount, bins, target, before);
+      target -= before;
+      prefix = prefix << w | (uint64_t)(bins - 1 - b);
+    }
+    __syncthreads();
+    return prefix;
+  }
+  // the smallest logit above -infinity
+  __device__ __forceinline__ float smallest() const {
+    float l = INFINITY;
+    columns([&](float v, int) { l = v > -INFINITY ? fminf(l, v) : l; });
+    l = -wave_max(-l);
+    __syncthreads();
+    if (lane == 0) sh.least[wave] = l;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < NW; ++w) l = fminf(l, sh.least[w]);
+    return l;
+  }
+  // A logit that k columns at least are not below (none above -infinity is, where there are fewer), by counting all in bins.  -infinity: no bins for them.
+  __device__ __forceinline__ float bound_of_all(int k, float top) const {
+    const float l = smallest(), span = top - l;
+    if (!(span < INFINITY)) return -INFINITY;
+    const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
+    clear(sh.bins.count, kBins);
+    __syncthreads();
+    columns([&](float v, int) {
+      if (v > -INFINITY) atomicAdd(&sh.bins.count[(int)((top - v) * scale)], 1u);
+    });
+    __syncthreads();
+    unsigned long long before;
+    const int b = find(sh.bins.count, kBins, k, before);
+    return b < kBins ? edge(b, top, scale) : l;
+  }
+  // a logit that none in bins 0 .. b is below, by the arithmetic that puts them there
+  static __device__ __forceinline__ float edge(int b, float top, float scale) {
+    if (scale == 0.f) return top;
+    const float e = top - (b + 1) / scale;
+    return e - (4e-7f * (fabsf(top) + fabsf(e)) + 1e-37f);
+  }
+  // Puts the list's n places in order, in sh.sorted: the first `most` of them.
+  __device__ __forceinline__ void sort(int n, int most) const {
+#pragma unroll 1
+    for (int i = tid; i < n; i += NT) {
+      const unsigned long long p = sh.list[i];
+      int at = 0;
+      for (int j = 0; j < n; ++j) at += sh.list[j] > p;
+      if (at < most) sh.sorted[at] = p;
+    }
+    __syncthreads();
+  }
+};
+
+// f(logit, column) of the columns at `from` (above -infinity) and above, which are few
+template <class R, class F> __device__ __forceinline__ void above(R &row, float from, F f) {
+  row.each([&](const typename R::P16 &y, int v) {
+    if (y.most() >= from) {
+#pragma unroll
+      for (int e = 0; e < R::N; ++e)
+        if (y[e] >= from) f(y[e], row.head + v * R::N + e);
+    }
+  });
+  if (row.xl >= from) f(row.xl, row.end);
+}
+// The row's largest logit (the thread's: `mine`), and the smallest of the threads' largest
+template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Search<NT> &sh, int wave, int lane, float &mine, float &top, float &low) {
+  float m = fmaxf(row.xl, -INFINITY);
+  row.each([&](const typename R::P16 &y, int) { m = fmaxf(m, y.most()); });
+  mine = m;
+  top = wave_max(m);
+  low = -wave_max(m > -INFINITY ? -m : -INFINITY);
+  if (lane == 0) { sh.most[wave] = top; sh.least[wave] = low; }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) { top = fmaxf(top, sh.most[w]); low = fminf(low, sh.least[w]); }
+}
+// A logit that k columns at least are not below, and not many more where logits differ, by counting in bins the threads' largest, the pieces' or all.  -infinity: none was found.
+template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &row, const Finder<BF, NT> &f, int k, float mine, float top, float low) {
+  const float span = top - low;
+  if (!(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
+  if (k <= NT / 2) {
+    const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
+    f.clear(f.sh.bins.count, kBins);
+    __syncthreads();
+    auto put = [&](float v) {
+      if (v >= low) atomicAdd(&f.sh.bins.count[(int)((top - v) * scale)], 1u);
+    };
+    if (8 * k <= NT) put(mine);
+    else {
+      row.each([&](const typename R::P16 &y, int) { put(y.most()); });
+      put(row.xl);
+    }
+    __syncthreads();
+    unsigned long long before;
+    const int b = f.find(f.sh.bins.count, kBins, k, before);
+    if (b < kBins) return f.edge(b, top, scale);
+  }
+  return f.bound_of_all(k, top);
+}
+// the list from the columns at `from` and above; their number, which may be more than the list holds
+template <int NT, class R> __device__ __forceinline__ int collect(R &row, Search<NT> &sh, float from) {
   __syncthreads();
-  return max(max(sh[0], sh[1]), max(sh[2], sh[3]));
+  if (threadIdx.x == 0) sh.n = 0;
+  __syncthreads();
+  above(row, from, [&](float v, int c) {
+    const int i = atomicAdd(&sh.n, 1);
+    if (i < kList) sh.list[i] = place(v, c);
+  });
+  __syncthreads();
+  return sh.n;
 }
 
-// The last place of the shortest beginning whose columns' amounts add up to `target` (at least 1, at most the whole row's), by halving what is left of the places: 64 passes.
-template <int BF, class F> __device__ uint64_t reach(const void *x, int64_t row, int V, uint64_t target, unsigned long long *sh, F amount) {
-  uint64_t lo = 0, hi = ~0ull;  // the beginning down to lo is long enough, the one down to hi + 1 is not
-  while (lo < hi) {
-    const uint64_t mid = hi - (hi - lo) / 2;
-    unsigned long long n = 0;
-    for (int c = threadIdx.x; c < V; c += kT) {
-      const float v = load1<BF>(x, row + c);
-      if (place(v, c) >= mid) n += amount(v);
+// One row's settings and what follows from them: probabilities are whole multiples of 2^-bits of the largest, in 64 bits, so that any order of their sums gives the same.
+struct Weigher {
+  float top, temp;
+  double c;  // log2(e) / temperature
+  int bits;
+  __device__ __forceinline__ double exponent(float v) const { return v == top ? 0.0 : ((double)v - (double)top) * c; }  // of 2
+  __device__ __forceinline__ unsigned long long operator()(float v) const {
+    if (!(v > -INFINITY)) return 0;
+    // (added to 2^52 the number is rounded to whole ones, which its last 52 bits are)
+    return (unsigned long long)__double_as_longlong(power2(exponent(v), bits) + 4503599627370496.0) & 0xfffffffffffffull;
+  }
+  // The smallest logit whose probability is `least` of the largest: near where the logarithm says, a lane a value, otherwise by halving.
+  __device__ float smallest(double least, int lane) const {
+    if (least >= 1.0) return top;
+    auto key = [](float v) { const uint32_t b = __float_as_uint(v); return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u); };
+    auto value = [](uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); };
+    auto enough = [&](uint32_t k) { return power2(exponent(value(k)), 0) >= least; };
+    uint32_t lo = key(-3.402823466e38f), hi = key(top);
+    const uint32_t guess = key((float)((double)top + log2(least) / c));
+    if (guess > lo + 32 && guess < hi) {
+      const uint64_t yes = __ballot(guess - 32 + lane >= hi || enough(guess - 32 + lane));
+      if (yes && !(yes & 1)) return value(min(hi, guess - 32 + (uint32_t)__builtin_ctzll(yes)));
     }
-    if (block_add(n, sh) >= target) lo = mid;
-    else hi = mid - 1;
-  }
-  return lo;
-}
-
-// A row a workgroup.  Sums of probabilities are whole multiples of 2^-bits of the largest, formed in 64 bits from exponentials in 64: any order gives the same, and a column's share of them
-// is exact to far less than the random number's last place.
-template <int BF>
-__global__ __launch_bounds__(kT) void draw_kernel(const void *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules R, int32_t *tokens, float *logprobs, int32_t *kept) {
-  __shared__ unsigned long long sh[4];
-  const int t = blockIdx.x;
-  const int64_t row = t * ld;
-  uint64_t first = 0;
-  unsigned long long n = 0;
-  for (int c = threadIdx.x; c < V; c += kT) {
-    const float v = load1<BF>(x, row + c);
-    const uint64_t p = place(v, c);
-    first = p > first ? p : first;
-    n += v > -INFINITY;
-  }
-  first = block_most((unsigned long long)first, sh);
-  n = block_add(n, sh);
-  const float top = key_value((uint32_t)(first >> 32)), temp = R.temperature ? R.temperature[t] : 1.f;
-  if (n == 0 || !(temp > 0.f)) {
-    if (threadIdx.x == 0) {
-      tokens[t] = n ? (int32_t)(0xffffffffu - (uint32_t)first) : -1;
-      if (logprobs) logprobs[t] = n ? 0.f : -INFINITY;
-      if (kept) kept[t] = n ? 1 : 0;
-    }
-    return;
-  }
-  const double scale = ldexp(1.0, bits);
-  auto exponent = [&](float v) { return v == top ? 0.0 : fmax(((double)v - (double)top) / (double)temp, -1e5); };  // (also where that is no number)
-  auto mass = [&](float v) -> unsigned long long { return v > -INFINITY ? (unsigned long long)(exp(exponent(v)) * scale + 0.5) : 0; };
-  auto one = [](float v) -> unsigned long long { return v > -INFINITY; };
-  auto sum_from = [&](uint64_t from) {
-    unsigned long long m = 0;
-    for (int c = threadIdx.x; c < V; c += kT) {
-      const float v = load1<BF>(x, row + c);
-      if (place(v, c) >= from) m += mass(v);
-    }
-    return block_add(m, sh);
-  };
-  // the last place that each rule keeps
-  uint64_t last = 0;
-  if (R.top_k && R.top_k[t] > 0 && (unsigned)R.top_k[t] < n) last = reach<BF>(x, row, V, R.top_k[t], sh, one);
-  unsigned long long total = sum_from(last);
-  if (R.top_p && R.top_p[t] < 1.f) {
-    const double share = ceil((double)R.top_p[t] * (double)total);
-    const uint64_t p = reach<BF>(x, row, V, share >= 1.0 ? min((unsigned long long)share, total) : 1, sh, mass);
-    last = p > last ? p : last;
-  }
-  if (R.min_p && R.min_p[t] > 0.f) {
-    const double least = min((double)R.min_p[t], 1.0);
-    uint32_t lo = (uint32_t)(last >> 32), hi = (uint32_t)(first >> 32);  // of the values that may be kept, the smallest that is probable enough
     while (lo < hi) {
       const uint32_t mid = lo + (hi - lo) / 2;
-      if (exp(exponent(key_value(mid))) >= least) hi = mid;
+      if (enough(mid)) hi = mid;
       else lo = mid + 1;
     }
-    if (lo > (uint32_t)(last >> 32)) last = (uint64_t)lo << 32;
+    return value(lo);
   }
-  total = sum_from(last);
-  n = 0;
-  for (int c = threadIdx.x; c < V; c += kT) {
-    const float v = load1<BF>(x, row + c);
-    n += v > -INFINITY && place(v, c) >= last;
+};
+
+// What wave 0 makes of n places in order (in LDS) that weigh weights[0 .. n): sums up to every one, 64 runs of them side by side.
+struct Sums {
+  const unsigned long long *weights;
+  int n, per, lane;
+  unsigned long long before, own, total;
+  __device__ __forceinline__ Sums(const unsigned long long *w, int n_, int lane_) : weights(w), n(n_), lane(lane_) {
+    per = (n + 63) / 64;
+    own = 0;
+    for (int i = lane * per; i < min(n, lane * per + per); ++i) own += weights[i];
+    unsigned long long upto = own;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned long long u = __shfl_up(upto, o, 64);
+      if (lane >= o) upto += u;
+    }
+    before = upto - own;
+    total = __shfl(upto, 63, 64);
   }
-  n = block_add(n, sh);
-  const float u = uniform[t];
-  const unsigned long long at = u > 0.f ? min((unsigned long long)((double)u * (double)total), total - 1) : 0;
-  const uint64_t p = reach<BF>(x, row, V, at + 1, sh, mass);
-  if (threadIdx.x == 0) {
-    tokens[t] = (int32_t)(0xffffffffu - (uint32_t)p);
-    if (logprobs) logprobs[t] = (float)(exponent(key_value((uint32_t)(p >> 32))) - log((double)total / scale));
-    if (kept) kept[t] = (int32_t)n;
+  // the first of them up to which they weigh `target`, and what they do (target at most the total)
+  __device__ __forceinline__ int reach(unsigned long long target, unsigned long long &upto) const {
+    const uint64_t hit = __ballot(before + own >= target);
+    const int who = hit ? __builtin_ctzll(hit) : 63;
+    unsigned long long s = before;
+    int i = lane * per;
+    if (lane == who)
+      for (; i < n; ++i) {
+        s += weights[i];
+        if (s >= target) break;
+      }
+    upto = __shfl(s, who, 64);
+    return __shfl(i, who, 64);
   }
+  __device__ __forceinline__ unsigned long long upto(int count) const {  // what the first `count` weigh
+    unsigned long long s = 0;
+    for (int i = lane * per; i < min(count, min(n, lane * per + per)); ++i) s += weights[i];
+    return wave_add(s);
+  }
+};
+
+// A token a workgroup and row.  Where top_k says how many columns matter, these are found, put in order and weighed alone; otherwise the probabilities of the whole row are added up in bins of
+// their size, and the columns of the bin in which a sum (top_p's, the random number's) ends are put in order.
+template <int BF, int NT, int NV>
+__global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules rules, int32_t *tokens, float *logprobs, int32_t *kept) {
+  __shared__ Search<NT> sh;
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char *at_row = x + t * ld * Piece<BF>::ES;
+  using R = Row<BF, NT, NV>;
+  R row(at_row, V, R::aligned(at_row, V), tid, wave);
+  const float u = uniform[t], temp = rules.temperature ? rules.temperature[t] : 1.f, p = rules.top_p ? rules.top_p[t] : 1.f, m = rules.min_p ? rules.min_p[t] : 0.f;
+  const int k = rules.top_k ? rules.top_k[t] : 0;
+  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
+  float mine, top, low;
+  extremes(row, sh, wave, lane, mine, top, low);
+  auto answer = [&](int32_t token, double logprob, int n) {
+    tokens[t] = token;
+    if (logprobs) logprobs[t] = (float)logprob;
+    if (kept) kept[t] = n;
+  };
+  if (!(top > -INFINITY)) {
+    if (tid == 0) answer(-1, -INFINITY, 0);
+    return;
+  }
+  if (!(temp > 0.f) || k == 1) {
+    if (tid == 0) sh.found[0] = 0;
+    __syncthreads();
+    above(row, top, [&](float v, int c) { atomicMax(&sh.found[0], (unsigned long long)place(v, c)); });
+    __syncthreads();
+    if (tid == 0) answer(column_of(sh.found[0]), 0.0, 1);
+    return;
+  }
+  const Weigher mass{top, temp, 1.4426950408889634 / (double)temp, bits};
+  auto share = [&](double part, unsigned long long total) {  // the first sum that is part of the total or more
+    const double s = ceil(part * (double)total);
+    return s >= 1.0 ? min((unsigned long long)s, total) : 1ull;
+  };
+  auto draw_at = [&](unsigned long long total) { return u > 0.f ? min((unsigned long long)((double)u * (double)total), total - 1) + 1 : 1ull; };
+  auto logprob = [&](float v, unsigned long long total) { return mass.exponent(v) * 0.6931471805599453 - log(ldexp((double)total, -bits)); };
+  const float least = m > 0.f ? mass.smallest(m, lane) : -INFINITY;
+  if (k > 1 && k <= kTop && k < V) {
+    const float from = bound_of(row, f, k, mine, top, low);
+    const int n = from > -INFINITY ? collect(row, sh, from) : kList + 1;
+    if (n <= kList) {
+      const int kk = min(k, n);
+      f.sort(n, kk);
+      for (int i = tid; i < kk; i += NT) sh.list[i] = mass(value_of(sh.sorted[i]));
+      __syncthreads();
+      if (wave) return;
+      const Sums sums(sh.list, kk, lane);
+      unsigned long long upto = sums.total;
+      int count = kk;
+      if (p < 1.f) count = sums.reach(share(p, sums.total), upto) + 1;
+      if (m > 0.f) {
+        int enough = 0;
+        for (int i = lane; i < count; i += 64) enough += value_of(sh.sorted[i]) >= least;
+        count = wave_add(enough);
+        upto = sums.upto(count);
+      }
+      const unsigned long long total = upto;
+      const int i = sums.reach(draw_at(total), upto);
+      if (lane == 0) {
+        const uint64_t where = sh.sorted[i];
+        answer(column_of(where), logprob(value_of(where), total), count);
+      }
+      return;
+    }
+  }
+  auto one = [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; };
+  uint64_t last = 0;  // the last place that is kept
+  if (k > 1 && k < V) {
+    unsigned long long n = 0;
+    f.columns([&](float v, int) { n += v > -INFINITY; });
+    if ((unsigned long long)k < f.block_add(n)) last = f.reach(k, one);
+  }
+  // bins of equal width from the largest logit down to the smallest, or to where probabilities are below 2^-48
+  const float span = fminf(top - f.smallest(), 48.f * (float)(1.0 / mass.c)), scale = span > 0.f && span < INFINITY ? (kBins - 1) / span : 0.f;
+  auto bin = [&](float v) {
+    const float b = (top - v) * scale;
+    return b < (float)(kBins - 1) ? (int)b : kBins - 1;
+  };
+  __syncthreads();
+  f.clear(sh.bins.amount, kBins);
+  __syncthreads();
+  f.columns([&](float v, int c) {
+    if (last && place(v, c) < last) return;
+    const unsigned long long w = mass(v);
+    if (w) atomicAdd(&sh.bins.amount[bin(v)], w);
+  });
+  __syncthreads();
+  unsigned long long before, total;
+  f.find(sh.bins.amount, kBins, ~0ull, total);
+  bool binned = true;
+  // the place at which the sum from the first on reaches `target`, and the sum up to it
+  auto where = [&](unsigned long long target, unsigned long long &upto) -> uint64_t {
+    if (binned) {
+      __syncthreads();
+      const int b = f.find(sh.bins.amount, kBins, target, before);
+      __syncthreads();
+      if (tid == 0) sh.n = 0;
+      __syncthreads();
+      f.columns([&](float v, int c) {
+        if (!(v > -INFINITY) || bin(v) != b || place(v, c) < last) return;
+        const int i = atomicAdd(&sh.n, 1);
+        if (i < kList) sh.list[i] = place(v, c);
+      });
+      __syncthreads();
+      const int n = sh.n;
+      if (n <= kList) {
+        f.sort(n, n);
+        for (int i = tid; i < n; i += NT) sh.list[i] = mass(value_of(sh.sorted[i]));
+        __syncthreads();
+        if (wave == 0) {
+          unsigned long long s;
+          const int i = Sums(sh.list, n, lane).reach(target - before, s);
+          if (lane == 0) { sh.found[0] = sh.sorted[i]; sh.found[1] = before + s; }
+        }
+        __syncthreads();
+        upto = sh.found[1];
+        return sh.found[0];
+      }
+    }
+    binned = false;  // (reach takes the bins)
+    const uint64_t at = f.reach(target, [&](float v, uint64_t q) -> unsigned long long { return q >= last ? mass(v) : 0; });
+    unsigned long long s = 0;
+    f.columns([&](float v, int c) {
+      if (place(v, c) >= at) s += mass(v);
+    });
+    upto = f.block_add(s);
+    return at;
+  };
+  if (p < 1.f) last = where(share(p, total), total);
+  const uint64_t probable = m > 0.f ? place(least, (1 << kColumnBits) - 1) : 0;
+  if (probable > last) {
+    last = probable;
+    unsigned long long s = 0;
+    f.columns([&](float v, int) {
+      if (v >= least) s += mass(v);
+    });
+    total = f.block_add(s);
+  }
+  unsigned long long n = 0;
+  const float end = last ? value_of(last) : -3.402823466e38f;
+  const int end_column = last ? column_of(last) : V;
+  f.columns([&](float v, int c) { n += v > end || (v == end && c <= end_column); });
+  n = f.block_add(n);
+  unsigned long long upto;
+  const uint64_t at = where(draw_at(total), upto);
+  if (tid == 0) answer(column_of(at), logprob(value_of(at), total), (int)n);
 }
 
-template <int BF>
-__global__ __launch_bounds__(kT) void top_kernel(const void *x, int64_t ld, int V, int k, float inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
-  __shared__ unsigned long long sh[4], list[kTop];
-  __shared__ float shf[4];
-  __shared__ int count;
-  const int64_t row = blockIdx.x * ld, out = blockIdx.x * ldk;
+// The k largest of a row a workgroup: those above a bound that few columns reach, put in order.
+template <int BF, int NT, int NV>
+__global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
+  __shared__ Search<NT> sh;
+  __shared__ float part[NT / 64];
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char *at_row = x + t * ld * Piece<BF>::ES;
+  using R = Row<BF, NT, NV>;
+  R row(at_row, V, R::aligned(at_row, V), tid, wave);
+  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
+  float mine, top, low;
+  extremes(row, sh, wave, lane, mine, top, low);
   const int n = min(k, V);
-  const uint64_t last = n < V ? reach<BF>(x, row, V, n, sh, [](float) -> unsigned long long { return 1; }) : 0;
-  if (threadIdx.x == 0) count = 0;
-  __syncthreads();
-  float m = -INFINITY;
-  for (int c = threadIdx.x; c < V; c += kT) {
-    const float v = load1<BF>(x, row + c);
-    const uint64_t p = place(v, c);
-    if (p >= last) list[atomicAdd(&count, 1)] = p;
-    else m = fmaxf(m, v);
+  const float from = bound_of(row, f, n, mine, top, low);
+  int found = from > -INFINITY ? collect(row, sh, from) : 0;
+  uint64_t last = 0;
+  const bool bounded = found >= n && found <= kList;  // (otherwise: equal logits, or none)
+  if (!bounded) {
+    last = n < V ? f.reach(n, [](float, uint64_t) -> unsigned long long { return 1; }) : 0;
+    if (tid == 0) sh.n = 0;
+    __syncthreads();
+    f.columns([&](float v, int c) {
+      const uint64_t p = place(v, c);
+      if (p >= last) sh.list[atomicAdd(&sh.n, 1)] = p;
+    });
+    found = n;
+    __syncthreads();
   }
-  m = block_most(m, shf);
-  for (int i = threadIdx.x; i < k; i += kT) {
-    int at = i;
-    if (i < n) {
-      at = 0;
-      for (int j = 0; j < n; ++j) at += list[j] > list[i];
-    }
-    ids[out + at] = i < n ? (int32_t)(0xffffffffu - (uint32_t)list[i]) : -1;
-    values[out + at] = i < n ? key_value((uint32_t)(list[i] >> 32)) : -INFINITY;
+  f.sort(found, found);
+  const int64_t out = t * ldk;
+  for (int i = tid; i < k; i += NT) {
+    const uint64_t p = i < n ? sh.sorted[i] : 0;
+    ids[out + i] = i < n ? column_of(p) : -1;
+    values[out + i] = i < n ? value_of(p) : -INFINITY;
   }
   if (!rest) return;
-  float s = 0.f;
-  for (int c = threadIdx.x; c < V; c += kT) {
-    const float v = load1<BF>(x, row + c);
-    if (place(v, c) < last && v > -INFINITY) s += v == m ? 1.f : __expf((v - m) * inv_temp);
+  auto others = [&](auto g) {  // of every column that is not among the k
+    if (bounded) {
+      row.each([&](const Piece<BF> &y, int) {
+#pragma unroll
+        for (int e = 0; e < Piece<BF>::N; ++e) g(y[e] < from ? y[e] : -INFINITY);
+      });
+      g(row.xl < from ? row.xl : -INFINITY);
+      for (int i = n + tid; i < found; i += NT) g(value_of(sh.sorted[i]));
+    } else
+      f.columns([&](float v, int c) { g(v > -INFINITY && place(v, c) < last ? v : -INFINITY); });
+  };
+  auto block = [&](float v, bool sum) {
+    v = sum ? wave_add(v) : wave_max(v);
+    __syncthreads();
+    if (lane == 0) part[wave] = v;
+    __syncthreads();
+    v = part[0];
+    for (int w = 1; w < NT / 64; ++w) v = sum ? v + part[w] : fmaxf(v, part[w]);
+    return v;
+  };
+  const float c = (float)(1.4426950408889634 * inv_temp);
+  auto sum = [&](float ref) {
+    float s = 0.f;
+    others([&](float v) { s += v == ref ? 1.f : __builtin_amdgcn_exp2f((v - ref) * c); });
+    return block(s, true);
+  };
+  // against the smallest of the k, which is near the largest of the others as a rule
+  float ref = value_of(sh.sorted[n - 1]), s = ref > -INFINITY && ref < INFINITY ? sum(ref) : 0.f;
+  if (!(s > 0.02f)) {
+    float m = -INFINITY;
+    others([&](float v) { m = fmaxf(m, v); });
+    ref = block(m, false);
+    s = ref > -INFINITY ? sum(ref) : 0.f;
   }
-  s = block_add(s, shf);
-  if (threadIdx.x == 0) rest[blockIdx.x] = m > -INFINITY ? m * inv_temp + logf(s) : -INFINITY;
+  if (tid == 0) rest[t] = ref > -INFINITY ? (float)((double)ref * inv_temp + log((double)s)) : -INFINITY;
 }
+
+// The kernel whose registers hold a row: few rows get more threads each.
+#define ROWS_BF16(LAUNCH)                              \
+  do {                                                 \
+    if (V <= 4 * 8 * 256) LAUNCH(1, 256, 4);           \
+    else if (T > 512 && V <= 16 * 8 * 256) LAUNCH(1, 256, 16); \
+    else if (T > 512 && V <= 16 * 8 * 512) LAUNCH(1, 512, 16); \
+    else if (V <= 4 * 8 * 1024) LAUNCH(1, 1024, 4);    \
+    else if (V <= 8 * 8 * 1024) LAUNCH(1, 1024, 8);    \
+    else LAUNCH(1, 1024, 0);                           \
+  } while (0)
+#define ROWS_F32(LAUNCH)                               \
+  do {                                                 \
+    if (V <= 4 * 4 * 256) LAUNCH(0, 256, 4);           \
+    else if (T > 512 && V <= 16 * 4 * 256) LAUNCH(0, 256, 16); \
+    else if (V <= 4 * 4 * 1024) LAUNCH(0, 1024, 4);    \
+    else if (V <= 16 * 4 * 1024) LAUNCH(0, 1024, 16);  \
+    else LAUNCH(0, 1024, 0);                           \
+  } while (0)
 
 twist_status check_rows(twist_ctx *ctx, const char *who, int64_t ld, int T) {
   const int V = ctx->d.vocab;
@@ -185,8 +583,11 @@ extern "C" twist_status twist_draw_raw(twist_ctx *ctx, const void *logits, int64
   int bits = 51;  // no row's sum reaches 2^63
   while (V > (int64_t)1 << (62 - bits)) --bits;
   const twist_draw_rules r = rules ? *rules : twist_draw_rules{};
-  if (ctx->d.dtype == TWIST_BF16 && !logits_f32) hipLaunchKernelGGL((draw_kernel<1>), dim3(T), dim3(kT), 0, ctx->stream, logits, ld, V, bits, uniform, r, tokens, logprobs, kept);
-  else hipLaunchKernelGGL((draw_kernel<0>), dim3(T), dim3(kT), 0, ctx->stream, logits, ld, V, bits, uniform, r, tokens, logprobs, kept);
+#define DRAW(BF, NT, NV) \
+  hipLaunchKernelGGL((draw_kernel<BF, NT, NV>), dim3(T), dim3(NT), 0, ctx->stream, static_cast<const char *>(logits), ld, V, bits, uniform, r, tokens, logprobs, kept)
+  if (ctx->d.dtype == TWIST_BF16 && !logits_f32) ROWS_BF16(DRAW);
+  else ROWS_F32(DRAW);
+#undef DRAW
   TW_HIP(ctx, hipGetLastError());
   return TWIST_OK;
 }
@@ -199,9 +600,13 @@ extern "C" twist_status twist_top_logits_raw(twist_ctx *ctx, const void *logits,
   if (k < 1 || k > kTop) TW_FAIL(ctx, TWIST_ESHAPE, "%s: lists of %d entries (1 to %d)", who, k, kTop);
   if (ldk < k) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows of the lists overlap", who);
   if (!(temperature > 0.f && temperature < INFINITY)) TW_FAIL(ctx, TWIST_EINVAL, "%s: the temperature must be above 0 and finite", who);
-  const float inv = 1.f / temperature;
-  if (ctx->d.dtype == TWIST_BF16 && !logits_f32) hipLaunchKernelGGL((top_kernel<1>), dim3(T), dim3(kT), 0, ctx->stream, logits, ld, ctx->d.vocab, k, inv, ids, values, ldk, rest);
-  else hipLaunchKernelGGL((top_kernel<0>), dim3(T), dim3(kT), 0, ctx->stream, logits, ld, ctx->d.vocab, k, inv, ids, values, ldk, rest);
+  const int V = ctx->d.vocab;
+  const double inv = 1.0 / (double)temperature;
+#define TOP(BF, NT, NV) \
+  hipLaunchKernelGGL((top_kernel<BF, NT, NV>), dim3(T), dim3(NT), 0, ctx->stream, static_cast<const char *>(logits), ld, V, k, inv, ids, values, ldk, rest)
+  if (ctx->d.dtype == TWIST_BF16 && !logits_f32) ROWS_BF16(TOP);
+  else ROWS_F32(TOP);
+#undef TOP
   TW_HIP(ctx, hipGetLastError());
   return TWIST_OK;
 }
