@@ -473,6 +473,15 @@ typedef struct {
   float temperature;    /* > 0: teacher's and student's logits are divided by it */
   float weight;         /* 0 to 1: the teacher's share of the loss; the targets have the others */
 } twist_teacher;
+/* Learning from a teacher, such as the whole model its subnets were taken from: twist_subnet_top_logits runs the forward half of twist_subnet_forward on one batch and leaves the
+ * k largest logits of each of its B * N positions (twist_top_logits_raw; any storage mode, no loss), and twist_subnet_fwd_bwd_distill is twist_subnet_fwd_bwd with the loss of
+ * twist_distill_raw against such lists, in the order of the positions.  Inputs, workspace and errors as theirs, and those of the two calls below; targets may be NULL at weight 1.
+ * TWIST_ESHAPE without a vocabulary. */
+TWIST_API twist_status twist_subnet_top_logits(twist_ctx *ctx, twist_subnet *sub, const void *inputs, int32_t B, int32_t N, int32_t k, float temperature, int32_t *ids,
+                                               float *values, int64_t ldk, float *rest, void *workspace, size_t workspace_bytes);
+TWIST_API twist_status twist_subnet_fwd_bwd_distill(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets, const twist_teacher *teacher, int32_t B, int32_t N,
+                                                    void *workspace, size_t workspace_bytes, float *loss_dev);
+
 /* The loss of T rows of a student's logits [T, vocab] (dtype, rows ld apart) and its gradient.  With the teacher's probabilities q of its entries, and of all its other tokens together (rest), and
  * the student's p of the same, both at the temperature, row t counts
  *     weight * temperature^2 * sum q (log q - log p)  +  (1 - weight) * cross-entropy(logits, targets[t])

@@ -190,7 +190,7 @@ def scale_factors(cfg, lw, scale_mode):
     return math.sqrt(cfg.n_heads / h_sub), math.sqrt(cfg.n_ffn_units / u_sub)
 
 
-def forward_backward(cfg, P, inputs, targets, scale_mode=True, q=_ident, need_grads=True, return_out=False):
+def forward_backward(cfg, P, inputs, targets, scale_mode=True, q=_ident, need_grads=True, return_out=False, loss_of=cross_entropy):
     """loss, grads (same nesting as P).  inputs: int tokens [B,N] or activations [B,N,d]."""
     dh = cfg.d_head
     G = P["globals"]
@@ -247,7 +247,7 @@ def forward_backward(cfg, P, inputs, targets, scale_mode=True, q=_ident, need_gr
         W_out = G["tok_embed"] if cfg.tied_head else G["lm_head"]
         logits = q("logits", hf @ W_out.T)                                    # [B,N,V]
         tgt = np.asarray(targets)
-        loss, dlogits = cross_entropy(logits, tgt)
+        loss, dlogits = loss_of(logits, tgt)
     else:
         Y = np.asarray(targets, dtype=np.float64)
         loss = float(((X - Y) ** 2).mean())

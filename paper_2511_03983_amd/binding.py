@@ -141,6 +141,8 @@ _SIGS = {
     "twist_cache_attention_floats": ([_vp, C.POINTER(PagesC), _i32, _i32, _i32, C.POINTER(_sz)], _i32),
     "twist_cache_attention_raw": ([_vp, C.POINTER(PagesC), _vp, _vp, C.c_int64, _vp, C.c_int64, _i32, _i32, _vp, _vp, _i32, _vp, C.c_int64, _vp, _vp, _sz], _i32),
     "twist_logits_raw": ([_vp, _vp, C.c_int64, _i32, C.POINTER(LogitRulesC), _vp, C.c_int64], _i32),
+    "twist_subnet_top_logits": ([_vp, _vp, _vp, _i32, _i32, _i32, C.c_float, _vp, _vp, C.c_int64, _vp, _vp, _sz], _i32),
+    "twist_subnet_fwd_bwd_distill": ([_vp, _vp, _vp, _vp, C.POINTER(TeacherC), _i32, _i32, _vp, _sz, _vp], _i32),
     "twist_draw_raw": ([_vp, _vp, C.c_int64, _i32, _i32, _vp, C.POINTER(DrawRulesC), _vp, _vp, _vp], _i32),
     "twist_top_logits_raw": ([_vp, _vp, C.c_int64, _i32, _i32, _i32, C.c_float, _vp, _vp, C.c_int64, _vp], _i32),
     "twist_distill_raw": ([_vp, _vp, C.c_int64, _vp, _i32, C.POINTER(TeacherC), _vp, C.c_int64, _vp, _vp], _i32),
@@ -325,6 +327,31 @@ class Context:
         self._call(lib.twist_subnet_decode, sub.h, _ints(tokens, T, "tokens", self.gpu), T, _ints(seq, T, "seq", self.gpu), _ints(lens, T, "lens", self.gpu), max_len,
                    pages.ref, *_storage(cache, "cache", self.gpu), *_storage(workspace, "workspace", self.gpu), logits.data_ptr(), ldl)
         return logits
+
+    def _batch(self, t, what):
+        """(B, N) of a batch of token ids on the context's GPU."""
+        if t.dtype is not torch.int32 or t.dim() != 2 or not t.is_contiguous() or t.get_device() != self.gpu:
+            _refuse(f"{what}: needs contiguous int32 [B, N] on {self.device}")
+        return t.shape
+
+    def twist_subnet_top_logits(self, sub: "Subnet", inputs: torch.Tensor, k: int, workspace: torch.Tensor, temperature: float = 1.0):
+        """(ids int32 [B*N, k], values fp32 [B*N, k], rest fp32 [B*N]) of the positions of inputs [B, N]: what a Teacher is made of.  See include/twist.h."""
+        B, N = self._batch(inputs, "inputs")
+        ids, values, rest = self._empty(torch.int32, B * N, max(k, 1)), self._empty(torch.float32, B * N, max(k, 1)), self._empty(torch.float32, B * N)
+        self._call(lib.twist_subnet_top_logits, sub.h, inputs.data_ptr(), B, N, k, temperature, ids.data_ptr(), values.data_ptr(), max(k, 1), rest.data_ptr(),
+                   *_storage(workspace, "workspace", self.gpu))
+        return ids, values, rest
+
+    def twist_subnet_fwd_bwd_distill(self, sub: "Subnet", inputs: torch.Tensor, targets: torch.Tensor | None, teacher: "Teacher", workspace: torch.Tensor, loss: torch.Tensor) -> None:
+        """twist_subnet_fwd_bwd with the loss of twist_distill_raw against the teacher's B * N lists (targets: None with weight 1).  See include/twist.h."""
+        B, N = self._batch(inputs, "inputs")
+        if targets is not None and self._batch(targets, "targets") != (B, N):
+            _refuse(f"targets: need [{B}, {N}]")
+        if teacher.T != B * N or teacher.gpu != self.gpu:
+            _refuse(f"teacher: needs {B * N} rows on {self.device}")
+        if loss.dtype is not torch.float32 or loss.get_device() != self.gpu or loss.numel() < 1:
+            _refuse(f"loss: needs an fp32 number on {self.device}")
+        self._call(lib.twist_subnet_fwd_bwd_distill, sub.h, inputs.data_ptr(), _addr(targets), teacher.ref, B, N, *_storage(workspace, "workspace", self.gpu), loss.data_ptr())
 
     def twist_subnet_step(self, sub: "Subnet", kind=OPT_SGD, lr=1e-2, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0) -> None:
         od = OptDesc(kind, lr, beta1, beta2, eps, weight_decay)

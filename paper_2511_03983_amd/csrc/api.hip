@@ -957,6 +957,31 @@ extern "C" twist_status twist_subnet_forward(twist_ctx *ctx, twist_subnet *sub, 
   return twist_train_fwd_bwd(ctx, sub, inputs, targets, B, N, workspace, workspace_bytes, loss_dev, true);
 }
 
+extern "C" twist_status twist_subnet_top_logits(twist_ctx *ctx, twist_subnet *sub, const void *inputs, int32_t B, int32_t N, int32_t k, float temperature, int32_t *ids,
+                                                float *values, int64_t ldk, float *rest, void *workspace, size_t workspace_bytes) {
+  const char *who = "twist_subnet_top_logits";
+  if (!ctx || !sub || !inputs || !ids || !values || !workspace) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
+  if (sub->ctx != ctx) TW_FAIL(ctx, TWIST_EINVAL, "%s: subnet belongs to another context", who);
+  if (B < 1 || N < 1 || (int64_t)B * N >= 1 << 22) TW_FAIL(ctx, TWIST_ESHAPE, "%s: batch of %d x %d tokens", who, B, N);
+  TW_TRY(twist_check_top(ctx, who, ctx->d.vocab, B * N, k, temperature, ldk));
+  LogitsUse use;
+  use.k = k; use.temperature = temperature; use.ids = ids; use.values = values; use.ldk = ldk; use.rest = rest;
+  return twist_train_fwd_bwd(ctx, sub, inputs, nullptr, B, N, workspace, workspace_bytes, nullptr, true, nullptr, 0, &use);
+}
+
+extern "C" twist_status twist_subnet_fwd_bwd_distill(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets, const twist_teacher *teacher, int32_t B, int32_t N,
+                                                     void *workspace, size_t workspace_bytes, float *loss_dev) {
+  const char *who = "twist_subnet_fwd_bwd_distill";
+  if (!ctx || !sub || !inputs || !teacher || !workspace || !loss_dev) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
+  if (sub->ctx != ctx) TW_FAIL(ctx, TWIST_EINVAL, "%s: subnet belongs to another context", who);
+  if (B < 1 || N < 1 || (int64_t)B * N >= 1 << 22) TW_FAIL(ctx, TWIST_ESHAPE, "%s: batch of %d x %d tokens", who, B, N);
+  TW_TRY(twist_check_teacher(ctx, who, teacher, B * N, ctx->d.vocab));
+  if (teacher->weight < 1.f && !targets) TW_FAIL(ctx, TWIST_EINVAL, "%s: targets are missing", who);
+  LogitsUse use;
+  use.teacher = teacher;
+  return twist_train_fwd_bwd(ctx, sub, inputs, targets, B, N, workspace, workspace_bytes, loss_dev, false, nullptr, 0, &use);
+}
+
 extern "C" twist_status twist_subnet_step(twist_ctx *ctx, twist_subnet *sub, const twist_opt_desc *opt) {
   if (!ctx || !sub || !opt) TW_FAIL(ctx, TWIST_EINVAL, "twist_subnet_step: null argument");
   if (sub->ctx != ctx) TW_FAIL(ctx, TWIST_EINVAL, "twist_subnet_step: subnet belongs to another context");

@@ -592,14 +592,19 @@ extern "C" twist_status twist_draw_raw(twist_ctx *ctx, const void *logits, int64
   return TWIST_OK;
 }
 
-extern "C" twist_status twist_top_logits_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t logits_f32, int32_t T, int32_t k, float temperature, int32_t *ids,
-                                             float *values, int64_t ldk, float *rest) {
-  const char *who = "twist_top_logits_raw";
-  if (!ctx || !logits || !ids || !values) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
+twist_status twist_check_top(twist_ctx *ctx, const char *who, int64_t ld, int T, int k, float temperature, int64_t ldk) {
   TW_TRY(check_rows(ctx, who, ld, T));
   if (k < 1 || k > kTop) TW_FAIL(ctx, TWIST_ESHAPE, "%s: lists of %d entries (1 to %d)", who, k, kTop);
   if (ldk < k) TW_FAIL(ctx, TWIST_ESHAPE, "%s: rows of the lists overlap", who);
   if (!(temperature > 0.f && temperature < INFINITY)) TW_FAIL(ctx, TWIST_EINVAL, "%s: the temperature must be above 0 and finite", who);
+  return TWIST_OK;
+}
+
+extern "C" twist_status twist_top_logits_raw(twist_ctx *ctx, const void *logits, int64_t ld, int32_t logits_f32, int32_t T, int32_t k, float temperature, int32_t *ids,
+                                             float *values, int64_t ldk, float *rest) {
+  const char *who = "twist_top_logits_raw";
+  if (!ctx || !logits || !ids || !values) TW_FAIL(ctx, TWIST_EINVAL, "%s: null argument", who);
+  TW_TRY(twist_check_top(ctx, who, ld, T, k, temperature, ldk));
   const int V = ctx->d.vocab;
   const double inv = 1.0 / (double)temperature;
 #define TOP(BF, NT, NV) \

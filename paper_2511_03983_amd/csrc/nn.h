@@ -169,9 +169,6 @@ twist_status twist_mean(twist_ctx *ctx, const float *v, int64_t n, float scale, 
 // the loss of twist_distill_raw and its gradient, which may overwrite the logits; columns V .. pad - 1 of the gradient's rows are cleared
 twist_status twist_distill(twist_ctx *ctx, const char *who, int bf16, const void *logits, int64_t ld, const int32_t *targets, int T, int V, const twist_teacher *teacher, void *grad,
                            int64_t ldg, int64_t pad, float *rowloss, float *loss);
-// what twist_distill refuses of a teacher and its rows
-twist_status twist_check_teacher(twist_ctx *ctx, const char *who, const twist_teacher *teacher, int T, int V);
-
 twist_status twist_sgd(twist_ctx *ctx, int bf16, void *params, float *master, const float *grads, int64_t n, float lr);
 twist_status twist_adamw(twist_ctx *ctx, int bf16, void *params, float *master, const float *grads, float *m, float *v, int64_t n, int64_t n_decay,
                          float lr, float b1, float b2, float eps, float wd, int64_t step);

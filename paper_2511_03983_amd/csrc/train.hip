@@ -285,7 +285,7 @@ bool twist_train_masked_compact(const twist_ctx *ctx, const twist_plan *plan, in
 }
 
 twist_status twist_train_fwd_bwd(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets, int B, int N, void *ws,
-                                 size_t ws_bytes, float *loss_dev, bool forward_only, const twist_plan *mask_plan, int mask_row) {
+                                 size_t ws_bytes, float *loss_dev, bool forward_only, const twist_plan *mask_plan, int mask_row, const LogitsUse *use) {
   TW_TRY(check_train_shape(ctx, sub, B, N));
   if (!forward_only && !sub->grads) TW_FAIL(ctx, TWIST_ESHAPE, "fwd_bwd: subnet was extracted without gradient storage");
   if (reinterpret_cast<uintptr_t>(ws) % 256) TW_FAIL(ctx, TWIST_ESHAPE, "fwd_bwd: workspace must be 256-byte aligned");
@@ -432,7 +432,7 @@ twist_status twist_train_fwd_bwd(twist_ctx *ctx, twist_subnet *sub, const void *
     {
       GemmEpilogue e;
       e.out = w.logits;
-      if (forward_only) {
+      if (forward_only && !use) {
         e.targets = static_cast<const int32_t *>(targets);
         e.loss_parts = static_cast<float *>(w.logits);  // (8 bytes for 64 columns or more: they fit the logits' place)
         e.target_logit = w.rowloss;
@@ -441,7 +441,10 @@ twist_status twist_train_fwd_bwd(twist_ctx *ctx, twist_subnet *sub, const void *
       TW_TRY(twist_gemm(ctx, bf, GEMM_NT, T, V, D, w.hf, D, P(wout), D, w.ld_logits, e));
     }
     if (blocks) return twist_ce_parts(ctx, static_cast<const float *>(w.logits), blocks, w.rowloss, loss_dev, T);
-    TW_TRY(twist_ce_fwd_bwd(ctx, bf, w.logits, w.ld_logits, static_cast<const int32_t *>(targets), w.rowloss, loss_dev, T, V, !forward_only));
+    if (use && !use->teacher) return twist_top_logits_raw(ctx, w.logits, w.ld_logits, 0, T, use->k, use->temperature, use->ids, use->values, use->ldk, use->rest);
+    if (use) TW_TRY(twist_distill(ctx, "fwd_bwd", bf, w.logits, w.ld_logits, static_cast<const int32_t *>(targets), T, V, use->teacher, w.logits, w.ld_logits, w.ld_logits, w.rowloss,
+                                  loss_dev));
+    else TW_TRY(twist_ce_fwd_bwd(ctx, bf, w.logits, w.ld_logits, static_cast<const int32_t *>(targets), w.rowloss, loss_dev, T, V, !forward_only));
     if (forward_only) return TWIST_OK;
     // projection weight gradient, then the gradient flowing back into the final norm
     TW_TRY(gemm(GEMM_TN, V, D, T, w.logits, w.ld_logits, w.hf, D, G(wout), D, 1));

@@ -163,8 +163,21 @@ twist_status twist_launch_zero(twist_ctx *ctx, void *dst, size_t bytes);
 
 // ---------------------------------------------------------------------------------------------- training
 twist_status twist_train_workspace_bytes(twist_ctx *ctx, const twist_subnet *sub, int B, int N, size_t *bytes);
+// what the loss against a teacher refuses of it and its rows, and twist_top_logits_raw of its lists
+twist_status twist_check_teacher(twist_ctx *ctx, const char *who, const twist_teacher *teacher, int T, int V);
+twist_status twist_check_top(twist_ctx *ctx, const char *who, int64_t ld, int T, int k, float temperature, int64_t ldk);
+// What a pass does with its logits instead of forming the cross-entropy: the loss against a teacher's lists (targets may be null at weight 1), or, without a backward half, lists of its
+// own (targets and loss are null).
+struct LogitsUse {
+  const twist_teacher *teacher = nullptr;
+  int32_t k = 0;
+  float temperature = 1.f;
+  int32_t *ids = nullptr;
+  float *values = nullptr, *rest = nullptr;
+  int64_t ldk = 0;
+};
 twist_status twist_train_fwd_bwd(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets, int B,
                                  int N, void *ws, size_t ws_bytes, float *loss_dev, bool forward_only = false,
-                                 const twist_plan *mask_plan = nullptr, int mask_row = 0);
+                                 const twist_plan *mask_plan = nullptr, int mask_row = 0, const LogitsUse *use = nullptr);
 bool twist_train_masked_compact(const twist_ctx *ctx, const twist_plan *plan, int B, int N);
 twist_status twist_train_step(twist_ctx *ctx, twist_subnet *sub, const twist_opt_desc *opt);
