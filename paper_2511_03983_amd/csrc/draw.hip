@@ -52,6 +52,18 @@ template <int NT> struct Search {
   int n;
 };
 
+// A value that all lanes have, known to be one: what depends on it is a branch of all
+__device__ __forceinline__ int uniform_of(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ float uniform_of(float v) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(v))); }
+__device__ __forceinline__ unsigned long long uniform_of(unsigned long long v) {
+  return (unsigned long long)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+}
+
+template <int NT> __device__ __forceinline__ Search<NT> &shared() {
+  __shared__ Search<NT> s;
+  return s;
+}
+
 // A workgroup's steps over a row that it reads again for every pass: what is seldom needed, or takes long in any case.  Nothing here touches the row in registers.
 template <int BF, int NT> struct Finder {
   using P16 = Piece<BF>;
@@ -65,14 +77,28 @@ template <int BF, int NT> struct Finder {
     pieces = (V - head) / N;
     first = row + head * P16::ES;
   }
-  // f(logit, column) of every column of the row
+  // f(logit, column) of every column of the row, whose pieces are read some at a time while those before them are at work
   template <class F> __device__ __forceinline__ void columns(F f) const {
-#pragma unroll 1
-    for (int v = tid; v < pieces; v += NT) {
-      P16 y;
-      y.load(first + (int64_t)v * 16);
+    constexpr int B = 4;
+    P16 next[B];
+    auto load = [&](int v) {
 #pragma unroll
-      for (int e = 0; e < N; ++e) f(y[e], head + v * N + e);
+      for (int b = 0; b < B; ++b)
+        if (v + b * NT < pieces) next[b].load(first + (int64_t)(v + b * NT) * 16);
+    };
+    load(tid);
+#pragma unroll 1
+    for (int v = tid; v < pieces; v += B * NT) {
+      P16 y[B];
+#pragma unroll
+      for (int b = 0; b < B; ++b) y[b] = next[b];
+      load(v + B * NT);
+#pragma unroll
+      for (int b = 0; b < B; ++b)
+        if (v + b * NT < pieces) {
+#pragma unroll
+          for (int e = 0; e < N; ++e) f(y[b][e], head + (v + b * NT) * N + e);
+        }
     }
     const int c = tid < head ? tid : pieces * N + tid;
     if (c < V && tid < V - pieces * N) f(load1<BF>(row, c), c);
@@ -85,7 +111,7 @@ template <int BF, int NT> struct Finder {
     unsigned long long s = 0;
 #pragma unroll 4
     for (int w = 0; w < NW; ++w) s += sh.wave_sum[w];
-    return s;
+    return uniform_of(s);
   }
   template <class T> __device__ __forceinline__ void clear(T *bins, int n) const {
     for (int i = tid; i < n; i += NT) bins[i] = 0;
@@ -114,8 +140,8 @@ template <int BF, int NT> struct Finder {
       }
     }
     __syncthreads();
-    before = sh.found[1];
-    return (int)sh.found[0];
+    before = uniform_of(sh.found[1]);
+    return uniform_of((int)sh.found[0]);
   }
 
   // The last place of the shortest beginning of the row whose columns' amounts add up to `target` (at least 1, at most the whole row's), a few bits of the places at a time.
@@ -144,22 +170,29 @@ template <int BF, int NT> struct Finder {
     __syncthreads();
     return prefix;
   }
-  // the smallest logit above -infinity
-  __device__ __forceinline__ float smallest() const {
-    float l = INFINITY;
-    columns([&](float v, int) { l = v > -INFINITY ? fminf(l, v) : l; });
+  // the row's largest logit and the smallest above -infinity
+  __device__ __forceinline__ void extremes(float &top, float &least) const {
+    float m = -INFINITY, l = INFINITY;
+    columns([&](float v, int) {
+      m = fmaxf(m, v);
+      l = v > -INFINITY ? fminf(l, v) : l;
+    });
+    m = wave_max(m);
     l = -wave_max(-l);
     __syncthreads();
-    if (lane == 0) sh.least[wave] = l;
+    if (lane == 0) { sh.most[wave] = m; sh.least[wave] = l; }
     __syncthreads();
 #pragma unroll
-    for (int w = 0; w < NW; ++w) l = fminf(l, sh.least[w]);
-    return l;
+    for (int w = 0; w < NW; ++w) { m = fmaxf(m, sh.most[w]); l = fminf(l, sh.least[w]); }
+    top = uniform_of(m);
+    least = uniform_of(l);
   }
   // A logit that k columns at least are not below (none above -infinity is, where there are fewer), by counting all in bins.  -infinity: no bins for them.
-  __device__ __forceinline__ float bound_of_all(int k, float top) const {
-    const float l = smallest(), span = top - l;
-    if (!(span < INFINITY)) return -INFINITY;
+  __device__ __forceinline__ float bound_of_all(int k) const {
+    float top, l;
+    extremes(top, l);
+    const float span = top - l;
+    if (!(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
     const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
     clear(sh.bins.count, kBins);
     __syncthreads();
@@ -178,7 +211,8 @@ template <int BF, int NT> struct Finder {
     return e - (4e-7f * (fabsf(top) + fabsf(e)) + 1e-37f);
   }
   // Puts the list's n places in order, in sh.sorted: the first `most` of them.
-  __device__ __forceinline__ void sort(int n, int most) const {
+  __device__ __forceinline__ void sort(int n, int most) const { sort(sh, tid, n, most); }
+  static __device__ __forceinline__ void sort(Search<NT> &sh, int tid, int n, int most) {
 #pragma unroll 1
     for (int i = tid; i < n; i += NT) {
       const unsigned long long p = sh.list[i];
@@ -212,29 +246,28 @@ template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Sear
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) { top = fmaxf(top, sh.most[w]); low = fminf(low, sh.least[w]); }
+  top = uniform_of(top);
+  low = uniform_of(low);
 }
-// A logit that k columns at least are not below, and not many more where logits differ, by counting in bins the threads' largest, the pieces' or all.  -infinity: none was found.
+// A logit that k columns at least are not below, and not many more where logits differ, by counting in bins the threads' largest or the pieces'.  -infinity: none was found.
 template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &row, const Finder<BF, NT> &f, int k, float mine, float top, float low) {
   const float span = top - low;
-  if (!(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
-  if (k <= NT / 2) {
-    const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
-    f.clear(f.sh.bins.count, kBins);
-    __syncthreads();
-    auto put = [&](float v) {
-      if (v >= low) atomicAdd(&f.sh.bins.count[(int)((top - v) * scale)], 1u);
-    };
-    if (8 * k <= NT) put(mine);
-    else {
-      row.each([&](const typename R::P16 &y, int) { put(y.most()); });
-      put(row.xl);
-    }
-    __syncthreads();
-    unsigned long long before;
-    const int b = f.find(f.sh.bins.count, kBins, k, before);
-    if (b < kBins) return f.edge(b, top, scale);
+  if (k > NT || !(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
+  const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
+  f.clear(f.sh.bins.count, kBins);
+  __syncthreads();
+  auto put = [&](float v) {
+    if (v >= low) atomicAdd(&f.sh.bins.count[(int)((top - v) * scale)], 1u);
+  };
+  if (8 * k <= NT) put(mine);
+  else {
+    row.each([&](const typename R::P16 &y, int) { put(y.most()); });
+    put(row.xl);
   }
-  return f.bound_of_all(k, top);
+  __syncthreads();
+  unsigned long long before;
+  const int b = f.find(f.sh.bins.count, kBins, k, before);
+  return b < kBins ? f.edge(b, top, scale) : -INFINITY;
 }
 // the list from the columns at `from` and above; their number, which may be more than the list holds
 template <int NT, class R> __device__ __forceinline__ int collect(R &row, Search<NT> &sh, float from) {
@@ -246,15 +279,43 @@ template <int NT, class R> __device__ __forceinline__ int collect(R &row, Search
     if (i < kList) sh.list[i] = place(v, c);
   });
   __syncthreads();
-  return sh.n;
+  return uniform_of(sh.n);
+}
+
+// The list of a row's k first places (k at most its columns; in any order, and more where that is as quick), by counting all of its columns in bins, or else bit by bit; their number.  Every
+// column of the list is before all others.  A function of its own, which leaves the registers of the quicker way alone.
+template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(const char *at_row, int V, int head, int wave, int k) {
+  Search<NT> &sh = shared<NT>();
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  const float from = f.bound_of_all(k);
+  int n = 0;
+  auto list = [&](auto may) {
+    __syncthreads();
+    if (f.tid == 0) sh.n = 0;
+    __syncthreads();
+    f.columns([&](float v, int c) {
+      if (!may(v, c)) return;
+      const int i = atomicAdd(&sh.n, 1);
+      if (i < kList) sh.list[i] = place(v, c);
+    });
+    __syncthreads();
+    return uniform_of(sh.n);
+  };
+  if (from > -INFINITY) n = list([&](float v, int) { return v >= from; });
+  if (n < k || n > kList) {
+    const uint64_t last = k < V ? f.reach(k, [](float, uint64_t) -> unsigned long long { return 1; }) : 0;
+    n = list([&](float v, int c) { return place(v, c) >= last; });
+  }
+  return n;
 }
 
 // One row's settings and what follows from them: probabilities are whole multiples of 2^-bits of the largest, in 64 bits, so that any order of their sums gives the same.
 struct Weigher {
-  float top, temp;
+  float top;
   double c;  // log2(e) / temperature
   int bits;
   __device__ __forceinline__ double exponent(float v) const { return v == top ? 0.0 : ((double)v - (double)top) * c; }  // of 2
+  __device__ __forceinline__ double logarithm(float v, unsigned long long total) const { return exponent(v) * 0.6931471805599453 - log(ldexp((double)total, -bits)); }
   __device__ __forceinline__ unsigned long long operator()(float v) const {
     if (!(v > -INFINITY)) return 0;
     // (added to 2^52 the number is rounded to whole ones, which its last 52 bits are)
@@ -278,6 +339,32 @@ struct Weigher {
       else lo = mid + 1;
     }
     return value(lo);
+  }
+};
+
+// The same for whole rows, in half the instructions (an exponential of power2 takes 25, several of which run at a fraction of the rate): 2^(n / 512) from a table, the rest of the exponent by a
+// polynomial of degree 3 (2^-48 off).  Not for every row: `usable` tells.
+constexpr int kTable = 512;
+struct QuickWeigher {
+  double top, c;  // 512 log2(e) / temperature
+  float least;    // below it nothing weighs anything
+  const double *table;
+  bool usable;
+  __device__ __forceinline__ QuickWeigher(const Weigher &w, const double *t) : top(w.top), c(w.c * kTable), table(t) {
+    least = fmaxf((float)(top - 190.0 / w.c), -3.402823466e38f);
+    const double span = (top - (double)least) * w.c;  // (rounded to fp32 it may be anything, for instance where the temperature is next to nothing)
+    usable = w.top < INFINITY && span <= 250.0 && (span >= 100.0 || least == -3.402823466e38f);
+  }
+  static __device__ __forceinline__ double entry(int i, int bits) { return power2((double)i / kTable - 1.0, bits + 1); }  // of the table
+  __device__ __forceinline__ unsigned long long operator()(float v) const {
+    const double d = (double)fmaxf(v, least) - top;
+    const double m = fma(d, c, 6755399441055744.0), r = fma(d, c, -(m - 6755399441055744.0));  // (1.5 2^52: rounds to whole numbers, which the last bits are)
+    const int n = __double2loint(m);
+    double q = fma(r, 4.1353784691025013e-10, 9.163914342180769e-07);
+    q = fma(q, r, 0.0013538030870311425);
+    q = fma(q, r, 1.0) * table[n & (kTable - 1)];
+    q = __hiloint2double(__double2hiint(q) + (n >> 9 << 20), __double2loint(q)) + 4503599627370496.0;
+    return v > -INFINITY ? (unsigned long long)__double_as_longlong(q) & 0xfffffffffffffull : 0;
   }
 };
 
@@ -320,116 +407,94 @@ struct Sums {
   }
 };
 
-// A token a workgroup and row.  Where top_k says how many columns matter, these are found, put in order and weighed alone; otherwise the probabilities of the whole row are added up in bins of
-// their size, and the columns of the bin in which a sum (top_p's, the random number's) ends are put in order.
-template <int BF, int NT, int NV>
-__global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules rules, int32_t *tokens, float *logprobs, int32_t *kept) {
-  __shared__ Search<NT> sh;
-  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const char *at_row = x + t * ld * Piece<BF>::ES;
-  using R = Row<BF, NT, NV>;
-  R row(at_row, V, R::aligned(at_row, V), tid, wave);
-  const float u = uniform[t], temp = rules.temperature ? rules.temperature[t] : 1.f, p = rules.top_p ? rules.top_p[t] : 1.f, m = rules.min_p ? rules.min_p[t] : 0.f;
-  const int k = rules.top_k ? rules.top_k[t] : 0;
-  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
-  float mine, top, low;
-  extremes(row, sh, wave, lane, mine, top, low);
-  auto answer = [&](int32_t token, double logprob, int n) {
-    tokens[t] = token;
-    if (logprobs) logprobs[t] = (float)logprob;
-    if (kept) kept[t] = n;
-  };
-  if (!(top > -INFINITY)) {
-    if (tid == 0) answer(-1, -INFINITY, 0);
-    return;
-  }
-  if (!(temp > 0.f) || k == 1) {
-    if (tid == 0) sh.found[0] = 0;
-    __syncthreads();
-    above(row, top, [&](float v, int c) { atomicMax(&sh.found[0], (unsigned long long)place(v, c)); });
-    __syncthreads();
-    if (tid == 0) answer(column_of(sh.found[0]), 0.0, 1);
-    return;
-  }
-  const Weigher mass{top, temp, 1.4426950408889634 / (double)temp, bits};
-  auto share = [&](double part, unsigned long long total) {  // the first sum that is part of the total or more
+// One row's settings
+struct Settings {
+  float u, temp, p, m;
+  int k;
+  // the first sum that is `part` of the total or more
+  static __device__ __forceinline__ unsigned long long share(double part, unsigned long long total) {
     const double s = ceil(part * (double)total);
     return s >= 1.0 ? min((unsigned long long)s, total) : 1ull;
-  };
-  auto draw_at = [&](unsigned long long total) { return u > 0.f ? min((unsigned long long)((double)u * (double)total), total - 1) + 1 : 1ull; };
-  auto logprob = [&](float v, unsigned long long total) { return mass.exponent(v) * 0.6931471805599453 - log(ldexp((double)total, -bits)); };
-  const float least = m > 0.f ? mass.smallest(m, lane) : -INFINITY;
-  if (k > 1 && k <= kTop && k < V) {
-    const float from = bound_of(row, f, k, mine, top, low);
-    const int n = from > -INFINITY ? collect(row, sh, from) : kList + 1;
-    if (n <= kList) {
-      const int kk = min(k, n);
-      f.sort(n, kk);
-      for (int i = tid; i < kk; i += NT) sh.list[i] = mass(value_of(sh.sorted[i]));
-      __syncthreads();
-      if (wave) return;
-      const Sums sums(sh.list, kk, lane);
-      unsigned long long upto = sums.total;
-      int count = kk;
-      if (p < 1.f) count = sums.reach(share(p, sums.total), upto) + 1;
-      if (m > 0.f) {
-        int enough = 0;
-        for (int i = lane; i < count; i += 64) enough += value_of(sh.sorted[i]) >= least;
-        count = wave_add(enough);
-        upto = sums.upto(count);
-      }
-      const unsigned long long total = upto;
-      const int i = sums.reach(draw_at(total), upto);
-      if (lane == 0) {
-        const uint64_t where = sh.sorted[i];
-        answer(column_of(where), logprob(value_of(where), total), count);
-      }
-      return;
-    }
   }
-  auto one = [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; };
+  __device__ __forceinline__ unsigned long long draw_at(unsigned long long total) const { return u > 0.f ? min((unsigned long long)((double)u * (double)total), total - 1) + 1 : 1ull; }
+};
+
+// A token of a row of which many columns may be kept: the probabilities of the whole row are added up in bins of their size, and the columns of the bin in which a sum (top_p's, the random
+// number's) ends are put in order.  A function of its own, which leaves the registers of the way through a list alone.
+template <int BF, int NT>
+__device__ __attribute__((noinline)) void draw_of_many(const char *at_row, int V, int head, int wave, int bits, const Settings set, int32_t *token, float *logprob_out, int32_t *kept) {
+  Search<NT> &sh = shared<NT>();
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  const int tid = f.tid, lane = f.lane, k = set.k;
+  float top, lowest;
+  f.extremes(top, lowest);
+  if (!(top > -INFINITY)) {
+    if (tid == 0) {
+      *token = -1;
+      if (logprob_out) *logprob_out = -INFINITY;
+      if (kept) *kept = 0;
+    }
+    return;
+  }
+  const Weigher slow{top, 1.4426950408889634 / (double)set.temp, bits};
+  __shared__ double table[kTable];
+  for (int i = tid; i < kTable; i += NT) table[i] = QuickWeigher::entry(i, bits);
+  const QuickWeigher quick(slow, table);
+  const bool usable = uniform_of((int)quick.usable);
+  const float p = set.p, m = set.m, least = m > 0.f ? uniform_of(slow.smallest(m, lane)) : -INFINITY;
   uint64_t last = 0;  // the last place that is kept
   if (k > 1 && k < V) {
     unsigned long long n = 0;
     f.columns([&](float v, int) { n += v > -INFINITY; });
-    if ((unsigned long long)k < f.block_add(n)) last = f.reach(k, one);
+    if ((unsigned long long)k < f.block_add(n)) last = f.reach(k, [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; });
   }
   // bins of equal width from the largest logit down to the smallest, or to where probabilities are below 2^-48
-  const float span = fminf(top - f.smallest(), 48.f * (float)(1.0 / mass.c)), scale = span > 0.f && span < INFINITY ? (kBins - 1) / span : 0.f;
-  auto bin = [&](float v) {
-    const float b = (top - v) * scale;
-    return b < (float)(kBins - 1) ? (int)b : kBins - 1;
-  };
+  const float span = fminf(top - lowest, 48.f * (float)(1.0 / slow.c)), scale = span > 0.f && span < INFINITY ? (kBins - 1) / span : 0.f;
+  auto bin = [&](float v) { return fminf((top - v) * scale, (float)(kBins - 1)); };  // (its whole part)
+  bool binned = usable;
+  unsigned long long total;
   __syncthreads();
-  f.clear(sh.bins.amount, kBins);
-  __syncthreads();
-  f.columns([&](float v, int c) {
-    if (last && place(v, c) < last) return;
-    const unsigned long long w = mass(v);
-    if (w) atomicAdd(&sh.bins.amount[bin(v)], w);
-  });
-  __syncthreads();
-  unsigned long long before, total;
-  f.find(sh.bins.amount, kBins, ~0ull, total);
-  bool binned = true;
-  // the place at which the sum from the first on reaches `target`, and the sum up to it
-  auto where = [&](unsigned long long target, unsigned long long &upto) -> uint64_t {
+  if (usable) {
+    f.clear(sh.bins.amount, kBins);
+    __syncthreads();
+    auto add = [&](float v) {
+      const unsigned long long w = quick(v);
+      if (w) atomicAdd(&sh.bins.amount[(int)bin(v)], w);
+    };
+    if (last)
+      f.columns([&](float v, int c) {
+        if (place(v, c) >= last) add(v);
+      });
+    else f.columns([&](float v, int) { add(v); });
+    __syncthreads();
+    f.find(sh.bins.amount, kBins, ~0ull, total);
+  } else {
+    unsigned long long n = 0;
+    f.columns([&](float v, int c) { n += place(v, c) >= last ? slow(v) : 0; });
+    total = f.block_add(n);
+  }
+  // The place at which the sum from the first on reaches `target`, and the sum up to it.  `also` sees every column.
+  auto where = [&](unsigned long long target, unsigned long long &upto, auto also) -> uint64_t {
     if (binned) {
+      unsigned long long before;
       __syncthreads();
       const int b = f.find(sh.bins.amount, kBins, target, before);
-      __syncthreads();
+      const float first = b, next = b < kBins - 1 ? b + 1 : INFINITY;
       if (tid == 0) sh.n = 0;
       __syncthreads();
       f.columns([&](float v, int c) {
-        if (!(v > -INFINITY) || bin(v) != b || place(v, c) < last) return;
-        const int i = atomicAdd(&sh.n, 1);
-        if (i < kList) sh.list[i] = place(v, c);
+        also(v, c);
+        const float at = bin(v);
+        if (at >= first && at < next && v > -INFINITY && place(v, c) >= last) {
+          const int i = atomicAdd(&sh.n, 1);
+          if (i < kList) sh.list[i] = place(v, c);
+        }
       });
       __syncthreads();
-      const int n = sh.n;
+      const int n = uniform_of(sh.n);
       if (n <= kList) {
         f.sort(n, n);
-        for (int i = tid; i < n; i += NT) sh.list[i] = mass(value_of(sh.sorted[i]));
+        for (int i = tid; i < n; i += NT) sh.list[i] = quick(value_of(sh.sorted[i]));
         __syncthreads();
         if (wave == 0) {
           unsigned long long s;
@@ -437,11 +502,12 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
           if (lane == 0) { sh.found[0] = sh.sorted[i]; sh.found[1] = before + s; }
         }
         __syncthreads();
-        upto = sh.found[1];
-        return sh.found[0];
+        upto = uniform_of(sh.found[1]);
+        return uniform_of(sh.found[0]);
       }
-    }
+    } else f.columns(also);
     binned = false;  // (reach takes the bins)
+    auto mass = [&](float v) { return usable ? quick(v) : slow(v); };
     const uint64_t at = f.reach(target, [&](float v, uint64_t q) -> unsigned long long { return q >= last ? mass(v) : 0; });
     unsigned long long s = 0;
     f.columns([&](float v, int c) {
@@ -450,81 +516,105 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
     upto = f.block_add(s);
     return at;
   };
-  if (p < 1.f) last = where(share(p, total), total);
+  if (p < 1.f) last = where(set.share(p, total), total, [](float, int) {});
   const uint64_t probable = m > 0.f ? place(least, (1 << kColumnBits) - 1) : 0;
   if (probable > last) {
     last = probable;
     unsigned long long s = 0;
     f.columns([&](float v, int) {
-      if (v >= least) s += mass(v);
+      if (v >= least) s += usable ? quick(v) : slow(v);
     });
     total = f.block_add(s);
   }
-  unsigned long long n = 0;
+  unsigned long long upto;
+  int n = 0;
   const float end = last ? value_of(last) : -3.402823466e38f;
   const int end_column = last ? column_of(last) : V;
-  f.columns([&](float v, int c) { n += v > end || (v == end && c <= end_column); });
-  n = f.block_add(n);
-  unsigned long long upto;
-  const uint64_t at = where(draw_at(total), upto);
-  if (tid == 0) answer(column_of(at), logprob(value_of(at), total), (int)n);
+  const uint64_t at = where(set.draw_at(total), upto, [&](float v, int c) { n += v > end || (v == end && c <= end_column); });
+  n = (int)f.block_add((unsigned long long)n);
+  if (tid == 0) {
+    *token = column_of(at);
+    if (logprob_out) *logprob_out = (float)slow.logarithm(value_of(at), total);
+    if (kept) *kept = n;
+  }
 }
 
-// The k largest of a row a workgroup: those above a bound that few columns reach, put in order.
 template <int BF, int NT, int NV>
-__global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
-  __shared__ Search<NT> sh;
-  __shared__ float part[NT / 64];
+__global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules rules, int32_t *tokens, float *logprobs, int32_t *kept) {
+  Search<NT> &sh = shared<NT>();
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const char *at_row = x + t * ld * Piece<BF>::ES;
   using R = Row<BF, NT, NV>;
-  R row(at_row, V, R::aligned(at_row, V), tid, wave);
-  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
+  const int head = R::aligned(at_row, V);
+  Settings set;
+  set.u = uniform_of(uniform[t]);
+  set.temp = rules.temperature ? uniform_of(rules.temperature[t]) : 1.f;
+  set.p = rules.top_p ? uniform_of(rules.top_p[t]) : 1.f;
+  set.m = rules.min_p ? uniform_of(rules.min_p[t]) : 0.f;
+  set.k = rules.top_k ? uniform_of(rules.top_k[t]) : 0;
+  const int k = min(V, set.temp > 0.f ? set.k : 1);
+  if (k < 1 || k > kTop) {
+    draw_of_many<BF, NT>(at_row, V, head, wave, bits, set, tokens + t, logprobs ? logprobs + t : nullptr, kept ? kept + t : nullptr);
+    return;
+  }
+  R row(at_row, V, head, tid, wave);
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
   float mine, top, low;
   extremes(row, sh, wave, lane, mine, top, low);
-  const int n = min(k, V);
-  const float from = bound_of(row, f, n, mine, top, low);
-  int found = from > -INFINITY ? collect(row, sh, from) : 0;
-  uint64_t last = 0;
-  const bool bounded = found >= n && found <= kList;  // (otherwise: equal logits, or none)
-  if (!bounded) {
-    last = n < V ? f.reach(n, [](float, uint64_t) -> unsigned long long { return 1; }) : 0;
-    if (tid == 0) sh.n = 0;
-    __syncthreads();
-    f.columns([&](float v, int c) {
-      const uint64_t p = place(v, c);
-      if (p >= last) sh.list[atomicAdd(&sh.n, 1)] = p;
-    });
-    found = n;
-    __syncthreads();
+  const float from = bound_of(row, f, k, mine, top, low);
+  int n = from > -INFINITY ? collect(row, sh, from) : 0;
+  if (n < k || n > kList) n = list_of_many<BF, NT>(at_row, V, head, wave, k);
+  f.sort(n, k);
+  const Weigher mass{top, 1.4426950408889634 / (double)set.temp, bits};
+  for (int i = tid; i < k; i += NT) sh.list[i] = mass(value_of(sh.sorted[i]));
+  __syncthreads();
+  if (wave) return;
+  const Sums sums(sh.list, k, lane);
+  unsigned long long upto = sums.total, total;
+  int count = 0;
+  for (int i = lane; i < k; i += 64) count += value_of(sh.sorted[i]) > -INFINITY;
+  count = wave_add(count);
+  if (set.p < 1.f && count > 1) count = sums.reach(set.share(set.p, sums.total), upto) + 1;
+  if (set.m > 0.f && count > 1) {
+    const float least = mass.smallest(set.m, lane);
+    int enough = 0;
+    for (int i = lane; i < count; i += 64) enough += value_of(sh.sorted[i]) >= least;
+    count = wave_add(enough);
+    upto = sums.upto(count);
   }
-  f.sort(found, found);
-  const int64_t out = t * ldk;
+  total = upto;
+  const int i = sums.reach(set.draw_at(total), upto);
+  if (lane == 0) {
+    const uint64_t where = sh.sorted[i];
+    tokens[t] = count ? column_of(where) : -1;
+    if (logprobs) logprobs[t] = count ? (float)mass.logarithm(value_of(where), total) : -INFINITY;
+    if (kept) kept[t] = count;
+  }
+}
+
+// The list of `found` places put in order, its first n written (and k - n entries that are not there), and the log-sum-exp of the others over the temperature: those behind the n in the list, and
+// those that `outside(f)` calls f with, which may be -infinity for the list's own.
+template <int BF, int NT, class O>
+__device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int lane, int wave, int n, int k, int found, double inv_temp, int32_t *ids, float *values, float *rest, O outside) {
+  Finder<BF, NT>::sort(sh, tid, found, found);
   for (int i = tid; i < k; i += NT) {
     const uint64_t p = i < n ? sh.sorted[i] : 0;
-    ids[out + i] = i < n ? column_of(p) : -1;
-    values[out + i] = i < n ? value_of(p) : -INFINITY;
+    ids[i] = i < n ? column_of(p) : -1;
+    values[i] = i < n ? value_of(p) : -INFINITY;
   }
   if (!rest) return;
-  auto others = [&](auto g) {  // of every column that is not among the k
-    if (bounded) {
-      row.each([&](const Piece<BF> &y, int) {
-#pragma unroll
-        for (int e = 0; e < Piece<BF>::N; ++e) g(y[e] < from ? y[e] : -INFINITY);
-      });
-      g(row.xl < from ? row.xl : -INFINITY);
-      for (int i = n + tid; i < found; i += NT) g(value_of(sh.sorted[i]));
-    } else
-      f.columns([&](float v, int c) { g(v > -INFINITY && place(v, c) < last ? v : -INFINITY); });
+  auto others = [&](auto g) {
+    outside(g);
+    for (int i = n + tid; i < found; i += NT) g(value_of(sh.sorted[i]));
   };
   auto block = [&](float v, bool sum) {
     v = sum ? wave_add(v) : wave_max(v);
     __syncthreads();
-    if (lane == 0) part[wave] = v;
+    if (lane == 0) sh.most[wave] = v;
     __syncthreads();
-    v = part[0];
-    for (int w = 1; w < NT / 64; ++w) v = sum ? v + part[w] : fmaxf(v, part[w]);
-    return v;
+    v = sh.most[0];
+    for (int w = 1; w < NT / 64; ++w) v = sum ? v + sh.most[w] : fmaxf(v, sh.most[w]);
+    return uniform_of(v);
   };
   const float c = (float)(1.4426950408889634 * inv_temp);
   auto sum = [&](float ref) {
@@ -540,7 +630,51 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
     ref = block(m, false);
     s = ref > -INFINITY ? sum(ref) : 0.f;
   }
-  if (tid == 0) rest[t] = ref > -INFINITY ? (float)((double)ref * inv_temp + log((double)s)) : -INFINITY;
+  if (tid == 0) *rest = ref > -INFINITY ? (float)((double)ref * inv_temp + log((double)s)) : -INFINITY;
+}
+
+template <int BF, int NT>
+__device__ __attribute__((noinline)) void top_of_many(const char *at_row, int V, int head, int wave, int n, int k, double inv_temp, int32_t *ids, float *values, float *rest) {
+  Search<NT> &sh = shared<NT>();
+  const int found = list_of_many<BF, NT>(at_row, V, head, wave, n);
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  uint64_t last = ~0ull;  // of the list
+  for (int i = f.tid; i < found; i += NT) last = min(last, (uint64_t)sh.list[i]);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) last = min(last, (uint64_t)__shfl_xor((unsigned long long)last, o, 64));
+  __syncthreads();
+  if (f.lane == 0) sh.wave_sum[wave] = last;
+  __syncthreads();
+  for (int w = 0; w < NT / 64; ++w) last = min(last, (uint64_t)sh.wave_sum[w]);
+  last = uniform_of((unsigned long long)last);
+  write_top<BF, NT>(sh, f.tid, f.lane, wave, n, k, found, inv_temp, ids, values, rest, [&](auto g) { f.columns([&](float v, int c) { g(v > -INFINITY && place(v, c) < last ? v : -INFINITY); }); });
+}
+
+// The k largest of a row a workgroup: those above a bound that few columns reach, put in order.
+template <int BF, int NT, int NV>
+__global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
+  Search<NT> &sh = shared<NT>();
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const char *at_row = x + t * ld * Piece<BF>::ES;
+  using R = Row<BF, NT, NV>;
+  R row(at_row, V, R::aligned(at_row, V), tid, wave);
+  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
+  float mine, top, low;
+  extremes(row, sh, wave, lane, mine, top, low);
+  const int n = min(k, V);
+  const float from = bound_of(row, f, n, mine, top, low);
+  int found = from > -INFINITY ? collect(row, sh, from) : 0;
+  if (found < n || found > kList) {
+    top_of_many<BF, NT>(at_row, V, row.head, wave, n, k, inv_temp, ids + t * ldk, values + t * ldk, rest ? rest + t : nullptr);
+    return;
+  }
+  write_top<BF, NT>(sh, tid, lane, wave, n, k, found, inv_temp, ids + t * ldk, values + t * ldk, rest ? rest + t : nullptr, [&](auto g) {  // every column that is not in the list
+    row.each([&](const Piece<BF> &y, int) {
+#pragma unroll
+      for (int e = 0; e < Piece<BF>::N; ++e) g(y[e] < from ? y[e] : -INFINITY);
+    });
+    g(row.xl < from ? row.xl : -INFINITY);
+  });
 }
 
 // The kernel whose registers hold a row: few rows get more threads each.
