@@ -50,12 +50,12 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   __shared__ double set_sums[4][NW];
   __shared__ int twice;
   const int t = blockIdx.x, tid = threadIdx.x, k = te.k, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const char *row = logits + (int64_t)t * ld * ES;
+  const device_bytes row = (device_bytes)(logits + (int64_t)t * ld * ES);
   char *out = grads + (int64_t)t * ldg * ES;
   const int head = min(V, (int)(-(reinterpret_cast<uintptr_t>(out) / ES) & (N - 1)));
   const int pieces = (V - head) / N, mine = pieces - 64 * wave;  // u NT >= mine: the wave's piece u lies beyond the row
   const int ends = V - pieces * N, end = tid < head ? tid : pieces * N + tid;  // columns that are in no piece, and the thread's
-  const char *first = row + head * ES;
+  const device_bytes first = row + head * ES;
   char *first_out = out + head * ES;
   // what the first of the list need, and the row
   const int64_t list = t * te.ld;

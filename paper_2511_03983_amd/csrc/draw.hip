@@ -9,6 +9,7 @@ constexpr int kTop = 1024;   // the longest list
 constexpr int kList = 1536;  // columns that are put in order by comparing them with each other
 constexpr int kBins = 1024;
 constexpr int kColumnBits = 20;
+constexpr int kTable = 512;
 
 // Unsigned numbers in the order of a row's columns: the logit's place in 32 bits, the column (turned over) below it.  Columns that hold no number count as -infinity, -0 is 0.
 __device__ __forceinline__ uint64_t place(float v, int c) {
@@ -49,6 +50,7 @@ template <int NT> struct Search {
   unsigned long long sorted[kList];
   unsigned long long found[2], wave_sum[NT / 64];
   float most[NT / 64], least[NT / 64];
+  double table[kTable];
   int n;
 };
 
@@ -69,39 +71,52 @@ template <int BF, int NT> struct Finder {
   using P16 = Piece<BF>;
   static constexpr int N = P16::N, NW = NT / 64;
   Search<NT> &sh;
-  const char *row, *first;
+  device_bytes row, first;
   int V, head, pieces, tid, wave, lane;
 
-  __device__ __forceinline__ Finder(Search<NT> &s, const char *row_, int V_, int head_, int wave_) : sh(s), row(row_), V(V_), head(head_), tid(threadIdx.x), wave(wave_) {
+  __device__ __forceinline__ Finder(Search<NT> &s, device_bytes row_, int V_, int head_, int wave_) : sh(s), row(row_), V(V_), head(head_), tid(threadIdx.x), wave(wave_) {
     lane = tid & 63;
     pieces = (V - head) / N;
     first = row + head * P16::ES;
   }
-  // f(logit, column) of every column of the row, whose pieces are read some at a time while those before them are at work
-  template <class F> __device__ __forceinline__ void columns(F f) const {
-    constexpr int B = 4;
-    P16 next[B];
-    auto load = [&](int v) {
+  // f(N logits, the first's column, how many of them are the row's) for all of the row, with D pieces on their way: the registers of one that is done take the one D behind it (not before it is
+  // done, and whether there is one or not: otherwise it is loaded somewhere else and waited for, to be moved)
+  template <int D, class F> __device__ __forceinline__ void runs(F f) const {
+    if (pieces > 0) {
+      P16 next[D];
 #pragma unroll
-      for (int b = 0; b < B; ++b)
-        if (v + b * NT < pieces) next[b].load(first + (int64_t)(v + b * NT) * 16);
-    };
-    load(tid);
+      for (int d = 0; d < D; ++d) next[d].load(first + (int64_t)min(tid + d * NT, pieces - 1) * 16);
 #pragma unroll 1
-    for (int v = tid; v < pieces; v += B * NT) {
-      P16 y[B];
+      for (int v = tid; v < pieces; v += D * NT) {
 #pragma unroll
-      for (int b = 0; b < B; ++b) y[b] = next[b];
-      load(v + B * NT);
+        for (int d = 0; d < D; ++d) {
+          if (v + d * NT < pieces) {
+            float x[N];
 #pragma unroll
-      for (int b = 0; b < B; ++b)
-        if (v + b * NT < pieces) {
-#pragma unroll
-          for (int e = 0; e < N; ++e) f(y[b][e], head + (v + b * NT) * N + e);
+            for (int e = 0; e < N; ++e) x[e] = next[d][e];
+            f(x, head + (v + d * NT) * N, N);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          next[d].load(first + (int64_t)min(v + (d + D) * NT, pieces - 1) * 16);
         }
+      }
     }
     const int c = tid < head ? tid : pieces * N + tid;
-    if (c < V && tid < V - pieces * N) f(load1<BF>(row, c), c);
+    if (tid < V - pieces * N) {
+      float x[N];
+      x[0] = load1<BF>(row, c);
+#pragma unroll
+      for (int e = 1; e < N; ++e) x[e] = -INFINITY;
+      f(x, c, 1);
+    }
+  }
+  // f(logit, column) of every column
+  template <class F> __device__ __forceinline__ void columns(F f) const {
+    runs<4>([&](const float *x, int c, int n) {
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (e == 0 || n > 1) f(x[e], c + e);
+    });
   }
   __device__ __forceinline__ unsigned long long block_add(unsigned long long v) const {
     v = wave_add(v);
@@ -173,9 +188,12 @@ template <int BF, int NT> struct Finder {
   // the row's largest logit and the smallest above -infinity
   __device__ __forceinline__ void extremes(float &top, float &least) const {
     float m = -INFINITY, l = INFINITY;
-    columns([&](float v, int) {
-      m = fmaxf(m, v);
-      l = v > -INFINITY ? fminf(l, v) : l;
+    runs<6>([&](const float *x, int, int) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        m = fmaxf(m, x[e]);
+        l = fminf(l, x[e] > -INFINITY ? x[e] : INFINITY);
+      }
     });
     m = wave_max(m);
     l = -wave_max(-l);
@@ -284,7 +302,7 @@ template <int NT, class R> __device__ __forceinline__ int collect(R &row, Search
 
 // The list of a row's k first places (k at most its columns; in any order, and more where that is as quick), by counting all of its columns in bins, or else bit by bit; their number.  Every
 // column of the list is before all others.  A function of its own, which leaves the registers of the quicker way alone.
-template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(const char *at_row, int V, int head, int wave, int k) {
+template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(device_bytes at_row, int V, int head, int wave, int k) {
   Search<NT> &sh = shared<NT>();
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
   const float from = f.bound_of_all(k);
@@ -307,6 +325,25 @@ template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(
     n = list([&](float v, int c) { return place(v, c) >= last; });
   }
   return n;
+}
+
+// The smallest finite float that is `enough`, which larger ones are, too: a wave tries 64 at a time.  (The largest, if none is.)
+template <class F> __device__ __forceinline__ float lowest_where(F enough, int lane) {
+  auto value = [](uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); };
+  uint32_t lo = 0x00800000u, hi = 0xff7fffffu;  // places of the finite floats
+  while (lo < hi) {
+    const uint32_t step = (hi - lo) / 64 + 1;
+    const uint64_t at = (uint64_t)lo + (uint64_t)step * lane;
+    const uint64_t yes = __ballot(at >= hi || enough(value((uint32_t)at)));
+    const int i = __builtin_ctzll(yes | 1ull << 63);
+    const bool none = !yes;
+    const uint64_t up = (uint64_t)lo + (uint64_t)step * (none ? 63 : i);
+    if (none) { lo = (uint32_t)up + 1; continue; }
+    hi = up < hi ? (uint32_t)up : hi;
+    if (i) lo = (uint32_t)(up - step + 1);
+    else lo = hi;
+  }
+  return value(lo);
 }
 
 // One row's settings and what follows from them: probabilities are whole multiples of 2^-bits of the largest, in 64 bits, so that any order of their sums gives the same.
@@ -344,7 +381,6 @@ struct Weigher {
 
 // The same for whole rows, in half the instructions (an exponential of power2 takes 25, several of which run at a fraction of the rate): 2^(n / 512) from a table, the rest of the exponent by a
 // polynomial of degree 3 (2^-48 off).  Not for every row: `usable` tells.
-constexpr int kTable = 512;
 struct QuickWeigher {
   double top, c;  // 512 log2(e) / temperature
   float least;    // below it nothing weighs anything
@@ -422,7 +458,7 @@ struct Settings {
 // A token of a row of which many columns may be kept: the probabilities of the whole row are added up in bins of their size, and the columns of the bin in which a sum (top_p's, the random
 // number's) ends are put in order.  A function of its own, which leaves the registers of the way through a list alone.
 template <int BF, int NT>
-__device__ __attribute__((noinline)) void draw_of_many(const char *at_row, int V, int head, int wave, int bits, const Settings set, int32_t *token, float *logprob_out, int32_t *kept) {
+__device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int V, int head, int wave, int bits, const Settings set, int32_t *token, float *logprob_out, int32_t *kept) {
   Search<NT> &sh = shared<NT>();
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
   const int tid = f.tid, lane = f.lane, k = set.k;
@@ -437,9 +473,8 @@ __device__ __attribute__((noinline)) void draw_of_many(const char *at_row, int V
     return;
   }
   const Weigher slow{top, 1.4426950408889634 / (double)set.temp, bits};
-  __shared__ double table[kTable];
-  for (int i = tid; i < kTable; i += NT) table[i] = QuickWeigher::entry(i, bits);
-  const QuickWeigher quick(slow, table);
+  for (int i = tid; i < kTable; i += NT) sh.table[i] = QuickWeigher::entry(i, bits);
+  const QuickWeigher quick(slow, sh.table);
   const bool usable = uniform_of((int)quick.usable);
   const float p = set.p, m = set.m, least = m > 0.f ? uniform_of(slow.smallest(m, lane)) : -INFINITY;
   uint64_t last = 0;  // the last place that is kept
@@ -457,15 +492,19 @@ __device__ __attribute__((noinline)) void draw_of_many(const char *at_row, int V
   if (usable) {
     f.clear(sh.bins.amount, kBins);
     __syncthreads();
-    auto add = [&](float v) {
-      const unsigned long long w = quick(v);
-      if (w) atomicAdd(&sh.bins.amount[(int)bin(v)], w);
-    };
-    if (last)
-      f.columns([&](float v, int c) {
-        if (place(v, c) >= last) add(v);
-      });
-    else f.columns([&](float v, int) { add(v); });
+    f.template runs<4>([&](const float *x, int c, int) {
+      constexpr int N = Piece<BF>::N;
+      unsigned long long w[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[e] = quick(x[e]);
+      if (last) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) w[e] = place(x[e], c + e) >= last ? w[e] : 0;
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (w[e]) atomicAdd(&sh.bins.amount[(int)bin(x[e])], w[e]);
+    });
     __syncthreads();
     f.find(sh.bins.amount, kBins, ~0ull, total);
   } else {
@@ -479,15 +518,26 @@ __device__ __attribute__((noinline)) void draw_of_many(const char *at_row, int V
       unsigned long long before;
       __syncthreads();
       const int b = f.find(sh.bins.amount, kBins, target, before);
-      const float first = b, next = b < kBins - 1 ? b + 1 : INFINITY;
+      // the logits of bin b: from `least` up to `most`
+      const float first = b, next = b + 1;
+      const float least = uniform_of(b < kBins - 1 ? lowest_where([&](float v) { return bin(v) < next; }, lane) : -3.402823466e38f);
+      const float most = uniform_of(b ? -lowest_where([&](float v) { return bin(-v) >= first; }, lane) : top);
       if (tid == 0) sh.n = 0;
       __syncthreads();
-      f.columns([&](float v, int c) {
-        also(v, c);
-        const float at = bin(v);
-        if (at >= first && at < next && v > -INFINITY && place(v, c) >= last) {
-          const int i = atomicAdd(&sh.n, 1);
-          if (i < kList) sh.list[i] = place(v, c);
+      f.template runs<4>([&](const float *x, int c, int n) {
+        bool any = false;
+#pragma unroll
+        for (int e = 0; e < Piece<BF>::N; ++e) {
+          also(x[e], c + e);
+          any |= x[e] >= least && x[e] <= most;
+        }
+        if (any) {
+#pragma unroll
+          for (int e = 0; e < Piece<BF>::N; ++e)
+            if (x[e] >= least && x[e] <= most && place(x[e], c + e) >= last) {
+              const int i = atomicAdd(&sh.n, 1);
+              if (i < kList) sh.list[i] = place(x[e], c + e);
+            }
         }
       });
       __syncthreads();
@@ -543,9 +593,9 @@ template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules rules, int32_t *tokens, float *logprobs, int32_t *kept) {
   Search<NT> &sh = shared<NT>();
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const char *at_row = x + t * ld * Piece<BF>::ES;
+  const device_bytes at_row = (device_bytes)(x + t * ld * Piece<BF>::ES);
   using R = Row<BF, NT, NV>;
-  const int head = R::aligned(at_row, V);
+  const int head = R::aligned((const char *)at_row, V);
   Settings set;
   set.u = uniform_of(uniform[t]);
   set.temp = rules.temperature ? uniform_of(rules.temperature[t]) : 1.f;
@@ -634,7 +684,7 @@ __device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int lane, int
 }
 
 template <int BF, int NT>
-__device__ __attribute__((noinline)) void top_of_many(const char *at_row, int V, int head, int wave, int n, int k, double inv_temp, int32_t *ids, float *values, float *rest) {
+__device__ __attribute__((noinline)) void top_of_many(device_bytes at_row, int V, int head, int wave, int n, int k, double inv_temp, int32_t *ids, float *values, float *rest) {
   Search<NT> &sh = shared<NT>();
   const int found = list_of_many<BF, NT>(at_row, V, head, wave, n);
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
@@ -655,9 +705,9 @@ template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
   Search<NT> &sh = shared<NT>();
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const char *at_row = x + t * ld * Piece<BF>::ES;
+  const device_bytes at_row = (device_bytes)(x + t * ld * Piece<BF>::ES);
   using R = Row<BF, NT, NV>;
-  R row(at_row, V, R::aligned(at_row, V), tid, wave);
+  R row(at_row, V, R::aligned((const char *)at_row, V), tid, wave);
   const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
   float mine, top, low;
   extremes(row, sh, wave, lane, mine, top, low);

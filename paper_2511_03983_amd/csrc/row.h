@@ -7,12 +7,15 @@
 namespace {
 
 typedef uint32_t u32x4v __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4u __attribute__((ext_vector_type(4), aligned(2)));
+// Memory of the device, said to be: what a function that is not inlined is given could be LDS as well, and its loads would be waited for with those
+typedef const __attribute__((address_space(1))) char *device_bytes;
 
 // Sixteen bytes of a row, as floats: eight of bf16, four of fp32.
 template <int BF> struct Piece {
   static constexpr int N = BF ? 8 : 4, ES = BF ? 2 : 4;
   u32x4v u;
-  __device__ __forceinline__ void load(const char *p) { __builtin_memcpy(&u, p, 16); }  // (from any element on)
+  __device__ __forceinline__ void load(device_bytes p) { u = *(const __attribute__((address_space(1))) u32x4u *)p; }  // (from any element on)
   static __device__ __forceinline__ u32x4v none() {  // -infinity throughout
     const uint32_t n = BF ? 0xff80ff80u : 0xff800000u;
     return u32x4v{n, n, n, n};
@@ -36,8 +39,9 @@ template <int BF> struct Piece {
     return m;
   }
 };
-template <int BF> __device__ __forceinline__ float load1(const char *row, int c) {
-  return BF ? __uint_as_float((uint32_t) reinterpret_cast<const uint16_t *>(row)[c] << 16) : reinterpret_cast<const float *>(row)[c];
+template <int BF> __device__ __forceinline__ float load1(device_bytes row, int c) {
+  if (BF) return __uint_as_float((uint32_t)((const __attribute__((address_space(1))) uint16_t *)row)[c] << 16);
+  return ((const __attribute__((address_space(1))) float *)row)[c];
 }
 template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, float v) {
   if (BF) reinterpret_cast<__bf16 *>(row)[c] = (__bf16)v;  // round to nearest even
@@ -62,9 +66,9 @@ template <int BF, int NT, int NV> struct Row {
   static constexpr int N = P16::N, ES = P16::ES, NW = NT / 64;
   P16 x[NV ? NV : 1];
   float xl;
-  const char *first;
+  device_bytes first;
   int head, pieces, mine, ends, end, tid;
-  __device__ __forceinline__ Row(const char *row, int V, int head_, int tid_, int wave) {
+  __device__ __forceinline__ Row(device_bytes row, int V, int head_, int tid_, int wave) {
     tid = tid_;
     head = head_;
     pieces = (V - head) / N;
