@@ -48,10 +48,12 @@ template <int NT> struct Search {
   } bins;
   unsigned long long list[kList];    // places that may be taken, in any order; then what the sorted ones weigh
   unsigned long long sorted[kList];
+  static constexpr int kMarks = 2 * kList;
+  __device__ __forceinline__ uint32_t *marks() { return reinterpret_cast<uint32_t *>(sorted); }  // pieces that hold columns for the list (before there are any in order)
   unsigned long long found[2], wave_sum[NT / 64];
   float most[NT / 64], least[NT / 64];
   double table[kTable];
-  int n;
+  int n, marked;
 };
 
 // A value that all lanes have, known to be one: what depends on it is a branch of all
@@ -110,6 +112,8 @@ template <int BF, int NT> struct Finder {
       f(x, c, 1);
     }
   }
+  // the number by which a run is marked
+  __device__ __forceinline__ int piece_of(int c, int n) const { return n > 1 ? (c - head) / N : pieces + tid; }
   // f(logit, column) of every column
   template <class F> __device__ __forceinline__ void columns(F f) const {
     runs<4>([&](const float *x, int c, int n) {
@@ -131,12 +135,12 @@ template <int BF, int NT> struct Finder {
   template <class T> __device__ __forceinline__ void clear(T *bins, int n) const {
     for (int i = tid; i < n; i += NT) bins[i] = 0;
   }
-  // The bin in which what lies in the bins up to it reaches `target` (n: none), and what lies before it.  n: a multiple of 64.
+  // The bin in which what lies in the bins up to it reaches `target` (n: none), and what lies before it.  n: 64 times a power of two.
   template <class T> __device__ __forceinline__ int find(const T *bins, int n, unsigned long long target, unsigned long long &before) const {
     if (wave == 0) {
       const int per = n / 64;
       unsigned long long s = 0, upto;
-      for (int i = 0; i < per; ++i) s += bins[lane * per + i];
+      for (int i = 0; i < per; ++i) s += bins[lane * per + ((i + lane) & (per - 1))];  // (in an order of its own: otherwise all lanes read from the same banks)
       upto = s;
 #pragma unroll
       for (int o = 1; o < 64; o <<= 1) {
@@ -228,6 +232,44 @@ template <int BF, int NT> struct Finder {
     const float e = top - (b + 1) / scale;
     return e - (4e-7f * (fabsf(top) + fabsf(e)) + 1e-37f);
   }
+  // The list of the row's columns that are `wanted(logit, column)`, in two steps: pieces (and, behind their numbers, the columns in none) that hold one are marked in a pass over the row, and
+  // looked through afterwards, a thread each.  A pass marks in few instructions; with what the list takes behind every column it is code that was not fetched before (2.4 and 6.4 us where both steps take
+  // 1.8 and 2.9).  begin(); mark() in a pass; then take(), the columns' number, which may be more than the list holds.
+  __device__ __forceinline__ void begin() const {
+    __syncthreads();
+    if (tid == 0) sh.n = sh.marked = 0;
+    __syncthreads();
+  }
+  __device__ __forceinline__ void mark(int v) const {
+    const int i = atomicAdd(&sh.marked, 1);
+    if (i < Search<NT>::kMarks) sh.marks()[i] = v;
+  }
+  template <class F> __device__ __forceinline__ int take(F wanted) const {
+    __syncthreads();
+    const int n = uniform_of(sh.marked);
+    if (n > Search<NT>::kMarks) return n;
+#pragma unroll 1
+    for (int i = tid; i < n; i += NT) {
+      const int v = (int)sh.marks()[i], end = v - pieces;
+      P16 y;
+      y.u = P16::none();
+      if (end < 0) y.load(first + (int64_t)v * 16);
+      const int c = end < 0 ? head + v * N : end < head ? end : pieces * N + end;
+      const float alone = end < 0 ? 0.f : load1<BF>(row, c);
+#pragma unroll 1
+      for (int e = 0; e < (end < 0 ? N : 1); ++e) {
+        float x = alone;
+#pragma unroll
+        for (int j = 0; j < N; ++j) x = end < 0 && e == j ? y[j] : x;
+        if (!wanted(x, c + e)) continue;
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < kList) sh.list[at] = place(x, c + e);
+      }
+    }
+    __syncthreads();
+    return uniform_of(sh.n);
+  }
+
   // Puts the list's n places in order, in sh.sorted: the first `most` of them.
   __device__ __forceinline__ void sort(int n, int most) const { sort(sh, tid, n, most); }
   static __device__ __forceinline__ void sort(Search<NT> &sh, int tid, int n, int most) {
@@ -242,17 +284,6 @@ template <int BF, int NT> struct Finder {
   }
 };
 
-// f(logit, column) of the columns at `from` (above -infinity) and above, which are few
-template <class R, class F> __device__ __forceinline__ void above(R &row, float from, F f) {
-  row.each([&](const typename R::P16 &y, int v) {
-    if (y.most() >= from) {
-#pragma unroll
-      for (int e = 0; e < R::N; ++e)
-        if (y[e] >= from) f(y[e], row.head + v * R::N + e);
-    }
-  });
-  if (row.xl >= from) f(row.xl, row.end);
-}
 // The row's largest logit (the thread's: `mine`), and the smallest of the threads' largest
 template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Search<NT> &sh, int wave, int lane, float &mine, float &top, float &low) {
   float m = fmaxf(row.xl, -INFINITY);
@@ -288,16 +319,13 @@ template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &
   return b < kBins ? f.edge(b, top, scale) : -INFINITY;
 }
 // the list from the columns at `from` and above; their number, which may be more than the list holds
-template <int NT, class R> __device__ __forceinline__ int collect(R &row, Search<NT> &sh, float from) {
-  __syncthreads();
-  if (threadIdx.x == 0) sh.n = 0;
-  __syncthreads();
-  above(row, from, [&](float v, int c) {
-    const int i = atomicAdd(&sh.n, 1);
-    if (i < kList) sh.list[i] = place(v, c);
+template <int BF, int NT, class R> __device__ __forceinline__ int collect(R &row, const Finder<BF, NT> &f, float from) {
+  f.begin();
+  row.each([&](const typename R::P16 &y, int v) {
+    if (y.most() >= from) f.mark(v);
   });
-  __syncthreads();
-  return uniform_of(sh.n);
+  if (row.xl >= from) f.mark(row.pieces + f.tid);
+  return f.take([&](float v, int) { return v >= from; });
 }
 
 // The list of a row's k first places (k at most its columns; in any order, and more where that is as quick), by counting all of its columns in bins, or else bit by bit; their number.  Every
@@ -307,17 +335,15 @@ template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
   const float from = f.bound_of_all(k);
   int n = 0;
-  auto list = [&](auto may) {
-    __syncthreads();
-    if (f.tid == 0) sh.n = 0;
-    __syncthreads();
-    f.columns([&](float v, int c) {
-      if (!may(v, c)) return;
-      const int i = atomicAdd(&sh.n, 1);
-      if (i < kList) sh.list[i] = place(v, c);
+  auto list = [&](auto wanted) {
+    f.begin();
+    f.template runs<4>([&](const float *x, int c, int n) {
+      bool any = false;
+#pragma unroll
+      for (int e = 0; e < Piece<BF>::N; ++e) any |= (e == 0 || n > 1) && wanted(x[e], c + e);
+      if (any) f.mark(f.piece_of(c, n));
     });
-    __syncthreads();
-    return uniform_of(sh.n);
+    return f.take(wanted);
   };
   if (from > -INFINITY) n = list([&](float v, int) { return v >= from; });
   if (n < k || n > kList) {
@@ -325,25 +351,6 @@ template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(
     n = list([&](float v, int c) { return place(v, c) >= last; });
   }
   return n;
-}
-
-// The smallest finite float that is `enough`, which larger ones are, too: a wave tries 64 at a time.  (The largest, if none is.)
-template <class F> __device__ __forceinline__ float lowest_where(F enough, int lane) {
-  auto value = [](uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); };
-  uint32_t lo = 0x00800000u, hi = 0xff7fffffu;  // places of the finite floats
-  while (lo < hi) {
-    const uint32_t step = (hi - lo) / 64 + 1;
-    const uint64_t at = (uint64_t)lo + (uint64_t)step * lane;
-    const uint64_t yes = __ballot(at >= hi || enough(value((uint32_t)at)));
-    const int i = __builtin_ctzll(yes | 1ull << 63);
-    const bool none = !yes;
-    const uint64_t up = (uint64_t)lo + (uint64_t)step * (none ? 63 : i);
-    if (none) { lo = (uint32_t)up + 1; continue; }
-    hi = up < hi ? (uint32_t)up : hi;
-    if (i) lo = (uint32_t)(up - step + 1);
-    else lo = hi;
-  }
-  return value(lo);
 }
 
 // One row's settings and what follows from them: probabilities are whole multiples of 2^-bits of the largest, in 64 bits, so that any order of their sums gives the same.
@@ -492,7 +499,7 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
   if (usable) {
     f.clear(sh.bins.amount, kBins);
     __syncthreads();
-    f.template runs<4>([&](const float *x, int c, int) {
+    f.template runs<2>([&](const float *x, int c, int) {
       constexpr int N = Piece<BF>::N;
       unsigned long long w[N];
 #pragma unroll
@@ -518,30 +525,22 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
       unsigned long long before;
       __syncthreads();
       const int b = f.find(sh.bins.amount, kBins, target, before);
-      // the logits of bin b: from `least` up to `most`
-      const float first = b, next = b + 1;
-      const float least = uniform_of(b < kBins - 1 ? lowest_where([&](float v) { return bin(v) < next; }, lane) : -3.402823466e38f);
-      const float most = uniform_of(b ? -lowest_where([&](float v) { return bin(-v) >= first; }, lane) : top);
-      if (tid == 0) sh.n = 0;
-      __syncthreads();
+      const float from = b, to = b + 1;
+      auto wanted = [&](float v) {
+        const float at = bin(v);
+        return at >= from && at < to && v > -INFINITY;
+      };
+      f.begin();
       f.template runs<4>([&](const float *x, int c, int n) {
         bool any = false;
 #pragma unroll
         for (int e = 0; e < Piece<BF>::N; ++e) {
           also(x[e], c + e);
-          any |= x[e] >= least && x[e] <= most;
+          any |= wanted(x[e]);
         }
-        if (any) {
-#pragma unroll
-          for (int e = 0; e < Piece<BF>::N; ++e)
-            if (x[e] >= least && x[e] <= most && place(x[e], c + e) >= last) {
-              const int i = atomicAdd(&sh.n, 1);
-              if (i < kList) sh.list[i] = place(x[e], c + e);
-            }
-        }
+        if (any) f.mark(f.piece_of(c, n));
       });
-      __syncthreads();
-      const int n = uniform_of(sh.n);
+      const int n = f.take([&](float v, int c) { return wanted(v) && place(v, c) >= last; });
       if (n <= kList) {
         f.sort(n, n);
         for (int i = tid; i < n; i += NT) sh.list[i] = quick(value_of(sh.sorted[i]));
@@ -612,7 +611,7 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
   float mine, top, low;
   extremes(row, sh, wave, lane, mine, top, low);
   const float from = bound_of(row, f, k, mine, top, low);
-  int n = from > -INFINITY ? collect(row, sh, from) : 0;
+  int n = from > -INFINITY ? collect(row, f, from) : 0;
   if (n < k || n > kList) n = list_of_many<BF, NT>(at_row, V, head, wave, k);
   f.sort(n, k);
   const Weigher mass{top, 1.4426950408889634 / (double)set.temp, bits};
@@ -713,7 +712,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   extremes(row, sh, wave, lane, mine, top, low);
   const int n = min(k, V);
   const float from = bound_of(row, f, n, mine, top, low);
-  int found = from > -INFINITY ? collect(row, sh, from) : 0;
+  int found = from > -INFINITY ? collect(row, f, from) : 0;
   if (found < n || found > kList) {
     top_of_many<BF, NT>(at_row, V, row.head, wave, n, k, inv_temp, ids + t * ldk, values + t * ldk, rest ? rest + t : nullptr);
     return;
