@@ -46,7 +46,7 @@ template <int NT> struct Search {
     unsigned long long amount[kBins];
     uint32_t count[kBins];
   } bins;
-  unsigned long long list[kList];    // places that may be taken, in any order; then what the sorted ones weigh
+  unsigned long long list[kList + 8];  // places that may be taken, in any order; then what the sorted ones weigh
   unsigned long long sorted[kList];
   static constexpr int kMarks = 2 * kList;
   __device__ __forceinline__ uint32_t *marks() { return reinterpret_cast<uint32_t *>(sorted); }  // pieces that hold columns for the list (before there are any in order)
@@ -273,11 +273,17 @@ template <int BF, int NT> struct Finder {
   // Puts the list's n places in order, in sh.sorted: the first `most` of them.
   __device__ __forceinline__ void sort(int n, int most) const { sort(sh, tid, n, most); }
   static __device__ __forceinline__ void sort(Search<NT> &sh, int tid, int n, int most) {
+    constexpr int U = 8;  // places that are read together (behind the list: none)
+    if (tid < U) sh.list[n + tid] = 0;
+    __syncthreads();
 #pragma unroll 1
     for (int i = tid; i < n; i += NT) {
       const unsigned long long p = sh.list[i];
       int at = 0;
-      for (int j = 0; j < n; ++j) at += sh.list[j] > p;
+#pragma unroll 1
+      for (int j = 0; j < n; j += U)
+#pragma unroll
+        for (int u = 0; u < U; ++u) at += sh.list[j + u] > p;
       if (at < most) sh.sorted[at] = p;
     }
     __syncthreads();
@@ -641,89 +647,96 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
   }
 }
 
-// The list of `found` places put in order, its first n written (and k - n entries that are not there), and the log-sum-exp of the others over the temperature: those behind the n in the list, and
-// those that `outside(f)` calls f with, which may be -infinity for the list's own.
-template <int BF, int NT, class O>
-__device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int lane, int wave, int n, int k, int found, double inv_temp, int32_t *ids, float *values, float *rest, O outside) {
+// The list of `found` places put in order and its first n written (and k - n entries that are not there).
+template <int BF, int NT>
+__device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int n, int k, int found, int32_t *ids, float *values) {
   Finder<BF, NT>::sort(sh, tid, found, found);
   for (int i = tid; i < k; i += NT) {
     const uint64_t p = i < n ? sh.sorted[i] : 0;
     ids[i] = i < n ? column_of(p) : -1;
     values[i] = i < n ? value_of(p) : -INFINITY;
   }
-  if (!rest) return;
-  auto others = [&](auto g) {
-    outside(g);
-    for (int i = n + tid; i < found; i += NT) g(value_of(sh.sorted[i]));
-  };
-  auto block = [&](float v, bool sum) {
-    v = sum ? wave_add(v) : wave_max(v);
-    __syncthreads();
-    if (lane == 0) sh.most[wave] = v;
-    __syncthreads();
-    v = sh.most[0];
-    for (int w = 1; w < NT / 64; ++w) v = sum ? v + sh.most[w] : fmaxf(v, sh.most[w]);
-    return uniform_of(v);
-  };
-  const float c = (float)(1.4426950408889634 * inv_temp);
-  auto sum = [&](float ref) {
-    float s = 0.f;
-    others([&](float v) { s += v == ref ? 1.f : __builtin_amdgcn_exp2f((v - ref) * c); });
-    return block(s, true);
-  };
-  // against the smallest of the k, which is near the largest of the others as a rule
-  float ref = value_of(sh.sorted[n - 1]), s = ref > -INFINITY && ref < INFINITY ? sum(ref) : 0.f;
-  if (!(s > 0.02f)) {
-    float m = -INFINITY;
-    others([&](float v) { m = fmaxf(m, v); });
-    ref = block(m, false);
-    s = ref > -INFINITY ? sum(ref) : 0.f;
-  }
-  if (tid == 0) *rest = ref > -INFINITY ? (float)((double)ref * inv_temp + log((double)s)) : -INFINITY;
 }
-
-template <int BF, int NT>
-__device__ __attribute__((noinline)) void top_of_many(device_bytes at_row, int V, int head, int wave, int n, int k, double inv_temp, int32_t *ids, float *values, float *rest) {
-  Search<NT> &sh = shared<NT>();
-  const int found = list_of_many<BF, NT>(at_row, V, head, wave, n);
-  const Finder<BF, NT> f(sh, at_row, V, head, wave);
-  uint64_t last = ~0ull;  // of the list
-  for (int i = f.tid; i < found; i += NT) last = min(last, (uint64_t)sh.list[i]);
+// Over the workgroup: the sum, or the largest
+template <int NT> __device__ __forceinline__ float block(Search<NT> &sh, int lane, int wave, float v, bool sum) {
+  v = sum ? wave_add(v) : wave_max(v);
+  __syncthreads();
+  if (lane == 0) sh.most[wave] = v;
+  __syncthreads();
+  v = sh.most[0];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) last = min(last, (uint64_t)__shfl_xor((unsigned long long)last, o, 64));
-  __syncthreads();
-  if (f.lane == 0) sh.wave_sum[wave] = last;
-  __syncthreads();
-  for (int w = 0; w < NT / 64; ++w) last = min(last, (uint64_t)sh.wave_sum[w]);
-  last = uniform_of((unsigned long long)last);
-  write_top<BF, NT>(sh, f.tid, f.lane, wave, n, k, found, inv_temp, ids, values, rest, [&](auto g) { f.columns([&](float v, int c) { g(v > -INFINITY && place(v, c) < last ? v : -INFINITY); }); });
+  for (int w = 1; w < NT / 64; ++w) v = sum ? v + sh.most[w] : fmaxf(v, sh.most[w]);
+  return uniform_of(v);
+}
+// The log-sum-exp over the temperature of a row's columns behind the place `last`, -infinity where there are none.
+template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind(device_bytes at_row, int V, int head, int wave, uint64_t last, double inv_temp) {
+  Search<NT> &sh = shared<NT>();
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  auto others = [&](auto g) {
+    f.columns([&](float v, int c) {
+      if (v > -INFINITY && place(v, c) < last) g(v);
+    });
+  };
+  float m = -INFINITY, s = 0.f;
+  others([&](float v) { m = fmaxf(m, v); });
+  m = block(sh, f.lane, wave, m, false);
+  if (!(m > -INFINITY)) return m;
+  const float c = (float)(1.4426950408889634 * inv_temp);
+  others([&](float v) { s += v == m ? 1.f : __builtin_amdgcn_exp2f((v - m) * c); });
+  s = block(sh, f.lane, wave, s, true);
+  return (float)((double)m * inv_temp + log((double)s));
 }
 
-// The k largest of a row a workgroup: those above a bound that few columns reach, put in order.
+// The k largest of a row a workgroup: those above a bound that few columns reach, put in order; the pass that marks them also sums up the others, against the bound.  Bound by memory in the end,
+// by the steps that wait for each other before that.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
-  Search<NT> &sh = shared<NT>();
-  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const device_bytes at_row = (device_bytes)(x + t * ld * Piece<BF>::ES);
   using R = Row<BF, NT, NV>;
-  R row(at_row, V, R::aligned((const char *)at_row, V), tid, wave);
-  const Finder<BF, NT> f(sh, at_row, V, row.head, wave);
-  float mine, top, low;
-  extremes(row, sh, wave, lane, mine, top, low);
-  const int n = min(k, V);
-  const float from = bound_of(row, f, n, mine, top, low);
-  int found = from > -INFINITY ? collect(row, f, from) : 0;
-  if (found < n || found > kList) {
-    top_of_many<BF, NT>(at_row, V, row.head, wave, n, k, inv_temp, ids + t * ldk, values + t * ldk, rest ? rest + t : nullptr);
-    return;
-  }
-  write_top<BF, NT>(sh, tid, lane, wave, n, k, found, inv_temp, ids + t * ldk, values + t * ldk, rest ? rest + t : nullptr, [&](auto g) {  // every column that is not in the list
-    row.each([&](const Piece<BF> &y, int) {
+  Search<NT> &sh = shared<NT>();
+  const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = min(k, V);
+  const device_bytes at_row = (device_bytes)(x + t * ld * Piece<BF>::ES);
+  const int head = R::aligned((const char *)at_row, V);
+  const float c = (float)(1.4426950408889634 * inv_temp);
+  const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  float s = 0.f, from;
+  int found = 0;
+  {
+    R row(at_row, V, head, tid, wave);
+    float mine, top, low;
+    extremes(row, sh, wave, lane, mine, top, low);
+    from = bound_of(row, f, n, mine, top, low);
+    f.begin();
+    // (without a bound nothing is marked, and what is summed up is no number)
+    const float least = from > -INFINITY ? from : INFINITY;
+    auto add = [&](float v) { s += __builtin_amdgcn_exp2f(fmaxf((v - least) * c, -126.f)); };  // (also of no number)
+    row.each([&](const Piece<BF> &y, int v) {
+      Piece<BF> z = y;
+      if (y.most() >= least) {
+        f.mark(v);
+        uint32_t above = 0;
 #pragma unroll
-      for (int e = 0; e < Piece<BF>::N; ++e) g(y[e] < from ? y[e] : -INFINITY);
+        for (int e = 0; e < Piece<BF>::N; ++e) above |= (uint32_t)(y[e] >= least) << e;
+        z.clear(above);
+      }
+#pragma unroll
+      for (int e = 0; e < Piece<BF>::N; ++e) add(z[e]);
     });
-    g(row.xl < from ? row.xl : -INFINITY);
-  });
+    if (row.xl >= least) f.mark(row.pieces + tid);
+    else add(row.xl);
+    found = f.take([&](float v, int) { return v >= least; });
+  }
+  const bool quick = from > -INFINITY && found >= n && found <= kList;
+  if (!quick) found = list_of_many<BF, NT>(at_row, V, head, wave, n);
+  write_top<BF, NT>(sh, tid, n, k, found, ids + t * ldk, values + t * ldk);
+  if (!rest) return;
+  // the list's others may lie far above the bound: then against the largest of them
+  const float ref = uniform_of(found > n ? value_of(sh.sorted[n]) : from);
+  s *= __builtin_amdgcn_exp2f((from - ref) * c);
+  for (int i = n + tid; i < found; i += NT) s += __builtin_amdgcn_exp2f((value_of(sh.sorted[i]) - ref) * c);
+  s = block(sh, lane, wave, s, true);
+  float r = (float)((double)ref * inv_temp + log((double)s));
+  if (!quick || !(s > 0.02f)) r = rest_behind<BF, NT>(at_row, V, head, wave, uniform_of(sh.sorted[n - 1]), inv_temp);  // (the others are far below the bound, or there is none)
+  if (tid == 0) rest[t] = r;
 }
 
 // The kernel whose registers hold a row: few rows get more threads each.

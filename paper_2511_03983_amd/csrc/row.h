@@ -68,7 +68,8 @@ template <int BF, int NT, int NV> struct Row {
   float xl;
   device_bytes first;
   int head, pieces, mine, ends, end, tid;
-  __device__ __forceinline__ Row(device_bytes row, int V, int head_, int tid_, int wave) {
+  __device__ __forceinline__ Row(device_bytes row, int V, int head_, int tid_, int wave) { fetch(row, V, head_, tid_, wave); }
+  __device__ __forceinline__ void fetch(device_bytes row, int V, int head_, int tid_, int wave) {
     tid = tid_;
     head = head_;
     pieces = (V - head) / N;
