@@ -8,6 +8,7 @@ namespace {
 constexpr int kTop = 1024;   // the longest list
 constexpr int kList = 1536;  // columns that are put in order by comparing them with each other
 constexpr int kBins = 1024;
+constexpr int kFew = 256;    // bins of a workgroup's largest
 constexpr int kColumnBits = 20;
 constexpr int kTable = 512;
 
@@ -46,13 +47,14 @@ template <int NT> struct Search {
     unsigned long long amount[kBins];
     uint32_t count[kBins];
   } bins;
-  unsigned long long list[kList + 8];  // places that may be taken, in any order; then what the sorted ones weigh
+  unsigned long long list[kList];    // places that may be taken, in any order; then what the sorted ones weigh
   unsigned long long sorted[kList];
   static constexpr int kMarks = 2 * kList;
   __device__ __forceinline__ uint32_t *marks() { return reinterpret_cast<uint32_t *>(sorted); }  // pieces that hold columns for the list (before there are any in order)
   unsigned long long found[2], wave_sum[NT / 64];
   float most[NT / 64], least[NT / 64];
   double table[kTable];
+  float part[NT / 64];
   int n, marked;
 };
 
@@ -141,12 +143,7 @@ template <int BF, int NT> struct Finder {
       const int per = n / 64;
       unsigned long long s = 0, upto;
       for (int i = 0; i < per; ++i) s += bins[lane * per + ((i + lane) & (per - 1))];  // (in an order of its own: otherwise all lanes read from the same banks)
-      upto = s;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const unsigned long long u = __shfl_up(upto, o, 64);
-        if (lane >= o) upto += u;
-      }
+      upto = wave_sums(s);
       const uint64_t hit = __ballot(upto >= target);
       if (hit == 0) {
         if (lane == 63) { sh.found[0] = n; sh.found[1] = upto; }
@@ -270,20 +267,25 @@ template <int BF, int NT> struct Finder {
     return uniform_of(sh.n);
   }
 
+  // What bound_of and the first list need, before the first barrier
+  __device__ __forceinline__ void prepare() const {
+    clear(sh.bins.count, kFew);
+    if (tid == 0) sh.n = sh.marked = 0;
+  }
   // Puts the list's n places in order, in sh.sorted: the first `most` of them.
   __device__ __forceinline__ void sort(int n, int most) const { sort(sh, tid, n, most); }
   static __device__ __forceinline__ void sort(Search<NT> &sh, int tid, int n, int most) {
-    constexpr int U = 8;  // places that are read together (behind the list: none)
-    if (tid < U) sh.list[n + tid] = 0;
-    __syncthreads();
+    constexpr int U = 8;  // places that are read together
 #pragma unroll 1
     for (int i = tid; i < n; i += NT) {
       const unsigned long long p = sh.list[i];
-      int at = 0;
+      int at = 0, j = 0;
 #pragma unroll 1
-      for (int j = 0; j < n; j += U)
+      for (; j + U <= n; j += U)
 #pragma unroll
         for (int u = 0; u < U; ++u) at += sh.list[j + u] > p;
+#pragma unroll 1
+      for (; j < n; ++j) at += sh.list[j] > p;
       if (at < most) sh.sorted[at] = p;
     }
     __syncthreads();
@@ -308,9 +310,7 @@ template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Sear
 template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &row, const Finder<BF, NT> &f, int k, float mine, float top, float low) {
   const float span = top - low;
   if (k > NT || !(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
-  const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
-  f.clear(f.sh.bins.count, kBins);
-  __syncthreads();
+  const float scale = span > 0.f ? (kFew - 1) / span : 0.f;
   auto put = [&](float v) {
     if (v >= low) atomicAdd(&f.sh.bins.count[(int)((top - v) * scale)], 1u);
   };
@@ -320,13 +320,23 @@ template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &
     put(row.xl);
   }
   __syncthreads();
-  unsigned long long before;
-  const int b = f.find(f.sh.bins.count, kBins, k, before);
-  return b < kBins ? f.edge(b, top, scale) : -INFINITY;
+  // every wave for itself: the bin in which the count reaches k
+  const u32x4v own = *reinterpret_cast<const u32x4v *>(f.sh.bins.count + 4 * f.lane);
+  const uint32_t sum = (own[0] + own[1]) + (own[2] + own[3]), upto = wave_sums(sum);
+  const uint64_t hit = __ballot(upto >= (uint32_t)k);
+  if (!hit) return -INFINITY;
+  const int who = __builtin_ctzll(hit);
+  uint32_t before = upto - sum;
+  int b = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    before += own[i];
+    b += before < (uint32_t)k;
+  }
+  return f.edge(4 * who + __builtin_amdgcn_readlane(b, who), top, scale);
 }
 // the list from the columns at `from` and above; their number, which may be more than the list holds
 template <int BF, int NT, class R> __device__ __forceinline__ int collect(R &row, const Finder<BF, NT> &f, float from) {
-  f.begin();
   row.each([&](const typename R::P16 &y, int v) {
     if (y.most() >= from) f.mark(v);
   });
@@ -426,14 +436,9 @@ struct Sums {
     per = (n + 63) / 64;
     own = 0;
     for (int i = lane * per; i < min(n, lane * per + per); ++i) own += weights[i];
-    unsigned long long upto = own;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned long long u = __shfl_up(upto, o, 64);
-      if (lane >= o) upto += u;
-    }
+    const unsigned long long upto = wave_sums(own);
     before = upto - own;
-    total = __shfl(upto, 63, 64);
+    total = last_of(upto);
   }
   // the first of them up to which they weigh `target`, and what they do (target at most the total)
   __device__ __forceinline__ int reach(unsigned long long target, unsigned long long &upto) const {
@@ -614,6 +619,7 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
   }
   R row(at_row, V, head, tid, wave);
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
+  f.prepare();
   float mine, top, low;
   extremes(row, sh, wave, lane, mine, top, low);
   const float from = bound_of(row, f, k, mine, top, low);
@@ -657,15 +663,15 @@ __device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int n, int k,
     values[i] = i < n ? value_of(p) : -INFINITY;
   }
 }
-// Over the workgroup: the sum, or the largest
+// Over the workgroup: the sum, or the largest.  (Each kind once between two barriers of another step.)
 template <int NT> __device__ __forceinline__ float block(Search<NT> &sh, int lane, int wave, float v, bool sum) {
   v = sum ? wave_add(v) : wave_max(v);
+  float *all = sum ? sh.part : sh.most;
+  if (lane == 0) all[wave] = v;
   __syncthreads();
-  if (lane == 0) sh.most[wave] = v;
-  __syncthreads();
-  v = sh.most[0];
+  v = all[0];
 #pragma unroll
-  for (int w = 1; w < NT / 64; ++w) v = sum ? v + sh.most[w] : fmaxf(v, sh.most[w]);
+  for (int w = 1; w < NT / 64; ++w) v = sum ? v + all[w] : fmaxf(v, all[w]);
   return uniform_of(v);
 }
 // The log-sum-exp over the temperature of a row's columns behind the place `last`, -infinity where there are none.
@@ -702,10 +708,10 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   int found = 0;
   {
     R row(at_row, V, head, tid, wave);
+    f.prepare();
     float mine, top, low;
     extremes(row, sh, wave, lane, mine, top, low);
     from = bound_of(row, f, n, mine, top, low);
-    f.begin();
     // (without a bound nothing is marked, and what is summed up is no number)
     const float least = from > -INFINITY ? from : INFINITY;
     auto add = [&](float v) { s += __builtin_amdgcn_exp2f(fmaxf((v - least) * c, -126.f)); };  // (also of no number)

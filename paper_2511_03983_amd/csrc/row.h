@@ -48,15 +48,48 @@ template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, f
   else reinterpret_cast<float *>(row)[c] = v;
 }
 
-template <class T> __device__ __forceinline__ T wave_add(T v) {
+// v of another lane, by the data-parallel moves of the vector unit (an eighth of what a trip through LDS takes): CTRL row_shr:1 to 8 (0x111 ..), row_bcast:15 and :31 (0x142, 0x143) for the rows of
+// ROWS; lanes that have no such neighbour get `none`.
+template <int CTRL, int ROWS, class T> __device__ __forceinline__ T moved(T none, T v) {
+  constexpr int W = sizeof(T) / 4;
+  uint32_t a[W], b[W];
+  __builtin_memcpy(a, &none, sizeof(T));
+  __builtin_memcpy(b, &v, sizeof(T));
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  for (int w = 0; w < W; ++w) a[w] = __builtin_amdgcn_update_dpp(a[w], b[w], CTRL, ROWS, 0xf, false);
+  __builtin_memcpy(&v, a, sizeof(T));
   return v;
 }
-__device__ __forceinline__ float wave_max(float v) {
+// v of lane 63, in all lanes
+template <class T> __device__ __forceinline__ T last_of(T v) {
+  constexpr int W = sizeof(T) / 4;
+  uint32_t a[W];
+  __builtin_memcpy(a, &v, sizeof(T));
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  for (int w = 0; w < W; ++w) a[w] = __builtin_amdgcn_readlane(a[w], 63);
+  __builtin_memcpy(&v, a, sizeof(T));
   return v;
+}
+// Sums over the lanes up to each: along the rows of 16, then over them
+template <class T> __device__ __forceinline__ T wave_sums(T v) {
+  const T zero = 0;
+  v += moved<0x111, 0xf>(zero, v);
+  v += moved<0x112, 0xf>(zero, v);
+  v += moved<0x114, 0xf>(zero, v);
+  v += moved<0x118, 0xf>(zero, v);
+  v += moved<0x142, 0xa>(zero, v);
+  v += moved<0x143, 0xc>(zero, v);
+  return v;
+}
+template <class T> __device__ __forceinline__ T wave_add(T v) { return last_of(wave_sums(v)); }
+__device__ __forceinline__ float wave_max(float v) {
+  v = fmaxf(v, moved<0x111, 0xf>(v, v));
+  v = fmaxf(v, moved<0x112, 0xf>(v, v));
+  v = fmaxf(v, moved<0x114, 0xf>(v, v));
+  v = fmaxf(v, moved<0x118, 0xf>(v, v));
+  v = fmaxf(v, moved<0x142, 0xa>(v, v));
+  v = fmaxf(v, moved<0x143, 0xc>(v, v));
+  return last_of(v);
 }
 
 // The row as NV pieces a thread, beginning where an address is aligned (`head` columns on); the columns before and behind the pieces, `ends` of them, are a thread's each (xl, column `end`).
