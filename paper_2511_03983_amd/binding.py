@@ -590,13 +590,22 @@ class Context:
         T, ld, f32 = self._logits(logits)
         if rules is not None and not (rules.T in (None, T) and rules.gpu in (None, self.gpu)):
             _refuse(f"rules: need {T} rows on {self.device}")
-        tokens = self._empty(torch.int32, T) if tokens is None else tokens
-        logprobs = self._empty(torch.float32, T) if logprobs is None else logprobs
-        kept = self._empty(torch.int32, T) if kept is None else kept
         if uniform is None:
             _refuse("uniform: a draw needs its random numbers")
+        if tokens is None:
+            tokens = self._empty(torch.int32, T)
+        else:
+            _ints(tokens, T, "tokens", self.gpu)
+        if logprobs is None:
+            logprobs = self._empty(torch.float32, T)
+        else:
+            _ints(logprobs, T, "logprobs", self.gpu, torch.float32)
+        if kept is None:
+            kept = self._empty(torch.int32, T)
+        else:
+            _ints(kept, T, "kept", self.gpu)
         self._call(lib.twist_draw_raw, logits.data_ptr(), ld, f32, T, _ints(uniform, T, "uniform", self.gpu, torch.float32), None if rules is None else rules.ref,
-                   _ints(tokens, T, "tokens", self.gpu), _ints(logprobs, T, "logprobs", self.gpu, torch.float32), _ints(kept, T, "kept", self.gpu))
+                   tokens.data_ptr(), logprobs.data_ptr(), kept.data_ptr())
         return tokens, logprobs, kept
 
     def twist_top_logits_raw(self, logits: torch.Tensor, k: int, temperature: float = 1.0, ids: torch.Tensor | None = None, values: torch.Tensor | None = None,
@@ -604,17 +613,19 @@ class Context:
         """(ids int32 [T, k], values fp32 [T, k], rest fp32 [T]): the k largest of logits [T, vocab] (fp32 or the model's type) in order, and the log-sum-exp of the
         others over the temperature.  Tensors that are given receive the results (ids and values: one row stride).  See include/twist.h."""
         T, ld, f32 = self._logits(logits)
-        if ids is None:
-            ids = self._empty(torch.int32, T, k)
-        if values is None:
-            values = self._empty(torch.float32, T, k)
         if rest is None:
             rest = self._empty(torch.float32, T)
-        ldk = self._rows(ids, T, k, "ids", torch.int32)
-        if self._rows(values, T, k, "values", torch.float32) != ldk:
-            _refuse("ids and values: need one row stride")
-        self._call(lib.twist_top_logits_raw, logits.data_ptr(), ld, f32, T, k, temperature, ids.data_ptr(), values.data_ptr(), ldk,
-                   _ints(rest, T, "rest", self.gpu, torch.float32))
+        else:
+            _ints(rest, T, "rest", self.gpu, torch.float32)
+        if ids is None and values is None:
+            ids, values, ldk = self._empty(torch.int32, T, max(k, 1)), self._empty(torch.float32, T, max(k, 1)), k
+        else:
+            ids = self._empty(torch.int32, T, k) if ids is None else ids
+            values = self._empty(torch.float32, T, k) if values is None else values
+            ldk = self._rows(ids, T, k, "ids", torch.int32)
+            if self._rows(values, T, k, "values", torch.float32) != ldk:
+                _refuse("ids and values: need one row stride")
+        self._call(lib.twist_top_logits_raw, logits.data_ptr(), ld, f32, T, k, temperature, ids.data_ptr(), values.data_ptr(), ldk, rest.data_ptr())
         return ids, values, rest
 
     def twist_distill_raw(self, logits: torch.Tensor, targets: torch.Tensor | None, teacher: "Teacher", grad: torch.Tensor | None = None):
