@@ -73,7 +73,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   float xl = tid < ends ? load1<BF>(row, end) : -INFINITY;
   const float aim = aimed ? load1<BF>(row, tgt) : 0.f;
   const double tau = te.temperature, inv_tau = 1.0 / tau;
-  for (int i = tid; i < V / 32 + 1; i += NT) in_set[i] = 0;
+  for (int i = tid; i < (V + N + 31) / 32; i += NT) in_set[i] = 0;
   if (tid == 0) twice = 0;
   auto bit = [&](int c) { return c - head + N; };  // of a column, in the table
   __syncthreads();

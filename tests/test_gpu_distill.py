@@ -116,6 +116,20 @@ def test_distill(lib, dtype, V):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("V", [25, 29, 31, 63, 95, 1023, 8191, 32767, 65535, 65563])
+def test_distill_last_columns(lib, dtype, V):
+    """A row's last columns in a list, then in none: nothing of a list stays for the next one."""
+    ctx, g = _ctx(lib, V, dtype), _gen(V + 7)
+    T, k = 4, min(V, 40)
+    for _ in range(2):
+        x = _logits(g, T, V).to(DT[dtype])
+        for ids in (torch.arange(V - k, V), torch.arange(1)):
+            ids = ids.to(torch.int32).expand(T, -1).contiguous().cuda()
+            values = torch.randn(ids.shape, generator=g, device="cuda")
+            _check(ctx, lib, x, _targets(g, ids, V), ids, values, torch.zeros(T, device="cuda"), 2.0, 0.5)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("V", [7, 1003, 50257, 70000])
 def test_distill_lists(lib, dtype, V):
     """Entries that are not there, tokens that are named twice and more often, lists of whole vocabularies, entries of no probability, rows without a teacher, a target or both."""
