@@ -116,9 +116,20 @@ template <int BF, int NT> struct Finder {
   }
   // the number by which a run is marked
   __device__ __forceinline__ int piece_of(int c, int n) const { return n > 1 ? (c - head) / N : pieces + tid; }
-  // f(logit, column) of every column
-  template <class F> __device__ __forceinline__ void columns(F f) const {
-    runs<4>([&](const float *x, int c, int n) {
+  // f(logit, column) of every column.  SHORT: in one copy of f for each piece on its way instead of one for each of its logits, for functions of many passes.  A branch reaches 128 KiB; in a function
+  // beyond that the compiler jumps through the registers of the return address, and the call does not return.
+  template <bool SHORT = false, class F> __device__ __forceinline__ void columns(F f) const {
+    if (SHORT)
+      runs<2>([&](const float *x, int c, int n) {
+#pragma unroll 1
+        for (int e = 0; e < (n > 1 ? N : 1); ++e) {
+          float v = x[0];
+#pragma unroll
+          for (int j = 1; j < N; ++j) v = e == j ? x[j] : v;
+          f(v, c + e);
+        }
+      });
+    else runs<4>([&](const float *x, int c, int n) {
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (e == 0 || n > 1) f(x[e], c + e);
@@ -150,7 +161,7 @@ template <int BF, int NT> struct Finder {
       } else if (lane == __builtin_ctzll(hit)) {
         upto -= s;
         int b = lane * per;
-        while (upto + bins[b] < target) upto += bins[b++];
+        for (const int end = b + per - 1; b < end && upto + bins[b] < target; ++b) upto += bins[b];
         sh.found[0] = b;
         sh.found[1] = upto;
       }
@@ -161,7 +172,7 @@ template <int BF, int NT> struct Finder {
   }
 
   // The last place of the shortest beginning of the row whose columns' amounts add up to `target` (at least 1, at most the whole row's), a few bits of the places at a time.
-  template <class F> __device__ __forceinline__ uint64_t reach(unsigned long long target, F amount) const {
+  template <bool SHORT = false, class F> __device__ __forceinline__ uint64_t reach(unsigned long long target, F amount) const {
     uint64_t prefix = 0;
     int shift = 32 + kColumnBits;
 #pragma unroll 1
@@ -171,7 +182,7 @@ template <int BF, int NT> struct Finder {
       __syncthreads();
       clear(sh.bins.amount, bins);
       __syncthreads();
-      columns([&](float v, int c) {
+      columns<SHORT>([&](float v, int c) {
         const uint64_t p = place(v, c);
         if (p >> above != prefix) return;
         const unsigned long long a = amount(v, p);
@@ -470,7 +481,7 @@ struct Settings {
     const double s = ceil(part * (double)total);
     return s >= 1.0 ? min((unsigned long long)s, total) : 1ull;
   }
-  __device__ __forceinline__ unsigned long long draw_at(unsigned long long total) const { return u > 0.f ? min((unsigned long long)((double)u * (double)total), total - 1) + 1 : 1ull; }
+  __device__ __forceinline__ unsigned long long draw_at(unsigned long long total) const { return u > 0.f ? min((unsigned long long)((double)fminf(u, 1.f) * (double)total), total - 1) + 1 : 1ull; }
 };
 
 // A token of a row of which many columns may be kept: the probabilities of the whole row are added up in bins of their size, and the columns of the bin in which a sum (top_p's, the random
@@ -498,8 +509,8 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
   uint64_t last = 0;  // the last place that is kept
   if (k > 1 && k < V) {
     unsigned long long n = 0;
-    f.columns([&](float v, int) { n += v > -INFINITY; });
-    if ((unsigned long long)k < f.block_add(n)) last = f.reach(k, [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; });
+    f.template columns<true>([&](float v, int) { n += v > -INFINITY; });
+    if ((unsigned long long)k < f.block_add(n)) last = f.template reach<true>(k, [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; });
   }
   // bins of equal width from the largest logit down to the smallest, or to where probabilities are below 2^-48
   const float span = fminf(top - lowest, 48.f * (float)(1.0 / slow.c)), scale = span > 0.f && span < INFINITY ? (kBins - 1) / span : 0.f;
@@ -527,7 +538,7 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
     f.find(sh.bins.amount, kBins, ~0ull, total);
   } else {
     unsigned long long n = 0;
-    f.columns([&](float v, int c) { n += place(v, c) >= last ? slow(v) : 0; });
+    f.template columns<true>([&](float v, int c) { n += place(v, c) >= last ? slow(v) : 0; });
     total = f.block_add(n);
   }
   // The place at which the sum from the first on reaches `target`, and the sum up to it.  `also` sees every column.
@@ -565,12 +576,12 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
         upto = uniform_of(sh.found[1]);
         return uniform_of(sh.found[0]);
       }
-    } else f.columns(also);
+    } else f.template columns<true>(also);
     binned = false;  // (reach takes the bins)
     auto mass = [&](float v) { return usable ? quick(v) : slow(v); };
-    const uint64_t at = f.reach(target, [&](float v, uint64_t q) -> unsigned long long { return q >= last ? mass(v) : 0; });
+    const uint64_t at = f.template reach<true>(target, [&](float v, uint64_t q) -> unsigned long long { return q >= last ? mass(v) : 0; });
     unsigned long long s = 0;
-    f.columns([&](float v, int c) {
+    f.template columns<true>([&](float v, int c) {
       if (place(v, c) >= at) s += mass(v);
     });
     upto = f.block_add(s);
@@ -581,7 +592,7 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
   if (probable > last) {
     last = probable;
     unsigned long long s = 0;
-    f.columns([&](float v, int) {
+    f.template columns<true>([&](float v, int) {
       if (v >= least) s += usable ? quick(v) : slow(v);
     });
     total = f.block_add(s);
