@@ -756,12 +756,15 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   if (tid == 0) rest[t] = r;
 }
 
-// The kernel whose registers hold a row: few rows get more threads each.
+// The kernel whose registers hold a row.  A CU holds one workgroup of 1024 threads, two of 512 or four of 256: while every CU has a row at most, 1024 threads are through it sooner, with more rows
+// it is several rows side by side that keep the memory busy while each has its steps to wait for (drawing from the top 50, bf16: 256 x 32000 10.6 us with 1024 threads, 13.3 with 256; 512 x 32000
+// 20.4 and 17.3, 4096 x 32000 147 and 77; 4096 x 50257 172 and, with 512, 120; fp32 4096 x 16384 127 and 72, 4096 x 32000 182 and 128).  The largest 64 of a row likewise.
+constexpr int kManyRows = 256;  // one for every CU
 #define ROWS_BF16(LAUNCH)                              \
   do {                                                 \
     if (V <= 4 * 8 * 256) LAUNCH(1, 256, 4);           \
-    else if (T > 512 && V <= 16 * 8 * 256) LAUNCH(1, 256, 16); \
-    else if (T > 512 && V <= 16 * 8 * 512) LAUNCH(1, 512, 16); \
+    else if (T > kManyRows && V <= 16 * 8 * 256) LAUNCH(1, 256, 16); \
+    else if (T > kManyRows && V <= 16 * 8 * 512) LAUNCH(1, 512, 16); \
     else if (V <= 4 * 8 * 1024) LAUNCH(1, 1024, 4);    \
     else if (V <= 8 * 8 * 1024) LAUNCH(1, 1024, 8);    \
     else LAUNCH(1, 1024, 0);                           \
@@ -769,7 +772,8 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
 #define ROWS_F32(LAUNCH)                               \
   do {                                                 \
     if (V <= 4 * 4 * 256) LAUNCH(0, 256, 4);           \
-    else if (T > 512 && V <= 16 * 4 * 256) LAUNCH(0, 256, 16); \
+    else if (T > kManyRows && V <= 16 * 4 * 256) LAUNCH(0, 256, 16); \
+    else if (T > kManyRows && V <= 16 * 4 * 512) LAUNCH(0, 512, 16); \
     else if (V <= 4 * 4 * 1024) LAUNCH(0, 1024, 4);    \
     else if (V <= 16 * 4 * 1024) LAUNCH(0, 1024, 16);  \
     else LAUNCH(0, 1024, 0);                           \

@@ -259,3 +259,36 @@ def test_top_logits_many_rows(lib):
     V, T = 1003, 3000
     ctx, g = _ctx(lib, V, "bf16"), _gen(2)
     _check_top(ctx, _logits(g, T, V).bfloat16(), 12, rows=range(0, T, 61))
+
+
+# ------------------------------------------------------------------------------------------------ both, of many rows
+@pytest.mark.parametrize("V", [4097, 9001, 16384, 16387, 32000, 32768, 40001, 50257, 65536])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_rows_side_by_side(lib, dtype, V):
+    """More rows than one for every CU, 264 of 22 kinds, which other kernels take than few rows: what they give for a kind is right and the same for all of its rows."""
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(V + 11)
+    kinds = [_logits(g, 3, V, k) for k in ("model", "flat", "steps", "masked", "wide")]
+    special = torch.zeros((7, V), device="cuda")
+    special[0] = -math.inf
+    special[1] = math.nan
+    special[2, V - 1] = math.inf
+    special[3] = -2000.0
+    special[3, V // 2] = 0.0
+    special[4, ::3] = math.nan
+    special[5] = torch.arange(V, device="cuda") / 64
+    n, times = 22, 12
+    few = torch.cat(kinds + [special]).to(dt)
+    whole = torch.zeros((n * times, V + 3), dtype=dt, device="cuda")
+    x = whole[:, :V]
+    x.copy_(few.repeat(times, 1))
+    u = torch.rand(n, generator=g, device="cuda")
+    for which in ("", "k", "p", "m", "tkpm"):
+        rules = {k: v if v is None else v.repeat(times) for k, v in _rules(g, n, V, which).items()}
+        for got in _check(ctx, lib, x, u.repeat(times), rows=range(n), **rules):
+            assert (got.view(times, n) == got[:n]).all()
+    for k in (1, 64, 300, 1024):
+        ids, values, rest = _check_top(ctx, x, k, 0.7, rows=range(0, 4 * n, 3))
+        for got in (ids, values):
+            assert (got.view(times, n, k) == got[:n]).all()
+        assert (rest.view(times // 4, 4 * n) == rest[: 4 * n]).all()   # a sum in 32 bits, grouped by aligned addresses, which a row has again 4 n rows on
