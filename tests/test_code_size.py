@@ -60,4 +60,4 @@ def test_called_device_functions_are_within_the_reach_of_a_branch():
                 called[i, name] = size
     assert kernels > 100                                        # the bundles were read
     assert any("draw_of_many" in name for _, name in called)       # and what is called is among them
-    assert {n: s for n, s in called.items() if s > REACH // 2} == {}
+    assert {n: s for n, s in called.items() if s > REACH * 3 // 4} == {}
