@@ -32,7 +32,7 @@ __device__ __forceinline__ float exp_f32(double x) {
 // A row a workgroup.  The row's tokens are the teacher's (the set) and the others, whose share of the distribution is formed from themselves and not as what the set leaves: it may be
 // next to nothing, or all but everything.  With tau the temperature, p and q over the set and over the others together (P, Q of them), the gradient of
 // KL(q || p) is (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.
-// Bound by memory: the row is read once and its gradient written once.  It stays in registers as it came (NV pieces of 16 bytes a thread; rows that NT threads cannot hold, NV = 0, are read
+// Bound by memory: the row is read once and its gradient written once (64 entries, 8192 x 50257 bf16: 342 us, 4.8 TB/s, the rate of a copy; 1024 x 50257 fp32, one row a CU at a time: 112 us, 3.7).  It stays in registers as it came (NV pieces of 16 bytes a thread; rows that NT threads cannot hold, NV = 0, are read
 // three times), the set's columns as -infinity, so that they weigh nothing in the others' sums; their own gradients, a thread each and in 64 bits where they meet a logarithm, are stored over
 // the others' behind a barrier.
 // Pieces begin where the gradient's row is aligned, which is where the logits' is as a rule (rows of an odd vocabulary start anywhere; 8192 x 50257 bf16 from any element on 554 us, all rows

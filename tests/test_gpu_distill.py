@@ -265,3 +265,22 @@ def test_distill_refuses_what_does_not_fit(lib):
                  lambda: ctx.twist_distill_raw(x, y, lib.Teacher(ids, values, weight=1.5)), lambda: ctx.twist_distill_raw(x, y, lib.Teacher(ids, values, temperature=0.0))):
         with pytest.raises(lib.TwistError):
             call()
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_distill_largest_vocabulary(lib, dtype):
+    V, T = 2 ** 20 - 1, 2
+    ctx, g = _ctx(lib, V, dtype), _gen(23)
+    x = _logits(g, T, V).to(DT[dtype])
+    ids, values, rest = _teacher(g, x, 300, 2.0)
+    _check(ctx, lib, x, _targets(g, ids, V), ids, values, rest, 2.0, 0.5)
+
+
+def test_distill_rows_beyond_32_bits(lib):
+    """Rows of logits and gradient so far apart that the last begin behind 2^32 elements."""
+    V, T, ld = 1003, 5, 2 ** 30 + 8
+    ctx, g = _ctx(lib, V, "bf16"), _gen(24)
+    x, grad = (torch.empty((T - 1) * ld + V, dtype=torch.bfloat16, device="cuda").as_strided((T, V), (ld, 1)) for _ in range(2))
+    x.copy_(_logits(g, T, V))
+    ids, values, rest = _teacher(g, x, 30, 2.0)
+    _check(ctx, lib, x, _targets(g, ids, V), ids, values, rest, 2.0, 0.5, grad=grad)

@@ -292,3 +292,28 @@ def test_rows_side_by_side(lib, dtype, V):
         for got in (ids, values):
             assert (got.view(times, n, k) == got[:n]).all()
         assert (rest.view(times // 4, 4 * n) == rest[: 4 * n]).all()   # a sum in 32 bits, grouped by aligned addresses, which a row has again 4 n rows on
+
+
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_largest_vocabulary(lib, dtype):
+    dt, model = DTYPES[dtype]
+    V, T = 2 ** 20 - 1, 2
+    ctx, g = _ctx(lib, V, model), _gen(21)
+    for kind in ("model", "flat"):
+        x = _logits(g, T, V, kind).to(dt)
+        for which in ("", "k", "p", "m"):
+            _check(ctx, lib, x, torch.rand(T, generator=g, device="cuda"), **_rules(g, T, V, which))
+        for k in (1, 200, 1024):
+            _check_top(ctx, x, k)
+
+
+def test_rows_beyond_32_bits(lib):
+    """Rows so far apart that the last begin behind 2^32 elements."""
+    V, T, ld = 1003, 5, 2 ** 30 + 1
+    ctx, g = _ctx(lib, V, "bf16"), _gen(22)
+    x = torch.empty((T - 1) * ld + V, dtype=torch.bfloat16, device="cuda").as_strided((T, V), (ld, 1))
+    near = _logits(g, T, V).bfloat16()
+    x.copy_(near)
+    u = torch.rand(T, generator=g, device="cuda")
+    for far, here in ((ctx.twist_draw_raw(x, u), ctx.twist_draw_raw(near, u)), (ctx.twist_top_logits_raw(x, 20), ctx.twist_top_logits_raw(near, 20))):
+        assert torch.equal(far[0], here[0]) and (far[1] - here[1]).abs().max() == 0 and (far[2] - here[2]).abs().max() <= 1e-5   # (rest, grouped differently: twice 38 u and 8 u)
