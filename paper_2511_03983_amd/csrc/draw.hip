@@ -11,6 +11,7 @@ constexpr int kBins = 1024;
 constexpr int kFew = 256;    // bins of a workgroup's largest
 constexpr int kColumnBits = 20;
 constexpr int kTable = 512;
+constexpr int kByBins = 64;  // longer lists are put in order by bins
 
 // Unsigned numbers in the order of a row's columns: the logit's place in 32 bits, the column (turned over) below it.  Columns that hold no number count as -infinity, -0 is 0.
 __device__ __forceinline__ uint64_t place(float v, int c) {
@@ -55,6 +56,7 @@ template <int NT> struct Search {
   float most[NT / 64], least[NT / 64];
   double table[kTable];
   float part[NT / 64];
+  float hi, lo;  // of list_of_many's list
   int n, marked;
 };
 
@@ -218,8 +220,8 @@ template <int BF, int NT> struct Finder {
     least = uniform_of(l);
   }
   // A logit that k columns at least are not below (none above -infinity is, where there are fewer), by counting all in bins.  -infinity: no bins for them.
-  __device__ __forceinline__ float bound_of_all(int k) const {
-    float top, l;
+  __device__ __forceinline__ float bound_of_all(int k, float &top) const {
+    float l;
     extremes(top, l);
     const float span = top - l;
     if (!(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
@@ -301,6 +303,41 @@ template <int BF, int NT> struct Finder {
     }
     __syncthreads();
   }
+  // The same of places from `hi` down to `lo` (not below it), all of them: counted in bins, put together by bin, and compared with those of their own bin alone.  Top 32, 64, 256 of
+  // 2048 x 32000 bf16: 42.8, 48.7 and 56.4 us, by comparing all with all 42.0, 51.0 and 72.9; top 512 of 2048 x 50257 104 and 166; 64 x 50257 fp32, top 64 and 1000, 11.7 and 19.4 against 12.0 and 55.8.
+  static __device__ __forceinline__ void sort_by_bins(Search<NT> &sh, int tid, int n, float hi, float scale) {
+    uint32_t *bins = sh.bins.count;
+    auto bin = [&](uint64_t p) { return min((int)((hi - value_of(p)) * scale), kFew - 1); };
+    for (int i = tid; i < kFew; i += NT) bins[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) atomicAdd(&bins[bin(sh.list[i])], 1u);
+    __syncthreads();
+    if (tid < 64) {
+      u32x4v &own = *reinterpret_cast<u32x4v *>(bins + 4 * tid);
+      const u32x4v c = own;
+      const uint32_t sum = (c[0] + c[1]) + (c[2] + c[3]), before = wave_sums(sum) - sum;
+      own = u32x4v{before, before + c[0], before + c[0] + c[1], before + c[0] + c[1] + c[2]};
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) {
+      const uint64_t p = sh.list[i];
+      sh.sorted[atomicAdd(&bins[bin(p)], 1u)] = p;  // (afterwards a bin's number is where the next one begins)
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < n; i += NT) {
+      const uint64_t p = sh.sorted[i];
+      const int b = bin(p), end = bins[b];
+      const int start = b ? bins[b - 1] : 0;
+      int at = start;
+#pragma unroll 1
+      for (int j = start; j < end; ++j) at += sh.sorted[j] > p;
+      sh.list[at] = p;
+    }
+    __syncthreads();
+    for (int i = tid; i < n; i += NT) sh.sorted[i] = sh.list[i];
+    __syncthreads();
+  }
 };
 
 // The row's largest logit (the thread's: `mine`), and the smallest of the threads' largest
@@ -360,10 +397,12 @@ template <int BF, int NT, class R> __device__ __forceinline__ int collect(R &row
 template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(device_bytes at_row, int V, int head, int wave, int k) {
   Search<NT> &sh = shared<NT>();
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
-  const float from = f.bound_of_all(k);
+  float top;
+  const float from = f.bound_of_all(k, top);
   int n = 0;
-  auto list = [&](auto wanted) {
+  auto list = [&](float lo, auto wanted) {
     f.begin();
+    if (f.tid == 0) { sh.hi = top; sh.lo = lo; }
     f.template runs<4>([&](const float *x, int c, int n) {
       bool any = false;
 #pragma unroll
@@ -372,10 +411,10 @@ template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(
     });
     return f.take(wanted);
   };
-  if (from > -INFINITY) n = list([&](float v, int) { return v >= from; });
+  if (from > -INFINITY) n = list(from, [&](float v, int) { return v >= from; });
   if (n < k || n > kList) {
     const uint64_t last = k < V ? f.reach(k, [](float, uint64_t) -> unsigned long long { return 1; }) : 0;
-    n = list([&](float v, int c) { return place(v, c) >= last; });
+    n = list(last ? value_of(last) : -INFINITY, [&](float v, int c) { return place(v, c) >= last; });
   }
   return n;
 }
@@ -696,8 +735,10 @@ __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, 
 
 // The list of `found` places put in order and its first n written (and k - n entries that are not there).
 template <int BF, int NT>
-__device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int n, int k, int found, int32_t *ids, float *values) {
-  Finder<BF, NT>::sort(sh, tid, found, found);
+__device__ __forceinline__ void write_top(Search<NT> &sh, int tid, int n, int k, int found, float hi, float lo, int32_t *ids, float *values) {
+  const float scale = (kFew - 1) / (hi - lo);  // (of a list that reaches from or to infinity: 0, or no number)
+  if (found > kByBins && scale > 0.f && scale < INFINITY) Finder<BF, NT>::sort_by_bins(sh, tid, found, hi, scale);
+  else Finder<BF, NT>::sort(sh, tid, found, found);
   for (int i = tid; i < k; i += NT) {
     const uint64_t p = i < n ? sh.sorted[i] : 0;
     ids[i] = i < n ? column_of(p) : -1;
@@ -735,7 +776,7 @@ template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind
 }
 
 // The k largest of a row a workgroup: those above a bound that few columns reach, put in order; the pass that marks them also sums up the others, against the bound.  Bound by memory in the end,
-// by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 253 us (3.2 TB/s), the top 256 of 2048 x 32000 in 75, where putting them in order is the longest step.
+// by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 253 us (3.2 TB/s), the top 256 of 2048 x 32000 in 56.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
   using R = Row<BF, NT, NV>;
@@ -745,7 +786,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   const int head = R::aligned((const char *)at_row, V);
   const float c = (float)(1.4426950408889634 * inv_temp);
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
-  float s = 0.f, from;
+  float s = 0.f, from, largest;
   int found = 0;
   {
     R row(at_row, V, head, tid, wave);
@@ -753,6 +794,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
     float mine, top, low;
     extremes(row, sh, wave, lane, mine, top, low);
     from = bound_of(row, f, n, mine, top, low);
+    largest = top;
     // (without a bound nothing is marked, and what is summed up is no number)
     const float least = from > -INFINITY ? from : INFINITY;
     auto add = [&](float v) { s += __builtin_amdgcn_exp2f(fmaxf((v - least) * c, -126.f)); };  // (also of no number)
@@ -774,7 +816,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   }
   const bool quick = from > -INFINITY && found >= n && found <= kList;
   if (!quick) found = list_of_many<BF, NT>(at_row, V, head, wave, n);
-  write_top<BF, NT>(sh, tid, n, k, found, ids + t * ldk, values + t * ldk);
+  write_top<BF, NT>(sh, tid, n, k, found, quick ? largest : sh.hi, quick ? from : sh.lo, ids + t * ldk, values + t * ldk);
   if (!rest) return;
   // the list's others may lie far above the bound: then against the largest of them
   const float ref = uniform_of(found > n ? value_of(sh.sorted[n]) : from);
