@@ -776,7 +776,7 @@ template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind
 }
 
 // The k largest of a row a workgroup: those above a bound that few columns reach, put in order; the pass that marks them also sums up the others, against the bound.  Bound by memory in the end,
-// by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 253 us (3.2 TB/s), the top 256 of 2048 x 32000 in 56.
+// by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 248 us (3.3 TB/s), the top 256 of 2048 x 32000 in 58.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
   using R = Row<BF, NT, NV>;
