@@ -1,5 +1,6 @@
 // What is taken from a row of logits: a token drawn from it, or its k largest.  A row's columns have one order, larger logits first and equal ones by column; everything here is a
 // beginning of it.
+#include "bins.h"
 #include "nn.h"
 #include "row.h"
 
@@ -225,7 +226,7 @@ template <int BF, int NT> struct Finder {
     extremes(top, l);
     const float span = top - l;
     if (!(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
-    const float scale = span > 0.f ? (kBins - 1) / span : 0.f;
+    const float scale = bin_scale(kBins, span);
     clear(sh.bins.count, kBins);
     __syncthreads();
     columns([&](float v, int) {
@@ -234,13 +235,7 @@ template <int BF, int NT> struct Finder {
     __syncthreads();
     unsigned long long before;
     const int b = find(sh.bins.count, kBins, k, before);
-    return b < kBins ? edge(b, top, scale) : l;
-  }
-  // a logit that none in bins 0 .. b is below, by the arithmetic that puts them there
-  static __device__ __forceinline__ float edge(int b, float top, float scale) {
-    if (scale == 0.f) return top;
-    const float e = top - (b + 1) / scale;
-    return e - (4e-7f * (fabsf(top) + fabsf(e)) + 1e-37f);
+    return b < kBins ? bin_edge(b, top, scale) : l;
   }
   // The list of the row's columns that are `wanted(logit, column)`, in two steps: pieces (and, behind their numbers, the columns in none) that hold one are marked in a pass over the row, and
   // looked through afterwards, a thread each.  A pass marks in few instructions; with what the list takes behind every column it is code that was not fetched before (2.4 and 6.4 us where both steps take
@@ -358,7 +353,7 @@ template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Sear
 template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &row, const Finder<BF, NT> &f, int k, float mine, float top, float low) {
   const float span = top - low;
   if (k > NT || !(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
-  const float scale = span > 0.f ? (kFew - 1) / span : 0.f;
+  const float scale = bin_scale(kFew, span);
   auto put = [&](float v) {
     if (v >= low) atomicAdd(&f.sh.bins.count[(int)((top - v) * scale)], 1u);
   };
@@ -381,7 +376,7 @@ template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &
     before += own[i];
     b += before < (uint32_t)k;
   }
-  return f.edge(4 * who + __builtin_amdgcn_readlane(b, who), top, scale);
+  return bin_edge(4 * who + __builtin_amdgcn_readlane(b, who), top, scale);
 }
 // the list from the columns at `from` and above; their number, which may be more than the list holds
 template <int BF, int NT, class R> __device__ __forceinline__ int collect(R &row, const Finder<BF, NT> &f, float from) {
@@ -581,7 +576,7 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
     }
   }
   // bins of equal width from the largest logit down to the smallest, or to where probabilities are below 2^-48
-  const float span = fminf(top - lowest, 48.f * (float)(1.0 / slow.c)), scale = span > 0.f && span < INFINITY ? (kBins - 1) / span : 0.f;
+  const float span = fminf(top - lowest, 48.f * (float)(1.0 / slow.c)), scale = span < INFINITY ? bin_scale(kBins, span) : 0.f;
   auto bin = [&](float v) { return fminf((top - v) * scale, (float)(kBins - 1)); };  // (its whole part)
   bool binned = usable;
   unsigned long long total;

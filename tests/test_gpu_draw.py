@@ -262,6 +262,33 @@ def test_top_logits_many_rows(lib):
 
 
 # ------------------------------------------------------------------------------------------------ both, of many rows
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [5, 1000, 9001, 33000, 66000])
+def test_rows_that_differ_by_next_to_nothing(lib, dtype, V):
+    """Logits less than 1e-36 apart, down to the smallest steps of their type: bins of equal width between them would be more than fp32 has numbers for a unit."""
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(V + 31)
+    step = 2.0 ** -149 if dt == torch.float32 else 2.0 ** -133
+    noise = torch.randn((3, V), generator=g, device="cuda")
+    few = torch.zeros((7, V), device="cuda")
+    few[0, V // 3] = 1e-37
+    few[1, V - 1] = -1e-37
+    few[2] = torch.randint(0, 5, (V,), generator=g, device="cuda") * step
+    few[3:6] = noise * torch.tensor([[1e-37], [5e-39], [1e-36]], device="cuda")
+    few[6, 0], few[6, V // 2] = 7e-37, 3e-37
+    for times in (1, 38):                                                 # (38: 266 rows, which other kernels take)
+        n = len(few)
+        x = few.to(dt).repeat(times, 1)
+        u = torch.rand(n, generator=g, device="cuda")
+        for rules in ({}, dict(top_k=3), dict(top_k=300), dict(top_k=1500), dict(top_p=0.5), dict(min_p=0.05), dict(temperature=1e-37, top_p=0.9), dict(temperature=1e-37, top_k=40, min_p=0.3)):
+            rules = {k: torch.full((n * times,), v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in rules.items()}
+            for got in _check(ctx, lib, x, u.repeat(times), rows=range(n), **rules):
+                assert (got.view(times, n) == got[:n]).all()
+        for k, tau in ((1, 1.0), (3, 1e-37), (64, 1.0), (200, 1e-37), (300, 1.0), (1024, 1.0)):
+            ids, values, _ = _check_top(ctx, x, k, tau, rows=range(n))
+            assert (ids.view(times, n, k) == ids[:n]).all() and (values.view(times, n, k) == values[:n]).all()
+
+
 @pytest.mark.parametrize("V", [4097, 9001, 16384, 16387, 32000, 32768, 40001, 50257, 65536])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_rows_side_by_side(lib, dtype, V):
