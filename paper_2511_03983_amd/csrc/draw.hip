@@ -45,7 +45,7 @@ __device__ __forceinline__ double power2(double x, int bits) {
 
 // What a workgroup shares while it searches a row
 template <int NT> struct Search {
-  union {
+  union alignas(16) {  // (read four counts at a time)
     unsigned long long amount[kBins];
     uint32_t count[kBins];
   } bins;
@@ -60,6 +60,8 @@ template <int NT> struct Search {
   float hi, lo;  // of list_of_many's list
   int n, marked;
 };
+
+static_assert(alignof(Search<256>) % sizeof(u32x4v) == 0 && offsetof(Search<256>, bins) % sizeof(u32x4v) == 0, "bins are read as vectors");
 
 // A value that all lanes have, known to be one: what depends on it is a branch of all
 __device__ __forceinline__ int uniform_of(int v) { return __builtin_amdgcn_readfirstlane(v); }
