@@ -1,5 +1,7 @@
 // What is taken from a row of logits: a token drawn from it, or its k largest.  A row's columns have one order, larger logits first and equal ones by column; everything here is a
 // beginning of it.
+#include <cstddef>
+
 #include "bins.h"
 #include "nn.h"
 #include "row.h"
@@ -430,7 +432,7 @@ struct Weigher {
   }
   // The smallest logit whose probability is `least` of the largest: near where the logarithm says, a lane a value, otherwise by halving.
   __device__ float smallest(double least, int lane) const {
-    if (least >= 1.0) return top;
+    if (least >= 1.0) return c > 0.0 || top == INFINITY ? top : -3.402823466e38f;  // (at an infinite temperature all are as probable)
     auto key = [](float v) { const uint32_t b = __float_as_uint(v); return b ^ (b >> 31 ? 0xffffffffu : 0x80000000u); };
     auto value = [](uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); };
     auto enough = [&](uint32_t k) { return power2(exponent(value(k)), 0) >= least; };

@@ -156,6 +156,22 @@ def test_draw_strides_and_places(lib, dtype):
         assert all((o[[0, -1]] == -7).all() and (o[1:-1] == r).all() for o, r in zip(out, got))
 
 
+@pytest.mark.parametrize("dtype", list(DTYPES))
+@pytest.mark.parametrize("V", [5, 1000, 9001, 66000])
+def test_draw_at_an_infinite_temperature(lib, dtype, V):
+    """All columns but those at -infinity are as probable as the most probable one, also for a min_p of 1."""
+    dt, model = DTYPES[dtype]
+    ctx, g = _ctx(lib, V, model), _gen(V + 41)
+    x = torch.cat([_logits(g, 1, V, kind) for kind in ("model", "flat", "masked", "wide", "model")])
+    x[4, V - 1] = math.inf
+    x = x.to(dt)
+    T = len(x)
+    hot = torch.full((T,), math.inf, device="cuda")
+    for rules in ({}, dict(top_k=3), dict(top_k=1200), dict(top_p=0.5), dict(min_p=0.5), dict(min_p=1.0), dict(min_p=2.0), dict(top_k=40, min_p=1.0), dict(top_p=0.7, min_p=1.0)):
+        rules = {k: torch.full((T,), v, dtype=torch.int32 if k == "top_k" else torch.float32, device="cuda") for k, v in rules.items()}
+        _check(ctx, lib, x, torch.rand(T, generator=g, device="cuda"), temperature=hot, **rules)
+
+
 def test_draw_many_rows(lib):
     V, T = 300, 5000
     ctx, g = _ctx(lib, V), _gen(9)
