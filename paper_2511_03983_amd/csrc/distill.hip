@@ -1,4 +1,5 @@
 // The loss of a student's logits against a teacher's top logits and the targets, with its gradient.
+#include <cfloat>
 #include <type_traits>
 
 #include "nn.h"
@@ -77,7 +78,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   if (tid == 0) twice = 0;
   auto bit = [&](int c) { return c - head + N; };  // of a column, in the table
   __syncthreads();
-  float top_t = rest, top_set = -INFINITY;  // largest of the teacher's, and of the student's in the set
+  float top_value = -INFINITY, top_set = -INFINITY;  // largest of the teacher's values, and of the student's in the set
   for (int j = tid; j < k; j += NT) {
     const int c = j == tid ? id0 : te.ids[list + j];
     const bool on = (unsigned)c < (unsigned)V;
@@ -87,17 +88,19 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     if (atomicOr(&in_set[bit(c) / 32], 1u << (bit(c) & 31)) >> (bit(c) & 31) & 1) twice = 1;
     logit[j] = s;
     top_set = fmaxf(top_set, s);
-    part[j] = (j == tid ? value0 : te.values[list + j]) * inv_tau;
-    top_t = fmaxf(top_t, (float)part[j]);
+    const float value = j == tid ? value0 : te.values[list + j];
+    part[j] = value * inv_tau;
+    top_value = fmaxf(top_value, value);
   }
   if (64 * wave < k) {
-    top_t = wave_max(top_t);
+    top_value = wave_max(top_value);
     top_set = wave_max(top_set);
   }
-  if (lane == 0) { most[0][wave] = top_t; most[1][wave] = top_set; }
+  if (lane == 0) { most[0][wave] = top_value; most[1][wave] = top_set; }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < NW; ++w) { top_t = fmaxf(top_t, most[0][w]); top_set = fmaxf(top_set, most[1][w]); }
+  for (int w = 0; w < NW; ++w) { top_value = fmaxf(top_value, most[0][w]); top_set = fmaxf(top_set, most[1][w]); }
+  const double top_t = fmax(top_value * inv_tau, (double)rest);  // (a finite value over the temperature may be beyond fp32)
   const bool taught = te.weight > 0.f && top_t > -INFINITY;
   if (!taught && !aimed) {
     const float zeros[N] = {};
@@ -151,7 +154,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
       part[j] -= top_t;
       weight[j] = taught ? exp(part[j]) : 0.0;
     }
-  const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - (double)top_t) : 0.0;
+  const double rest_weight = taught && rest > -INFINITY ? exp((double)rest - top_t) : 0.0;
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) other = fmaxf(other, most[2][w]);
@@ -185,7 +188,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   const float ref = other > -INFINITY ? other : 0.f, m = fmaxf(top_set, other);
   // Sums over the others against their largest, and over the set against the row's.  Exponentials of (v - ref) / tau, and of v - ref: the same or only one of them asked for (mode 0), squares
   // (temperature 2: 1; 4: 2), or an exponential each (3).  8192 x 50257 bf16 at temperature 2, both asked for: 372 us, with an exponential each and the choice made for every element 487; one of them alone 338
-  const float c1 = kLog2e, ct = (float)(kLog2e * inv_tau), c = taught ? ct : c1;
+  const float c1 = kLog2e, ct = fminf((float)(kLog2e * inv_tau), FLT_MAX), c = taught ? ct : c1;
   const int mode = !(taught && aimed) || te.temperature == 1.f ? 0 : te.temperature == 2.f ? 1 : te.temperature == 4.f ? 2 : 3;
   auto exps = [&](auto how, float v, auto f) {  // f(first, second)
     const float d = v - ref, a = __builtin_amdgcn_exp2f(d * c);

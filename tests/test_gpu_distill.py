@@ -186,6 +186,41 @@ def test_distill_far_apart(lib, dtype):
 
 
 @pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("V", [1003, 70003])
+def test_distill_values_and_temperatures_near_their_ends(lib, dtype, V):
+    """Logits of the type's lowest value on either side, and values that fp32 does not hold once they are divided by the temperature: a teacher all the same.  An exponential below 2^-126, the least
+    that the instruction forms, counts as nothing: with a temperature of at most 1 that is 2^-126 of a row's gradient."""
+    ctx, g = _ctx(lib, V, dtype), _gen(V + 19)
+    T, k = 6, 20
+    low = torch.finfo(DT[dtype]).min
+    x = _logits(g, T, V).to(DT[dtype])
+    ids, values, rest = _teacher(g, x, k, 1.0)
+    y = _targets(g, ids, V)
+    masked = torch.where(torch.rand((T, V), generator=g, device="cuda") < 0.5, low, x.float()).to(x.dtype).scatter_(1, ids.long(), x.gather(1, ids.long()))
+    masked.scatter_(1, y.long()[:, None], x.gather(1, y.long()[:, None]))
+    some = torch.where(torch.rand((T, k), generator=g, device="cuda") < 0.5, low, values)
+    some[::2] = low                                                    # (rows of nothing else: all as probable)
+    high = 1e38 * (1.0 + torch.randint(0, 3, (T, k), generator=g, device="cuda") * 1e-3)
+    half, tiny = (U, 2.0 ** -149) if dtype == "f32" else (2.0 ** -8, 2.0 ** -133)
+    for xx, v, s, tau, weight in [(*c, w) for w in (1.0, 0.5) for c in (
+            (x, some, None, 0.5), (x, some, None, 0.01), (x, some, rest, 0.5), (masked, values, rest, 1.0), (masked, some, None, 0.5), (x, high, None, 0.1), (x, -high, None, 0.1),
+            (x, high, torch.full_like(rest, 3e38), 0.1), (x, values, None, 1e-30), (masked, some, None, 1e-30))] + [(x, values, None, 1e-40, 0.5)]:
+        loss, rowloss, grad = ctx.twist_distill_raw(xx, y, lib.Teacher(ids, v, rest=s, temperature=tau, weight=weight))
+        tau = float(np.float32(tau))
+        for t in range(T):
+            # the same teacher with its largest value taken off the others, in 64 bits: of numbers of 1e38 and more their log-sum-exp would leave nothing of the logarithms
+            theirs = v[t].double().cpu().numpy()
+            m = theirs.max()
+            want, off, e, err = _want(xx[t].double().cpu().numpy(), int(y[t]), ids[t].cpu().numpy(), theirs - m, None if s is None else float(s[t]) - m / tau, tau, weight)
+            got = grad[t].double().cpu().numpy() * T
+            assert abs(float(rowloss[t]) - want) <= off + 2.0 ** -149, (t, tau, weight, float(rowloss[t]), want, off)
+            over = np.abs(got - e) - (half * np.abs(e) + (1 + half) * (err + 2 * U * np.abs(e)) + T * tiny + 2.0 ** -126)
+            c = int(np.argmax(np.where(np.isnan(over), np.inf, over)))
+            assert over[c] <= 0, (t, tau, weight, c, got[c], e[c], err[c])
+        assert torch.isfinite(loss)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
 def test_distill_places(lib, dtype):
     """Rows of any stride from any element on, the gradient in other memory or in the logits' place; nothing else is written."""
     for V, pad, first, gpad in ((1003, 0, 1, 0), (1003, 5, 0, 0), (4100, 4, 3, 12), (50257, 7, 0, 0), (50257, 0, 0, 7), (70003, 1, 5, 1)):
