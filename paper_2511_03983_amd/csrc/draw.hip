@@ -755,6 +755,12 @@ template <int NT> __device__ __forceinline__ float block(Search<NT> &sh, int lan
   for (int w = 1; w < NT / 64; ++w) v = sum ? v + all[w] : fmaxf(v, all[w]);
   return uniform_of(v);
 }
+// log2(e) over the temperature in 32 bits, with which differences of logits and their exponents are numbers of fp32, or else so large that their exponential is 0: not (no number) at temperatures
+// next to nothing or to fp32's largest number.
+__device__ __forceinline__ float exponent_of_2(double inv_temp) {
+  const float c = (float)(1.4426950408889634 * inv_temp);
+  return c > 1e-30f && c < 1e30f ? c : NAN;
+}
 // The log-sum-exp over the temperature of a row's columns behind the place `last`, -infinity where there are none.
 template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind(device_bytes at_row, int V, int head, int wave, uint64_t last, double inv_temp) {
   Search<NT> &sh = shared<NT>();
@@ -768,8 +774,9 @@ template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind
   others([&](float v) { m = fmaxf(m, v); });
   m = block(sh, f.lane, wave, m, false);
   if (!(m > -INFINITY)) return m;
-  const float c = (float)(1.4426950408889634 * inv_temp);
-  others([&](float v) { s += v == m ? 1.f : __builtin_amdgcn_exp2f((v - m) * c); });
+  const float c = exponent_of_2(inv_temp);
+  if (c == c) others([&](float v) { s += v == m ? 1.f : __builtin_amdgcn_exp2f((v - m) * c); });
+  else others([&](float v) { s += __builtin_amdgcn_exp2f((float)(((double)v - (double)m) * (1.4426950408889634 * inv_temp))); });
   s = block(sh, f.lane, wave, s, true);
   return (float)((double)m * inv_temp + log((double)s));
 }
@@ -783,7 +790,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   const int t = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = min(k, V);
   const device_bytes at_row = (device_bytes)(x + t * ld * Piece<BF>::ES);
   const int head = R::aligned((const char *)at_row, V);
-  const float c = (float)(1.4426950408889634 * inv_temp);
+  const float c = exponent_of_2(inv_temp);
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
   float s = 0.f, from, largest;
   int found = 0;
@@ -823,7 +830,7 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   for (int i = n + tid; i < found; i += NT) s += __builtin_amdgcn_exp2f((value_of(sh.sorted[i]) - ref) * c);
   s = block(sh, lane, wave, s, true);
   float r = (float)((double)ref * inv_temp + log((double)s));
-  if (!quick || !(s > 0.02f)) r = rest_behind<BF, NT>(at_row, V, head, wave, uniform_of(sh.sorted[n - 1]), inv_temp);  // (the others are far below the bound, or there is none)
+  if (!quick || !(s > 0.02f)) r = rest_behind<BF, NT>(at_row, V, head, wave, uniform_of(sh.sorted[n - 1]), inv_temp);  // (the others are far below the bound, there is none, or c is no number)
   if (tid == 0) rest[t] = r;
 }
 

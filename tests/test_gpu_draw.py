@@ -277,6 +277,29 @@ def test_top_logits_many_rows(lib):
     _check_top(ctx, _logits(g, T, V).bfloat16(), 12, rows=range(0, T, 61))
 
 
+@pytest.mark.parametrize("V", [1000, 9001, 70001])
+def test_rest_at_temperatures_near_their_ends(lib, V):
+    """Differences of logits that fp32 does not hold, at temperatures that make them small; and the smallest ones, at temperatures as small."""
+    ctx, g = _ctx(lib, V), _gen(V + 51)
+    far = torch.where(torch.rand((2, V), generator=g, device="cuda") < 0.5, -1.0, 1.0) * (3e38 + 3e37 * torch.rand((2, V), generator=g, device="cuda"))
+    near = torch.randint(0, 5, (2, V), generator=g, device="cuda") * 2.0 ** -149
+    for k in (1, 64, 300):
+        for x, taus in ((far, (3e38, 1e38, 1e32, 1.0, 1e-3)), (near, (2.0 ** -149, 1e-44, 1e-40, 1e-30, 1.0)), (_logits(g, 2, V), (1e-28, 1e-20, 1e20, 1e31, 3e38))):
+            for tau in taus:
+                t = float(np.float32(tau))
+                xs = x.double().cpu().numpy()
+                ids, values, rest = ctx.twist_top_logits_raw(x, k, temperature=tau)
+                for row in range(2):
+                    at, z = _order(xs[row])
+                    assert (ids[row].cpu().numpy() == at[:k]).all() and (values[row].double().cpu().numpy() == z[:k]).all()
+                    want = z[k] / t + math.log(np.exp((z[k:] - z[k]) / t).sum())
+                    if abs(want) > 3.4e38:
+                        assert float(rest[row]) == math.copysign(math.inf, want)
+                        continue
+                    off = U * (2 * math.log(V) + 4 + V / 256 + 16 + 2 * abs(z[k] / t) + 2 * abs(want - z[k] / t) + abs(want))      # (as for other temperatures)
+                    assert abs(float(rest[row]) - want) <= off, (k, tau, row, float(rest[row]), want, off)
+
+
 # ------------------------------------------------------------------------------------------------ both, of many rows
 @pytest.mark.parametrize("dtype", list(DTYPES))
 @pytest.mark.parametrize("V", [5, 1000, 9001, 33000, 66000])
