@@ -332,13 +332,22 @@ class Context:
         """(B, N) of a batch of token ids on the context's GPU."""
         if t.dtype is not torch.int32 or t.dim() != 2 or not t.is_contiguous() or t.get_device() != self.gpu:
             _refuse(f"{what}: needs contiguous int32 [B, N] on {self.device}")
+        if t.numel() >> 31:
+            _refuse(f"{what}: {t.numel()} tokens are too many for one call")
         return t.shape
+
+    @staticmethod
+    def _entries(k):
+        """Refuses lists of k entries before there is memory for them (the library: because of them)."""
+        if not 1 <= k <= 1024:
+            _refuse(f"lists of {k} entries (1 to 1024)")
 
     def twist_subnet_top_logits(self, sub: "Subnet", inputs: torch.Tensor, k: int, workspace: torch.Tensor, temperature: float = 1.0):
         """(ids int32 [B*N, k], values fp32 [B*N, k], rest fp32 [B*N]) of the positions of inputs [B, N]: what a Teacher is made of.  See include/twist.h."""
         B, N = self._batch(inputs, "inputs")
-        ids, values, rest = self._empty(torch.int32, B * N, max(k, 1)), self._empty(torch.float32, B * N, max(k, 1)), self._empty(torch.float32, B * N)
-        self._call(lib.twist_subnet_top_logits, sub.h, inputs.data_ptr(), B, N, k, temperature, ids.data_ptr(), values.data_ptr(), max(k, 1), rest.data_ptr(),
+        self._entries(k)
+        ids, values, rest = self._empty(torch.int32, B * N, k), self._empty(torch.float32, B * N, k), self._empty(torch.float32, B * N)
+        self._call(lib.twist_subnet_top_logits, sub.h, inputs.data_ptr(), B, N, k, temperature, ids.data_ptr(), values.data_ptr(), k, rest.data_ptr(),
                    *_storage(workspace, "workspace", self.gpu))
         return ids, values, rest
 
@@ -521,6 +530,8 @@ class Context:
         stride = t.stride()
         if t.dtype is not dtype or t.shape != (T, cols) or (stride[1] != 1 and cols > 1) or t.get_device() != self.gpu:
             _refuse(f"{what}: needs [{T}, {cols}] of {dtype} with contiguous rows on {self.device}")
+        if T >> 31:         # (the library counts rows in 32 bits)
+            _refuse(f"{what}: {T} rows are too many for one call")
         return stride[0] if T > 1 or stride[0] > cols else cols
 
     def twist_cache_append_raw(self, cache: "PagedCache", qkv: torch.Tensor, lens: torch.Tensor, seq: torch.Tensor | None = None,
@@ -613,12 +624,13 @@ class Context:
         """(ids int32 [T, k], values fp32 [T, k], rest fp32 [T]): the k largest of logits [T, vocab] (fp32 or the model's type) in order, and the log-sum-exp of the
         others over the temperature.  Tensors that are given receive the results (ids and values: one row stride).  See include/twist.h."""
         T, ld, f32 = self._logits(logits)
+        self._entries(k)
         if rest is None:
             rest = self._empty(torch.float32, T)
         else:
             _ints(rest, T, "rest", self.gpu, torch.float32)
         if ids is None and values is None:
-            ids, values, ldk = self._empty(torch.int32, T, max(k, 1)), self._empty(torch.float32, T, max(k, 1)), k
+            ids, values, ldk = self._empty(torch.int32, T, k), self._empty(torch.float32, T, k), k
         else:
             ids = self._empty(torch.int32, T, k) if ids is None else ids
             values = self._empty(torch.float32, T, k) if values is None else values
@@ -841,7 +853,7 @@ class Teacher:
 
     def __init__(self, ids: torch.Tensor, values: torch.Tensor, rest: torch.Tensor | None = None, temperature: float = 1.0, weight: float = 1.0):
         if not (ids.is_cuda and ids.dim() == 2 and ids.dtype == torch.int32 and values.dtype == torch.float32 and ids.shape == values.shape
-                and ids.device == values.device and (ids.shape[1] < 2 or ids.stride(1) == values.stride(1) == 1)):
+                and ids.device == values.device and ids.shape[1] < 2 ** 31 and (ids.shape[1] < 2 or ids.stride(1) == values.stride(1) == 1)):
             _refuse("ids and values: need CUDA int32 and fp32 [T, k] with contiguous rows")
         self.T, k = ids.shape
         ld = [t.stride(0) if self.T > 1 else max(t.stride(0), k) for t in (ids, values)]

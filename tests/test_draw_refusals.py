@@ -79,3 +79,41 @@ def test_holders_refuse_what_is_not_on_a_gpu_or_not_of_its_type(tw):
     with pytest.raises(tw.TwistError):
         tw.Teacher(i.view(1, 3), z.view(1, 3))
     assert tw.DrawRules().T is None
+
+
+class _NoGPU:
+    """What the binding looks at of a context, with no memory to be had."""
+
+    def __new__(cls, tw, vocab=8):
+        class Bare(tw.Context):
+            def __init__(self):
+                self.gpu, self.device, self.torch_dtype, self.desc = -1, "cpu", torch.bfloat16, tw.ModelDesc(vocab=vocab)
+
+            def _empty(self, *a, **kw):
+                raise AssertionError("asks for memory")
+
+            def _call(self, *a):
+                raise AssertionError("calls the library")
+        return Bare()
+
+
+@pytest.mark.parametrize("T", [2 ** 31, 2 ** 32 + 3])
+def test_rows_that_the_library_counts_otherwise_are_refused(tw, T):
+    """Its numbers of rows have 32 bits: of 2^32 + 3 rows it would see 3."""
+    ctx = _NoGPU(tw)
+    x = torch.empty((T, 8), dtype=torch.bfloat16, device="meta")       # (no memory)
+    for call in (lambda: ctx._rows(x, T, 8, "logits", torch.bfloat16), lambda: ctx._logits(x), lambda: ctx._batch(torch.empty((T, 8), dtype=torch.int32, device="meta"), "inputs"),
+                 lambda: ctx._batch(torch.empty((8, T), dtype=torch.int32, device="meta"), "inputs")):
+        with pytest.raises(tw.TwistError, match="logits|inputs"):
+            call()
+    assert ctx._rows(x[:5], 5, 8, "logits", torch.bfloat16) == 8
+
+
+@pytest.mark.parametrize("k", [-2 ** 32 + 5, -1, 0, 1025, 2 ** 31, 2 ** 32 + 5])
+def test_lists_of_a_length_that_there_is_not_ask_for_no_memory(tw, k):
+    ctx = _NoGPU(tw)
+    x, i = torch.empty((4, 8), dtype=torch.bfloat16, device="meta"), torch.empty((4, 8), dtype=torch.int32, device="meta")
+    given = torch.empty((4, 5), dtype=torch.int32, device="meta")
+    for call in (lambda: ctx.twist_top_logits_raw(x, k), lambda: ctx.twist_top_logits_raw(x, k, ids=given), lambda: ctx.twist_subnet_top_logits(None, i, k, None)):
+        with pytest.raises(tw.TwistError, match="entries"):
+            call()
