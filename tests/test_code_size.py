@@ -61,3 +61,34 @@ def test_called_device_functions_are_within_the_reach_of_a_branch():
     assert kernels > 100                                        # the bundles were read
     assert any("draw_of_many" in name for _, name in called)       # and what is called is among them
     assert {n: s for n, s in called.items() if s > REACH * 3 // 4} == {}
+
+
+def _symbols(elf):
+    """(name, type, size) of an ELF file's symbols."""
+    (shoff,) = struct.unpack_from("<Q", elf, 0x28)
+    entry, count = struct.unpack_from("<HH", elf, 0x3A)
+    sections = [struct.unpack_from("<IIQQQQIIQQ", elf, shoff + i * entry) for i in range(count)]
+    for s in sections:
+        if s[1] in (2, 11):
+            for at in range(s[4], s[4] + s[5], 24):
+                name, info, _, _, _, size = struct.unpack_from("<IBBHQQ", elf, at)
+                start = sections[s[6]][4] + name
+                yield elf[start: elf.index(b"\0", start)].decode(), info & 15, size
+
+
+def test_functions_are_told_from_kernels_by_the_descriptors_that_launches_read():
+    """Every kernel has one, an object of 64 bytes by its name; whatever has none is called, whatever its name."""
+    if not os.path.exists(LIB):
+        pytest.skip("the library is not built")
+    with open(LIB, "rb") as f:
+        data = f.read()
+    kernels, called = 0, {}
+    for i, elf in enumerate(_device_objects(data)):
+        symbols = list(_symbols(elf))
+        launched = {name[:-3] for name, kind, size in symbols if kind == 1 and name.endswith(".kd") and size == 64}      # STT_OBJECT
+        functions = {name: size for name, kind, size in symbols if kind == 2}                                          # STT_FUNC
+        assert launched <= set(functions)
+        kernels += len(launched)
+        called.update({(i, name): size for name, size in functions.items() if name not in launched})
+    assert kernels > 100 and all(any(f in name for _, name in called) for f in ("draw_of_many", "list_of_many", "rest_behind"))
+    assert {n: s for n, s in called.items() if s > REACH * 3 // 4} == {}
