@@ -65,7 +65,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   const int tgt = te.weight < 1.f ? targets[t] : -1;
   const bool aimed = (unsigned)tgt < (unsigned)V;
   const float rest = te.rest ? te.rest[t] : -INFINITY;
-  P16 x[NV ? NV : 1];
+  P16 x[NV ? NV : 1];  // (as a Row's, but that the list's columns are taken out of it, also of pieces that are read again)
 #pragma unroll
   for (int u = 0; u < NV; ++u) {
     x[u].u = P16::none();

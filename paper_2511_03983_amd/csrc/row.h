@@ -118,8 +118,8 @@ template <int BF, int NT, int NV> struct Row {
     xl = tid < ends ? load1<BF>(row, end) : -INFINITY;
   }
   __device__ __forceinline__ static int aligned(const void *row, int V) { return min(V, (int)(-(reinterpret_cast<uintptr_t>(row) / ES) & (N - 1))); }
-  // f(piece, its number) for all of the thread's pieces; read again, a piece goes through `fresh` first
-  template <class F, class G> __device__ __forceinline__ void each(F f, G fresh) {
+  // f(piece, its number) for all of the thread's pieces
+  template <class F> __device__ __forceinline__ void each(F f) {
     if (NV) {
       int at = tid;
       asm volatile("" : "+v"(at));  // (neither places nor what one pass makes of the pieces are kept for the next: registers)
@@ -133,12 +133,10 @@ template <int BF, int NT, int NV> struct Row {
       for (int v = tid; v < pieces; v += NT) {
         P16 y;
         y.load(first + (int64_t)v * 16);
-        fresh(y, v);
         f(y, v);
       }
     }
   }
-  template <class F> __device__ __forceinline__ void each(F f) { each(f, [](P16 &, int) {}); }
 };
 
 }  // namespace
