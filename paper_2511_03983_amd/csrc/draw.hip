@@ -776,7 +776,7 @@ template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind
   if (!(m > -INFINITY)) return m;
   const float c = exponent_of_2(inv_temp);
   if (c == c) others([&](float v) { s += v == m ? 1.f : __builtin_amdgcn_exp2f((v - m) * c); });
-  else others([&](float v) { s += __builtin_amdgcn_exp2f((float)(((double)v - (double)m) * (1.4426950408889634 * inv_temp))); });
+  else others([&](float v) { s += v == m ? 1.f : __builtin_amdgcn_exp2f((float)(((double)v - (double)m) * (1.4426950408889634 * inv_temp))); });
   s = block(sh, f.lane, wave, s, true);
   return (float)((double)m * inv_temp + log((double)s));
 }

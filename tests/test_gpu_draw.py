@@ -300,6 +300,19 @@ def test_rest_at_temperatures_near_their_ends(lib, V):
                     assert abs(float(rest[row]) - want) <= off, (k, tau, row, float(rest[row]), want, off)
 
 
+@pytest.mark.parametrize("V", [1000, 9001, 70001])
+def test_rest_of_infinite_logits(lib, V):
+    """More columns at +infinity than the list has: so are the others together, at any temperature."""
+    ctx, g = _ctx(lib, V), _gen(V + 61)
+    x = torch.where(torch.rand((2, V), generator=g, device="cuda") < 0.5, math.inf, _logits(g, 2, V))
+    for k in (1, 64, 300):
+        for tau in (2.0 ** -149, 1e-20, 1.0, 3e38):
+            ids, values, rest = ctx.twist_top_logits_raw(x, k, temperature=tau)
+            for row in range(2):
+                assert (ids[row].cpu().numpy() == _order(x[row].double().cpu().numpy())[0][:k]).all()
+            assert (values == math.inf).all() and (rest == math.inf).all(), (k, tau)
+
+
 # ------------------------------------------------------------------------------------------------ both, of many rows
 @pytest.mark.parametrize("dtype", list(DTYPES))
 @pytest.mark.parametrize("V", [5, 1000, 9001, 33000, 66000])
