@@ -451,7 +451,8 @@ typedef struct {
  * the token is the first at which the probabilities of the kept columns, summed in this order, exceed uniform[t] times their sum.  tokens [T] (dev) receives its column, logprobs [T]
  * (fp32, may be NULL) the logarithm of its probability among the kept columns, kept [T] (int32, may be NULL) their number.  Columns at -infinity, and those that hold no
  * number, are never kept; a row without any other gives token -1, -infinity and 0.  Of a row with +infinity only such columns have a probability.  Probabilities and their sums are whole
- * multiples of 2^-42 of the largest (2^-46 up to 2^16 columns), so that no order of summation changes a token.
+ * multiples of 2^-42 of the largest (2^-46 up to 2^16 columns), so that no order of summation changes a token.  Rows with a top_k of 1 to 1024 are weighed by a formula that
+ * is 2^-51 off, others by one that is 2^-48 off: where a sum meets its border to that, a row may give another token with a top_k of 1024 than with one of 1025.
  *
  * twist_top_logits_raw: the k largest (1 <= k <= 1024) of each of T rows of logits in the same order: ids [T, k] (int32) and values [T, k] (fp32; rows of both ldk apart), and rest
  * [T] (fp32, may be NULL), the log-sum-exp of the row's other logits divided by the temperature (> 0): -infinity where there are none.  Columns that hold no number count as
@@ -463,7 +464,7 @@ TWIST_API twist_status twist_top_logits_raw(twist_ctx *ctx, const void *logits, 
                                             float *values, int64_t ldk, float *rest);
 
 /* What a teacher says about T tokens: k of its logits each (1 <= k <= 1024; ids outside the vocabulary are entries that are not there, of one that is named twice the
- * probabilities add up), and optionally the log-sum-exp of its other logits divided by the temperature: what twist_top_logits_raw gives. */
+ * probabilities add up), and optionally the log-sum-exp of its other logits divided by the temperature: what twist_top_logits_raw gives.  Values and rest are finite or -infinity. */
 typedef struct {
   const int32_t *ids;   /* dev [T] rows of k, ld apart */
   const float *values;  /* dev, likewise */
@@ -482,12 +483,14 @@ TWIST_API twist_status twist_subnet_top_logits(twist_ctx *ctx, twist_subnet *sub
 TWIST_API twist_status twist_subnet_fwd_bwd_distill(twist_ctx *ctx, twist_subnet *sub, const void *inputs, const void *targets, const twist_teacher *teacher, int32_t B, int32_t N,
                                                     void *workspace, size_t workspace_bytes, float *loss_dev);
 
-/* The loss of T rows of a student's logits [T, vocab] (dtype, rows ld apart) and its gradient.  With the teacher's probabilities q of its entries, and of all its other tokens together (rest), and
- * the student's p of the same, both at the temperature, row t counts
+/* The loss of T rows of a student's logits [T, vocab] (dtype, rows ld apart) and its gradient.  With the teacher's probabilities q of its entries, and of all its other tokens
+ * together (rest), and the student's p of the same, both at the temperature, row t counts
  *     weight * temperature^2 * sum q (log q - log p)  +  (1 - weight) * cross-entropy(logits, targets[t])
- * A row without an entry or rest has no teacher, one with a target outside the vocabulary no target: that part of it is 0.  targets (dev [T]) may be NULL where weight is 1.  loss (fp32
- * scalar) receives the mean over all T rows, rowloss [T] (fp32) the rows', grad [T, vocab] (dtype, rows ldg apart; the logits themselves, ldg = ld, or memory apart from them) the mean's
- * gradient; columns beyond vocab are left as they were.  Errors as twist_top_logits_raw. */
+ * A row without an entry or rest has no teacher, one with a target outside the vocabulary no target: that part of it is 0.  targets (dev [T]) may be NULL where weight is 1.
+ * loss (fp32 scalar) receives the mean over all T rows, rowloss [T] (fp32) the rows', grad [T, vocab] (dtype, rows ldg apart; the logits themselves, ldg = ld, or memory apart
+ * from them) the mean's gradient; columns beyond vocab are left as they were.  Probabilities enter the gradient in 32 bits, so that it is off by the temperature times some
+ * 2^-22 of them, and the loss in 64, off by the temperature's square times 2^-43 of its terms: at temperatures of thousands that is what two nearly equal distributions differ
+ * by.  Errors as twist_top_logits_raw. */
 TWIST_API twist_status twist_distill_raw(twist_ctx *ctx, const void *logits, int64_t ld, const int32_t *targets, int32_t T, const twist_teacher *teacher, void *grad, int64_t ldg,
                                          float *rowloss, float *loss);
 

@@ -30,14 +30,15 @@ __device__ __forceinline__ float exp_f32(double x) {
   return __builtin_amdgcn_exp2f(h) * fmaf((float)(y - h), 0.69314718f, 1.f);
 }
 
-// A row a workgroup.  The row's tokens are the teacher's (the set) and the others, whose share of the distribution is formed from themselves and not as what the set leaves: it may be
-// next to nothing, or all but everything.  With tau the temperature, p and q over the set and over the others together (P, Q of them), the gradient of
-// KL(q || p) is (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.
-// Bound by memory: the row is read once and its gradient written once (64 entries, 8192 x 50257 bf16: 342 us, 4.8 TB/s, the rate of a copy; 1024 x 50257 fp32, one row a CU at a time: 112 us, 3.7).  It stays in registers as it came (NV pieces of 16 bytes a thread; rows that NT threads cannot hold, NV = 0, are read
-// three times), the set's columns as -infinity, so that they weigh nothing in the others' sums; their own gradients, a thread each and in 64 bits where they meet a logarithm, are stored over
-// the others' behind a barrier.
-// Pieces begin where the gradient's row is aligned, which is where the logits' is as a rule (rows of an odd vocabulary start anywhere; 8192 x 50257 bf16 from any element on 554 us, all rows
-// aligned 440); the columns before and behind them are a thread's each.
+// A row a workgroup.  The row's tokens are the teacher's (the set) and the others, whose share of the distribution is formed from themselves and not as what the set leaves: it
+// may be next to nothing, or all but everything.  With tau the temperature, p and q over the set and over the others together (P, Q of them), the gradient of KL(q || p) is
+// (p_i - q_i) / tau in the set and p_i (P - Q) / P / tau outside it.
+// Bound by memory: the row is read once and its gradient written once (64 entries, 8192 x 50257 bf16: 342 us, 4.8 TB/s, the rate of a copy; 1024 x 50257 fp32, one row a CU at a
+// time: 112 us, 3.7).  It stays in registers as it came (NV pieces of 16 bytes a thread; bf16 with 16 of them spills one register), the set's columns as -infinity, so that they
+// weigh nothing in the others' sums; their own gradients, a thread each and in 64 bits where they meet a logarithm, are stored over the others' behind a barrier.  Rows that NT
+// threads cannot hold, NV = 0, are read three times (1024 x 131072: bf16 212 us, 2.5 TB/s of what one pass would move, fp32 357, 3.0).
+// Pieces begin where the gradient's row is aligned, which is where the logits' is as a rule (rows of an odd vocabulary start anywhere; 8192 x 50257 bf16 from any element on
+// 554 us, all rows aligned 440); the columns before and behind them are a thread's each.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int64_t ld, const int32_t *targets, int V, twist_teacher te, char *grads, int64_t ldg, int64_t pad, float inv_T,
                                                         float *rowloss) {
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < NW; ++w) other = fmaxf(other, most[2][w]);
-  if (twice) {
+  if (twice) {  // (every entry is compared with every other: 2048 x 32000 bf16, 64 entries 63 -> 73 us, 256 70 -> 99, 1024 106 -> 547)
     constexpr int M = (kTop + NT - 1) / NT;
     double sum[M];
     bool first_of[M];
@@ -186,8 +187,9 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
     }
   }
   const float ref = other > -INFINITY ? other : 0.f, m = fmaxf(top_set, other);
-  // Sums over the others against their largest, and over the set against the row's.  Exponentials of (v - ref) / tau, and of v - ref: the same or only one of them asked for (mode 0), squares
-  // (temperature 2: 1; 4: 2), or an exponential each (3).  8192 x 50257 bf16 at temperature 2, both asked for: 372 us, with an exponential each and the choice made for every element 487; one of them alone 338
+  // Sums over the others against their largest, and over the set against the row's.  Exponentials of (v - ref) / tau, and of v - ref: the same or only one of them asked for
+  // (mode 0), squares (temperature 2: 1; 4: 2), or an exponential each (3).  8192 x 50257 bf16, both asked for: at temperature 2 341 us, at 1.5 or 3 383 (with the choice made
+  // for every element 487); the teacher's alone, at 1.5, 318
   const float c1 = kLog2e, ct = fminf((float)(kLog2e * inv_tau), FLT_MAX), c = taught ? ct : c1;
   const int mode = !(taught && aimed) || te.temperature == 1.f ? 0 : te.temperature == 2.f ? 1 : te.temperature == 4.f ? 2 : 3;
   auto exps = [&](auto how, float v, auto f) {  // f(first, second)
@@ -260,7 +262,8 @@ __global__ __launch_bounds__(NT, 4) void distill_kernel(const char *logits, int6
   });
   for (int64_t c = V + tid; c < pad; c += NT) store1<BF>(out, c, 0.f);
   if (wave == NW - 1) {
-    // the row's loss, in 64 bits: the share of one of two amounts is formed from their quotient, so that it is as exact near 1 as far from it.  A lane each for what would be one call behind the other.
+    // the row's loss, in 64 bits: the share of one of two amounts is formed from their quotient, so that it is as exact near 1 as far from it.  A lane each for what would be one
+    // call behind the other.
     auto of = [](double v, int from) { return __shfl(v, from, 64); };
     const double e = exp(lane == 0 ? down * inv_tau : down), rm = others * of(e, 0), r1 = others1 * of(e, 1) + set1, whole = rm + set, qall = qs + rest_weight;
     const double a = lane == 0 ? rm : rest_weight, b = lane == 0 ? set : qs, ratio = b < a ? b / a : a / b;  // (lanes 0 and 1)
@@ -309,8 +312,8 @@ twist_status twist_distill(twist_ctx *ctx, const char *who, int bf16, const void
   const char *x = static_cast<const char *>(logits);
   char *g = static_cast<char *>(grad);
 #define DISTILL(BF, NT, NV) hipLaunchKernelGGL((distill_kernel<BF, NT, NV>), dim3(T), dim3(NT), 0, ctx->stream, x, ld, targets, V, *te, g, ldg, pad, inv_T, rowloss)
-  // The fewest threads whose registers hold a row, so that a CU has several rows (64 entries, bf16: 256 x 32000 19.8 us with 256 threads and 18.3 with 1024, but 1024 x 32000 39 and 57, 4096 x 32000
-  // 121 and 212; 4096 x 50257 192 with 512, 290 with 1024; fp32 4096 x 16384 122 with 256, 177 with 1024, 4096 x 32000 207 with 512, 277 with 1024)
+  // The fewest threads whose registers hold a row, so that a CU has several rows (64 entries, bf16: 256 x 32000 19.8 us with 256 threads and 18.3 with 1024, but 1024 x 32000 39
+  // and 57, 4096 x 32000 121 and 212; 4096 x 50257 192 with 512, 290 with 1024; fp32 4096 x 16384 122 with 256, 177 with 1024, 4096 x 32000 207 with 512, 277 with 1024)
   if (bf16) {
     if (V <= 4 * 8 * 256) DISTILL(1, 256, 4);
     else if (V <= 16 * 8 * 256) DISTILL(1, 256, 16);

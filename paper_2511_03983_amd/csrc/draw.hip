@@ -90,8 +90,8 @@ template <int BF, int NT> struct Finder {
     pieces = (V - head) / N;
     first = row + head * P16::ES;
   }
-  // f(N logits, the first's column, how many of them are the row's) for all of the row, with D pieces on their way: the registers of one that is done take the one D behind it (not before it is
-  // done, and whether there is one or not: otherwise it is loaded somewhere else and waited for, to be moved)
+  // f(N logits, the first's column, how many of them are the row's) for all of the row, with D pieces on their way: the registers of one that is done take the one D behind it
+  // (not before it is done, and whether there is one or not: otherwise it is loaded somewhere else and waited for, to be moved)
   template <int D, class F> __device__ __forceinline__ void runs(F f) const {
     if (pieces > 0) {
       P16 next[D];
@@ -123,8 +123,8 @@ template <int BF, int NT> struct Finder {
   }
   // the number by which a run is marked
   __device__ __forceinline__ int piece_of(int c, int n) const { return n > 1 ? (c - head) / N : pieces + tid; }
-  // f(logit, column) of every column.  SHORT: in one copy of f for each piece on its way instead of one for each of its logits, for functions of many passes.  A branch reaches 128 KiB; in a function
-  // beyond that the compiler jumps through the registers of the return address, and the call does not return.
+  // f(logit, column) of every column.  SHORT: in one copy of f for each piece on its way instead of one for each of its logits, for functions of many passes.  A branch reaches
+  // 128 KiB; in a function beyond that the compiler jumps through the registers of the return address, and the call does not return.
   template <bool SHORT = false, class F> __device__ __forceinline__ void columns(F f) const {
     if (SHORT)
       runs<2>([&](const float *x, int c, int n) {
@@ -241,9 +241,9 @@ template <int BF, int NT> struct Finder {
     const int b = find(sh.bins.count, kBins, k, before);
     return b < kBins ? bin_edge(b, top, scale) : l;
   }
-  // The list of the row's columns that are `wanted(logit, column)`, in two steps: pieces (and, behind their numbers, the columns in none) that hold one are marked in a pass over the row, and
-  // looked through afterwards, a thread each.  A pass marks in few instructions; with what the list takes behind every column it is code that was not fetched before (2.4 and 6.4 us where both steps take
-  // 1.8 and 2.9).  begin(); mark() in a pass; then take(), the columns' number, which may be more than the list holds.
+  // The list of the row's columns that are `wanted(logit, column)`, in two steps: pieces (and, behind their numbers, the columns in none) that hold one are marked in a pass over
+  // the row, and looked through afterwards, a thread each.  A pass marks in few instructions; with what the list takes behind every column it is code that was not fetched before
+  // (2.4 and 6.4 us where both steps take 1.8 and 2.9).  begin(); mark() in a pass; then take(), the columns' number, which may be more than the list holds.
   __device__ __forceinline__ void begin() const {
     __syncthreads();
     if (tid == 0) sh.n = sh.marked = 0;
@@ -302,8 +302,9 @@ template <int BF, int NT> struct Finder {
     }
     __syncthreads();
   }
-  // The same of places from `hi` down to `lo` (not below it), all of them: counted in bins, put together by bin, and compared with those of their own bin alone.  Top 32, 64, 256 of
-  // 2048 x 32000 bf16: 42.8, 48.7 and 56.4 us, by comparing all with all 42.0, 51.0 and 72.9; top 512 of 2048 x 50257 104 and 166; 64 x 50257 fp32, top 64 and 1000, 11.7 and 19.4 against 12.0 and 55.8.
+  // The same of places from `hi` down to `lo` (not below it), all of them: counted in bins, put together by bin, and compared with those of their own bin alone.  Top 32, 64, 256
+  // of 2048 x 32000 bf16: 42.8, 48.7 and 56.4 us, by comparing all with all 42.0, 51.0 and 72.9; top 512 of 2048 x 50257 104 and 166; 64 x 50257 fp32, top 64 and 1000, 11.7 and
+  // 19.4 against 12.0 and 55.8.
   static __device__ __forceinline__ void sort_by_bins(Search<NT> &sh, int tid, int n, float hi, float scale) {
     uint32_t *bins = sh.bins.count;
     auto bin = [&](uint64_t p) { return min((int)((hi - value_of(p)) * scale), kFew - 1); };
@@ -353,7 +354,9 @@ template <int NT, class R> __device__ __forceinline__ void extremes(R &row, Sear
   top = uniform_of(top);
   low = uniform_of(low);
 }
-// A logit that k columns at least are not below, and not many more where logits differ, by counting in bins the threads' largest or the pieces'.  -infinity: none was found.
+// A logit that k columns at least are not below, and not many more where logits differ, by counting in bins the threads' largest or the pieces'.  -infinity: none was found, or k
+// is above the workgroup's threads (the pieces would give a bound then too, with another `low`): such rows are read three times more, top 512 of 2048 x 32000 bf16 139 us where
+// 256 take 58, drawing from the top 1000 of 4096 x 32000 499 where 50 take 72.
 template <int BF, int NT, class R> __device__ __forceinline__ float bound_of(R &row, const Finder<BF, NT> &f, int k, float mine, float top, float low) {
   const float span = top - low;
   if (k > NT || !(top > -INFINITY) || !(span < INFINITY)) return -INFINITY;
@@ -391,8 +394,8 @@ template <int BF, int NT, class R> __device__ __forceinline__ int collect(R &row
   return f.take([&](float v, int) { return v >= from; });
 }
 
-// The list of a row's k first places (k at most its columns; in any order, and more where that is as quick), by counting all of its columns in bins, or else bit by bit; their number.  Every
-// column of the list is before all others.  A function of its own, which leaves the registers of the quicker way alone.
+// The list of a row's k first places (k at most its columns; in any order, and more where that is as quick), by counting all of its columns in bins, or else bit by bit; their
+// number.  Every column of the list is before all others.  A function of its own, which leaves the registers of the quicker way alone.
 template <int BF, int NT> __device__ __attribute__((noinline)) int list_of_many(device_bytes at_row, int V, int head, int wave, int k) {
   Search<NT> &sh = shared<NT>();
   const Finder<BF, NT> f(sh, at_row, V, head, wave);
@@ -451,8 +454,8 @@ struct Weigher {
   }
 };
 
-// The same for whole rows, in half the instructions (an exponential of power2 takes 25, several of which run at a fraction of the rate): 2^(n / 512) from a table, the rest of the exponent by a
-// polynomial of degree 3 (2^-48 off).  Not for every row: `usable` tells.
+// The same for whole rows, in half the instructions (an exponential of power2 takes 25, several of which run at a fraction of the rate): 2^(n / 512) from a table, the rest of
+// the exponent by a polynomial of degree 3 (2^-48 off).  Not for every row: `usable` tells.
 struct QuickWeigher {
   double top, c;  // 512 log2(e) / temperature
   float least;    // below it nothing weighs anything
@@ -522,8 +525,8 @@ struct Settings {
   __device__ __forceinline__ unsigned long long draw_at(unsigned long long total) const { return u > 0.f ? min((unsigned long long)((double)fminf(u, 1.f) * (double)total), total - 1) + 1 : 1ull; }
 };
 
-// A token of a row of which many columns may be kept: the probabilities of the whole row are added up in bins of their size, and the columns of the bin in which a sum (top_p's, the random
-// number's) ends are put in order.  A function of its own, which leaves the registers of the way through a list alone.
+// A token of a row of which many columns may be kept: the probabilities of the whole row are added up in bins of their size, and the columns of the bin in which a sum (top_p's,
+// the random number's) ends are put in order.  A function of its own, which leaves the registers of the way through a list alone.
 template <int BF, int NT>
 __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int V, int head, int wave, int bits, const Settings set, int32_t *token, float *logprob_out, int32_t *kept) {
   Search<NT> &sh = shared<NT>();
@@ -544,15 +547,16 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
   const QuickWeigher quick(slow, sh.table);
   const bool usable = uniform_of((int)quick.usable);
   const float p = set.p, m = set.m, least = m > 0.f ? uniform_of(slow.smallest(m, lane)) : -INFINITY;
-  uint64_t last = 0;  // the last place that is kept
+  // the last place that is kept: of more than kTop columns bit by bit, in seven passes before the others (from the top 2000 of 64 x 32000 bf16: 68 us, of 64 x 50257 fp32 85)
+  uint64_t last = 0;
   if (k > 1 && k < V) {
     unsigned long long n = 0;
     f.template columns<true>([&](float v, int) { n += v > -INFINITY; });
     if ((unsigned long long)k < f.block_add(n)) last = f.reach(k, [](float v, uint64_t) -> unsigned long long { return v > -INFINITY; });
   }
   auto mass = [&](float v) { return usable ? quick(v) : slow(v); };
-  // min_p alone: its columns, where they are few, are all there is to weigh (64 x 32000 bf16, min_p 0.05: 32 us by bins, 13 so.  top_p's beginning is as a rule long: put in order as a whole instead of the
-  // columns of one bin of it, 64 x 32000 with top_p 0.9 take 88 us instead of 32)
+  // min_p alone: its columns, where they are few, are all there is to weigh (64 x 32000 bf16, min_p 0.05: 32 us by bins, 13 so.  top_p's beginning is as a rule long: put in
+  // order as a whole instead of the columns of one bin of it, 64 x 32000 with top_p 0.9 take 88 us instead of 32)
   if (m > 0.f && !(p < 1.f)) {
     f.begin();
     f.template runs<4>([&](const float *x, int c, int n) {
@@ -675,9 +679,9 @@ __device__ __attribute__((noinline)) void draw_of_many(device_bytes at_row, int 
   }
 }
 
-// A token of a row a workgroup.  Up to kTop candidates (top_k, or the largest alone) are listed and put in order, and one wave does the rest with them; other rows are weighed as a whole (above).  Few
-// bytes and many steps, each waiting for the one before: the top 50 of 1 x 50257 fp32 in 8.8 us, of 4096 x 32000 bf16 in 77 (3.4 TB/s), top_p of 256 x 50257 fp32 in 51, 11 of them 64-bit exponentials and
-// LDS additions.
+// A token of a row a workgroup.  Up to kTop candidates (top_k, or the largest alone) are listed and put in order, and one wave does the rest with them; other rows are weighed as
+// a whole (above).  Few bytes and many steps, each waiting for the one before: the top 50 of 1 x 50257 fp32 in 8.9 us, of 4096 x 32000 bf16 in 72 (3.7 TB/s), top_p of 256 x
+// 50257 fp32 in 50, 11 of them 64-bit exponentials and LDS additions.  With 16 pieces a thread 8 to 12 registers are spilled around the calls.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void draw_kernel(const char *x, int64_t ld, int V, int bits, const float *uniform, twist_draw_rules rules, int32_t *tokens, float *logprobs, int32_t *kept) {
   Search<NT> &sh = shared<NT>();
@@ -755,8 +759,8 @@ template <int NT> __device__ __forceinline__ float block(Search<NT> &sh, int lan
   for (int w = 1; w < NT / 64; ++w) v = sum ? v + all[w] : fmaxf(v, all[w]);
   return uniform_of(v);
 }
-// log2(e) over the temperature in 32 bits, with which differences of logits and their exponents are numbers of fp32, or else so large that their exponential is 0: not (no number) at temperatures
-// next to nothing or to fp32's largest number.
+// log2(e) over the temperature in 32 bits, with which differences of logits and their exponents are numbers of fp32, or else so large that their exponential is 0: not (no
+// number) at temperatures next to nothing or to fp32's largest number.
 __device__ __forceinline__ float exponent_of_2(double inv_temp) {
   const float c = (float)(1.4426950408889634 * inv_temp);
   return c > 1e-30f && c < 1e30f ? c : NAN;
@@ -781,8 +785,10 @@ template <int BF, int NT> __device__ __attribute__((noinline)) float rest_behind
   return (float)((double)m * inv_temp + log((double)s));
 }
 
-// The k largest of a row a workgroup: those above a bound that few columns reach, put in order; the pass that marks them also sums up the others, against the bound.  Bound by memory in the end,
-// by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 248 us (3.3 TB/s), the top 256 of 2048 x 32000 in 58.
+// The k largest of a row a workgroup: those above a bound that few columns reach, put in order; the pass that marks them also sums up the others, against the bound.  Bound by
+// memory in the end, by the steps that wait for each other before that: the top 64 of 8192 x 50257 bf16 in 249 us (3.3 TB/s), the top 256 of 2048 x 32000 in 58.  With 16 pieces
+// a thread 16 registers are spilled (8 with 256 threads and fp32) around the calls of the seldom ways, 32 or 64 bytes a thread that go to memory: 134 MB of the 139 that the
+// first of these writes, 34 of 38 of the second.
 template <int BF, int NT, int NV>
 __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, int V, int k, double inv_temp, int32_t *ids, float *values, int64_t ldk, float *rest) {
   using R = Row<BF, NT, NV>;
@@ -834,9 +840,10 @@ __global__ __launch_bounds__(NT, 4) void top_kernel(const char *x, int64_t ld, i
   if (tid == 0) rest[t] = r;
 }
 
-// The kernel whose registers hold a row.  A CU holds one workgroup of 1024 threads, two of 512 or four of 256: while every CU has a row at most, 1024 threads are through it sooner, with more rows
-// it is several rows side by side that keep the memory busy while each has its steps to wait for (drawing from the top 50, bf16: 256 x 32000 10.6 us with 1024 threads, 13.3 with 256; 512 x 32000
-// 20.4 and 17.3, 4096 x 32000 147 and 77; 4096 x 50257 172 and, with 512, 120; fp32 4096 x 16384 127 and 72, 4096 x 32000 182 and 128).  The largest 64 of a row likewise.
+// The kernel whose registers hold a row.  A CU holds one workgroup of 1024 threads, two of 512 or four of 256: while every CU has a row at most, 1024 threads are through it
+// sooner, with more rows it is several rows side by side that keep the memory busy while each has its steps to wait for (drawing from the top 50, bf16: 256 x 32000 10.6 us with
+// 1024 threads, 13.3 with 256; 512 x 32000 20.4 and 17.3, 4096 x 32000 147 and 77; 4096 x 50257 172 and, with 512, 120; fp32 4096 x 16384 127 and 72, 4096 x 32000 182 and 128).
+// The largest 64 of a row likewise.
 constexpr int kManyRows = 256;  // one for every CU
 #define ROWS_BF16(LAUNCH)                              \
   do {                                                 \

@@ -48,8 +48,8 @@ template <int BF> __device__ __forceinline__ void store1(char *row, int64_t c, f
   else reinterpret_cast<float *>(row)[c] = v;
 }
 
-// v of another lane, by the data-parallel moves of the vector unit (an eighth of what a trip through LDS takes): CTRL row_shr:1 to 8 (0x111 ..), row_bcast:15 and :31 (0x142, 0x143) for the rows of
-// ROWS; lanes that have no such neighbour get `none`.
+// v of another lane, by the data-parallel moves of the vector unit (an eighth of what a trip through LDS takes): CTRL row_shr:1 to 8 (0x111 ..), row_bcast:15 and :31 (0x142,
+// 0x143) for the rows of ROWS; lanes that have no such neighbour get `none`.
 template <int CTRL, int ROWS, class T> __device__ __forceinline__ T moved(T none, T v) {
   constexpr int W = sizeof(T) / 4;
   uint32_t a[W], b[W];
@@ -92,8 +92,8 @@ __device__ __forceinline__ float wave_max(float v) {
   return last_of(v);
 }
 
-// The row as NV pieces a thread, beginning where an address is aligned (`head` columns on); the columns before and behind the pieces, `ends` of them, are a thread's each (xl, column `end`).
-// Pieces beyond the row hold -infinity.  NV = 0: rows that NT threads cannot hold are read again for every pass.
+// The row as NV pieces a thread, beginning where an address is aligned (`head` columns on); the columns before and behind the pieces, `ends` of them, are a thread's each (xl,
+// column `end`).  Pieces beyond the row hold -infinity.  NV = 0: rows that NT threads cannot hold are read again for every pass.
 template <int BF, int NT, int NV> struct Row {
   using P16 = Piece<BF>;
   static constexpr int N = P16::N, ES = P16::ES, NW = NT / 64;
